@@ -332,6 +332,64 @@ int adore_topk_attention(const void *q, const void *k, const void *v, void *out,
 int adore_topk_attention_static(const void *q, const void *k, const void *v, void *out, int32_t rows, int32_t seq,
                                 int32_t head_dim, int32_t top_k, void *hip_stream);
 
+/* ---- Attention over whole prompts (Sec. 2.1, Eq. 1 for every token of the prompt) ----
+ * The pass that makes what adore_init_cache and the 4-bit cache below are loaded with, its gradients, and the attention
+ * every token received in it (what H2O goes by, Sec. 3.1).  Stateless: no context.  Causal, with grouped heads: query head
+ * h reads kv head h / (heads / kv_heads).
+ *   w_ij = scale q_i . k_j for j <= i + nk - nq (a sequence's last query sees its last key; with nq < nk the keys before
+ *   its first query are a prefix that is there already, with nq > nk the first queries see nothing)
+ *   lse_i = ln sum_j exp w_ij;   out_i = sum_j exp(w_ij - lse_i) v_j   (no key: out_i = 0, lse_i = -inf)
+ *   received_j = the sum of exp(w_ij - lse_i) over the queries of all heads of j's group
+ * Sequences: with q_start and k_start (both [batch + 1] i32, DEVICE) packed ones, of any lengths from 0 on: the tokens
+ * of sequence b are rows q_start[b] .. q_start[b + 1] - 1 of the q_tokens rows of q, d_out, out, dq (k_start: of the k_tokens
+ * rows of k, v, dk, dv); starts that do not rise or leave the tensor are cut off at its ends.  Outputs at rows
+ * behind the last sequence are set to zero (lse to -inf), so that a buffer may be longer than its sequences together.  Without (both NULL): `batch` sequences of q_tokens queries and k_tokens keys each.
+ * lse: fp32 [heads][q_tokens] packed, [batch][heads][q_tokens] without starts; scores alike with kv_heads and k_tokens,
+ * which for a dense batch is the layout that adore_init_cache takes as score_override in H2O mode.
+ * Products are accumulated in fp32, softmax statistics are fp32, weights and their gradients are rounded to the storage
+ * type where they enter a product; outputs are rounded once.  No atomics: equal inputs give equal bits.
+ * Calls only enqueue work on hip_stream (a hipStream_t, NULL = the default stream).
+ * Errors of all: E_INVALID (null, sizes, kv_heads that do not divide heads, a scale that is negative or not finite, one of
+ * the two starts alone, rows not on 16-byte boundaries, a negative stride or a token stride beyond 2^22 elements),
+ * E_UNSUPPORTED (head_dim not in {64,128}, more than 2^24 tokens, 4096 heads, 65536 sequences, or 2^24 blocks of 32
+ * tokens x heads), E_HIP. */
+typedef struct {
+  int32_t batch, heads, kv_heads, head_dim;
+  int32_t q_tokens, k_tokens; /* rows of the packed tensors, or tokens of every sequence */
+  int32_t dtype;              /* ADORE_F32 | ADORE_BF16: q, k, v, out and the gradients */
+  float scale;                /* 0: 1 / sqrt(head_dim) */
+} adore_prompt_config;
+
+/* Where rows are: token t of sequence b, head h at data + b * seq + (start[b] + t) * token + h * head (elements; start[b] = 0
+ * without starts), head_dim elements one behind the other. */
+typedef struct {
+  void *data; /* DEVICE, 16-byte aligned like every row */
+  int64_t seq, token, head;
+} adore_rows;
+
+/* lse may be NULL.  rest, bf16 only, may be NULL: what rounding out to bf16 left, rounded to bf16 itself; the weights then
+ * enter their product as two bf16 terms instead of one.  Handed to the backward pass it makes the gradients of rows with
+ * few or sharp weights up to 1.6 times as exact. */
+int adore_prompt_attention(const adore_prompt_config *cfg, const int32_t *q_start, const int32_t *k_start,
+                           const adore_rows *q, const adore_rows *k, const adore_rows *v, const adore_rows *out,
+                           float *lse, const adore_rows *rest, void *hip_stream);
+
+/* Gradients of sum(d_out . out) by q, k and v; dk and dv are summed over the heads of a group.  out, rest and lse as
+ * adore_prompt_attention wrote them (rest may be NULL).  workspace: DEVICE, 256-byte aligned, at least
+ * adore_prompt_backward_workspace_bytes(cfg, packed) bytes (packed != 0: with starts; 0 for a configuration that is not
+ * taken), free to reuse after the work enqueued here has run.  dq, dk, dv may not alias the inputs.
+ * Errors also: E_WORKSPACE. */
+size_t adore_prompt_backward_workspace_bytes(const adore_prompt_config *cfg, int32_t packed);
+int adore_prompt_attention_backward(const adore_prompt_config *cfg, const int32_t *q_start, const int32_t *k_start,
+                                    const adore_rows *d_out, const adore_rows *q, const adore_rows *k,
+                                    const adore_rows *v, const adore_rows *out, const adore_rows *rest, const float *lse,
+                                    const adore_rows *dq, const adore_rows *dk, const adore_rows *dv, void *workspace,
+                                    size_t workspace_bytes, void *hip_stream);
+
+/* scores (fp32): received_j.  lse as adore_prompt_attention wrote it for the same q and k. */
+int adore_prompt_scores(const adore_prompt_config *cfg, const int32_t *q_start, const int32_t *k_start,
+                        const adore_rows *q, const adore_rows *k, const float *lse, float *scores, void *hip_stream);
+
 const char *adore_strerror(int code);
 /* Debug aid for callers and tests, not a step of the method (no passage of the paper): with ADORE_GUARD_WORDS=1
  * in the environment of the process, adore_workspace_bytes and adore_create lay the workspace out with 256 bytes of

@@ -26,6 +26,7 @@ EXPORTS = [
     "adore_schedule", "adore_rebuild", "adore_decode_step", "adore_forward_step", "adore_get_state", "adore_set_state",
     "adore_set_input_order", "adore_check_guards", "adore_set_timing", "adore_read_timing", "adore_kernel_name", "adore_strerror", "adore_abi_version",
     "adore_topk_attention_workspace_bytes", "adore_topk_attention", "adore_topk_attention_static",
+    "adore_prompt_attention", "adore_prompt_backward_workspace_bytes", "adore_prompt_attention_backward", "adore_prompt_scores",
 ]
 
 
@@ -47,6 +48,15 @@ class AdoreWeights(ctypes.Structure):
 
 class AdoreForwardWeights(ctypes.Structure):
     _fields_ = [("w_q", ctypes.c_void_p), ("w_o", ctypes.c_void_p)]
+
+
+class AdorePromptConfig(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in
+                ("batch", "heads", "kv_heads", "head_dim", "q_tokens", "k_tokens", "dtype")] + [("scale", ctypes.c_float)]
+
+
+class AdoreRows(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p)] + [(n, ctypes.c_int64) for n in ("seq", "token", "head")]
 
 
 class AdoreError(RuntimeError):
@@ -112,6 +122,15 @@ def load_library() -> ctypes.CDLL:
     lib.adore_topk_attention.argtypes = [vp, vp, vp, vp, vp, sz, i32, i32, i32, i32, vp]
     lib.adore_topk_attention_static.restype = ctypes.c_int
     lib.adore_topk_attention_static.argtypes = [vp, vp, vp, vp, i32, i32, i32, i32, vp]
+    cfg, rows = ctypes.POINTER(AdorePromptConfig), ctypes.POINTER(AdoreRows)
+    lib.adore_prompt_attention.restype = ctypes.c_int
+    lib.adore_prompt_attention.argtypes = [cfg, vp, vp, rows, rows, rows, rows, vp, rows, vp]
+    lib.adore_prompt_backward_workspace_bytes.restype = sz
+    lib.adore_prompt_backward_workspace_bytes.argtypes = [cfg, i32]
+    lib.adore_prompt_attention_backward.restype = ctypes.c_int
+    lib.adore_prompt_attention_backward.argtypes = [cfg, vp, vp] + [rows] * 6 + [vp] + [rows] * 3 + [vp, sz, vp]
+    lib.adore_prompt_scores.restype = ctypes.c_int
+    lib.adore_prompt_scores.argtypes = [cfg, vp, vp, rows, rows, vp, vp, vp]
     _lib = lib
     return lib
 
@@ -163,6 +182,121 @@ def topk_attention_static(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, top
     _check(lib, lib.adore_topk_attention_static(q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), rows, seq, d,
                                                 int(top_k), stream))
     return out
+
+
+_CODES = {torch.float32: ADORE_F32, torch.bfloat16: ADORE_BF16}
+
+
+class _Prompts:
+    """The sequences and heads of a call on prompts, read off q and k, and its tensors' descriptions.
+
+    With starts, q is [q tokens, heads, head_dim] and k [k tokens, kv heads, head_dim]; without, [batch, heads, tokens, head_dim].
+    The last dimension is dense, the others may have any strides that keep every row on a 16-byte boundary."""
+
+    def __init__(self, q: torch.Tensor, k: torch.Tensor, q_start, k_start, scale):
+        if (q_start is None) != (k_start is None):
+            raise ValueError("q_start and k_start: both or neither")
+        self.packed, self.device, self.dtype = q_start is not None, q.device, q.dtype
+        if q.dtype not in _CODES or not q.is_cuda:
+            raise ValueError(f"q: expected a bf16 or fp32 GPU tensor, got {q.device} {q.dtype}")
+        dims = 3 if self.packed else 4
+        if q.dim() != dims or k.dim() != dims:
+            raise ValueError("q, k: expected [tokens, heads, head_dim] with starts, [batch, heads, tokens, head_dim] without")
+        heads, tokens = (1, 0) if self.packed else (1, 2)
+        self.starts = []
+        for name, t in (("q_start", q_start), ("k_start", k_start)):
+            if t is None:
+                self.starts.append(None)
+            elif t.dtype != torch.int32 or t.device != q.device or t.dim() != 1 or not t.is_contiguous() or t.numel() < 2 or \
+                    t.numel() != q_start.numel():
+                raise ValueError(f"{name}: expected contiguous int32 [batch + 1] on q's device")
+            else:
+                self.starts.append(t.data_ptr())
+        self.batch = q_start.numel() - 1 if self.packed else q.shape[0]
+        self.q_shape, self.k_shape = tuple(q.shape), tuple(k.shape)
+        if scale is None:
+            scale = 0.0
+        elif not scale > 0.0:
+            raise ValueError("scale: expected a positive number")
+        self.cfg = AdorePromptConfig(self.batch, q.shape[heads], k.shape[heads], q.shape[-1], q.shape[tokens], k.shape[tokens],
+                                     _CODES[q.dtype], float(scale))
+        self.q_rows = (q.shape[1], q.shape[0]) if self.packed else tuple(q.shape[:3])     # of one value per row: lse
+        self.k_rows = (k.shape[1], k.shape[0]) if self.packed else tuple(k.shape[:3])
+
+    def rows(self, t: torch.Tensor, shape, name: str, written: bool = False):
+        if not isinstance(t, torch.Tensor) or t.device != self.device or t.dtype != self.dtype or tuple(t.shape) != shape or \
+                (t.shape[-1] > 1 and t.stride(-1) != 1):
+            raise ValueError(f"{name}: expected a {self.dtype} tensor of shape {shape} on {self.device}, its last dimension dense")
+        stride = [0 if n <= 1 else s for n, s in zip(t.shape, t.stride())]
+        if written and any(n > 1 and s == 0 for n, s in zip(t.shape, stride)):
+            raise ValueError(f"{name}: its rows lie on one another")
+        where = (0, stride[0], stride[1]) if self.packed else (stride[0], stride[2], stride[1])
+        # an empty tensor has no address, and no row of it is touched
+        return ctypes.byref(AdoreRows(t.data_ptr() or 16, *where))
+
+    def values(self, t: torch.Tensor, shape, name: str):
+        if not isinstance(t, torch.Tensor) or t.device != self.device or t.dtype != torch.float32 or tuple(t.shape) != shape or \
+                not t.is_contiguous():
+            raise ValueError(f"{name}: expected contiguous fp32 of shape {shape} on {self.device}")
+        return t.data_ptr() or 16
+
+    @property
+    def stream(self):
+        return torch.cuda.current_stream(self.device).cuda_stream
+
+
+def prompt_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, *, q_start: torch.Tensor = None,
+                     k_start: torch.Tensor = None, scale: float = None, out: torch.Tensor = None, rest: bool = False):
+    """adore_prompt_attention on torch's current stream: causal attention over whole prompts; returns (out, lse), and with rest=True
+    (out, lse, rest) for the backward pass (rest is None where out is fp32 and nothing is lost).
+
+    Packed sequences: q [q tokens, heads, head_dim], k and v [k tokens, kv heads, head_dim], q_start and k_start int32
+    [batch + 1] on the GPU.  A dense batch: [batch, heads, tokens, head_dim] without starts.  bf16 or fp32, any strides with a
+    dense last dimension (q, k and v may be views of one projection).  out is allocated here unless given."""
+    lib = load_library()
+    p = _Prompts(q, k, q_start, k_start, scale)
+    if out is None:
+        out = torch.empty(p.q_shape, dtype=q.dtype, device=q.device)
+    lse = torch.empty(p.q_rows, dtype=torch.float32, device=q.device)
+    left = torch.empty(p.q_shape, dtype=q.dtype, device=q.device) if rest and q.dtype == torch.bfloat16 else None
+    _check(lib, lib.adore_prompt_attention(ctypes.byref(p.cfg), *p.starts, p.rows(q, p.q_shape, "q"), p.rows(k, p.k_shape, "k"),
+                                           p.rows(v, p.k_shape, "v"), p.rows(out, p.q_shape, "out", True), p.values(lse, p.q_rows, "lse"),
+                                           None if left is None else p.rows(left, p.q_shape, "rest", True), p.stream))
+    return (out, lse, left) if rest else (out, lse)
+
+
+def prompt_attention_backward(d_out: torch.Tensor, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, out: torch.Tensor,
+                              lse: torch.Tensor, *, rest: torch.Tensor = None, q_start: torch.Tensor = None,
+                              k_start: torch.Tensor = None, scale: float = None, dq: torch.Tensor = None, dk: torch.Tensor = None,
+                              dv: torch.Tensor = None):
+    """adore_prompt_attention_backward on torch's current stream: (dq, dk, dv) of sum(d_out * out).  out, lse and rest as
+    prompt_attention returned them for these q, k, v, starts and scale; dq, dk, dv are allocated here unless given (the places of
+    q, k and v in the gradient of one projection, say)."""
+    lib = load_library()
+    p = _Prompts(q, k, q_start, k_start, scale)
+    dq, dk, dv = (torch.empty(s, dtype=q.dtype, device=q.device) if t is None else t
+                  for t, s in ((dq, p.q_shape), (dk, p.k_shape), (dv, p.k_shape)))
+    need = lib.adore_prompt_backward_workspace_bytes(ctypes.byref(p.cfg), int(p.packed))
+    workspace = torch.empty(max(need, 1), dtype=torch.uint8, device=q.device)
+    _check(lib, lib.adore_prompt_attention_backward(
+        ctypes.byref(p.cfg), *p.starts, p.rows(d_out, p.q_shape, "d_out"), p.rows(q, p.q_shape, "q"), p.rows(k, p.k_shape, "k"),
+        p.rows(v, p.k_shape, "v"), p.rows(out, p.q_shape, "out"), None if rest is None else p.rows(rest, p.q_shape, "rest"),
+        p.values(lse, p.q_rows, "lse"), p.rows(dq, p.q_shape, "dq", True), p.rows(dk, p.k_shape, "dk", True),
+        p.rows(dv, p.k_shape, "dv", True), workspace.data_ptr(), need, p.stream))
+    return dq, dk, dv
+
+
+def prompt_scores(q: torch.Tensor, k: torch.Tensor, lse: torch.Tensor, *, q_start: torch.Tensor = None, k_start: torch.Tensor = None,
+                  scale: float = None, scores: torch.Tensor = None) -> torch.Tensor:
+    """adore_prompt_scores on torch's current stream: the attention every key received from the queries of its group's heads, fp32
+    [kv heads, k tokens] (packed) or [batch, kv heads, tokens].  lse as prompt_attention returned it."""
+    lib = load_library()
+    p = _Prompts(q, k, q_start, k_start, scale)
+    if scores is None:
+        scores = torch.empty(p.k_rows, dtype=torch.float32, device=q.device)
+    _check(lib, lib.adore_prompt_scores(ctypes.byref(p.cfg), *p.starts, p.rows(q, p.q_shape, "q"), p.rows(k, p.k_shape, "k"),
+                                        p.values(lse, p.q_rows, "lse"), p.values(scores, p.k_rows, "scores"), p.stream))
+    return scores
 
 
 class Adore:

@@ -1,0 +1,408 @@
+// Causal attention over whole prompts (paper Sec. 2.1, Eq. 1 for every token of the prompt) and the attention every key receives
+// (Sec. 3.1, baseline 6: what H2O goes by), for packed sequences of any lengths and grouped heads.
+//
+//   w_ij = scale q_i . k_j,   j <= i + nk - nq;   lse_i = ln sum_j exp w_ij;   out_i = sum_j exp(w_ij - lse_i) v_j
+//   received_j = sum over the query heads of j's group and their queries i of exp(w_ij - lse_i)
+//
+// Forward: a workgroup of four waves takes 128 queries of a head, a wave 32 of them, and goes over the keys once, tile by tile, with
+// the running maximum and sum of the softmax (fp32).  S^T = K Q^T leaves a query's weights in two lanes, so the maximum is a tree
+// over a lane's registers and one exchange, and P^T is already the right operand of O^T += V^T P^T; V comes out of LDS
+// transposed.  P is rounded to the storage type, like every tensor the matrix cores take; its sum is not.
+#include <hip/hip_runtime.h>
+
+#include <cmath>
+
+#include "prompt_device.h"
+
+namespace adore {
+
+namespace {
+
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr double kLn2 = 0.6931471805599453;
+
+template <typename T>
+struct AttendArgs {
+  PromptShape s;
+  Rows<const T> q, k, v;
+  Rows<T> out, rest;      // rest.p may be null
+  float *lse;             // or null
+};
+
+// Keys of a tile: 16 KB of K and as much of V at head dimension 128.
+template <typename T>
+constexpr int kKeys = sizeof(T) == 2 ? 64 : 32;
+
+// REST: P goes in as two bf16 terms (within 2^-16) and what rounding out leaves is handed out, for a backward pass whose delta is as good
+// as its other terms.
+template <typename T, int DH, bool REST>
+__global__ __launch_bounds__(256, 2) void prompt_attend_kernel(const AttendArgs<T> a) {
+  constexpr int NT = 256, BQ = 128, KT = kKeys<T>, KB = KT / 32, DB = DH / 32, ST = DH / 16;
+  typedef Tile<T, DH> L;
+  typedef typename Operand<T>::type Frag;
+  constexpr int kTile = KT * L::kRow;
+  extern __shared__ __align__(16) unsigned char smem[];   // K 0, K 1, V 0, V 1; at the end the outputs
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), c = lane & 31, h = lane >> 5;
+  // kv head fastest: with a multiple of eight of them a head's workgroups share an XCD and its L2
+  const int hk = blockIdx.x % a.s.kv_heads, item = blockIdx.x / a.s.kv_heads, head = hk * a.s.group + item % a.s.group;
+  Sequence sq;
+  int block;
+  if (!find_block<BQ, true>(a.s, item / a.s.group, sq, block)) {
+    int first;
+    const int n = tail_rows<BQ>(a.s.q_start, a.s.batch, a.s.q_tokens, block, first);
+    zero_rows<T, DH>(a.out, head, first, n, tid, NT);
+    if (REST) zero_rows<T, DH>(a.rest, head, first, n, tid, NT);
+    if (a.lse && tid < n) a.lse[size_t(head) * a.s.q_tokens + first + tid] = -INFINITY;
+    return;
+  }
+  block = (sq.nq + BQ - 1) / BQ - 1 - block;   // the longest first
+  const int q0 = block * BQ + wave * 32, off = sq.nk - sq.nq;
+  const int rows = min(32, sq.nq - q0);        // may be <= 0
+  const char *kp = reinterpret_cast<const char *>(a.k.p + sq.b * a.k.seq + sq.k_first * a.k.token + hk * a.k.head);
+  const char *vp = reinterpret_cast<const char *>(a.v.p + sq.b * a.v.seq + sq.k_first * a.v.token + hk * a.v.head);
+  const int64_t ks = a.k.token * int64_t(sizeof(T)), vs = a.v.token * int64_t(sizeof(T));
+
+  // the query operand, through the wave's own quarter of LDS (4 x 32 rows: 16 KB, or 32, of the 64)
+  Frag qf[ST];
+  {
+    unsigned char *own = smem + wave * (32 * L::kRow);
+    const char *qp = reinterpret_cast<const char *>(a.q.p + sq.b * a.q.seq + (int64_t(sq.q_first) + q0) * a.q.token + head * a.q.head);
+    Carrier<T, DH, 32, 64> cq;
+    if (rows > 0) {
+      cq.template load<true>(qp, a.q.token * int64_t(sizeof(T)), 0, rows, lane);
+      cq.store(own, lane);
+    }
+    wave_lds_fence();
+#pragma unroll
+    for (int t = 0; t < ST; ++t) qf[t] = L::by_row(own, c, t, h);
+    __syncthreads();
+  }
+
+  f32x16 o[DB];
+#pragma unroll
+  for (int db = 0; db < DB; ++db) o[db] = f32x16{0.f};
+  float top = -INFINITY, sum = 0.f;             // of the lane's query: running maximum of the products, sum of its share of the keys
+  const int last = min(block * BQ + BQ, sq.nq) - 1 + off;             // the last key that a query of the workgroup sees
+  const int tiles = last < 0 ? 0 : last / KT + 1;
+  const int mine = rows > 0 ? q0 + rows - 1 + off : -1;               // ... of the wave
+  const int seen = q0 + c + off;                                      // ... of the lane
+  const float scale = a.s.scale_log2;
+  Carrier<T, DH, KT, NT> ck, cv;
+  if (tiles > 0) {
+    ck.template load<false>(kp, ks, 0, sq.nk, tid);
+    cv.template load<true>(vp, vs, 0, sq.nk, tid);
+    ck.store(smem, tid);
+    cv.store(smem + 2 * kTile, tid);
+  }
+  for (int it = 0; it < tiles; ++it) {
+    const unsigned char *kt = smem + (it & 1) * kTile, *vt = kt + 2 * kTile;
+    const int k0 = it * KT;
+    __syncthreads();
+    if (it + 1 < tiles) {
+      ck.template load<false>(kp, ks, k0 + KT, sq.nk, tid);
+      cv.template load<true>(vp, vs, k0 + KT, sq.nk, tid);
+    }
+    if (k0 <= mine) {
+      f32x16 s[KB];
+#pragma unroll
+      for (int kb = 0; kb < KB; ++kb) {
+        s[kb] = f32x16{0.f};
+#pragma unroll
+        for (int t = 0; t < ST; ++t) s[kb] = Operand<T>::mma(L::by_row(kt, kb * 32 + c, t, h), qf[t], s[kb]);
+      }
+      if (k0 + KT - 1 > q0 + off) {             // some of the wave's queries do not see all of the tile
+#pragma unroll
+        for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+          for (int r = 0; r < 16; ++r)
+            if (k0 + kb * 32 + 8 * (r >> 2) + 4 * h + (r & 3) > seen) s[kb][r] = -INFINITY;
+      }
+      float m = s[0][0];
+#pragma unroll
+      for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) m = fmaxf(m, s[kb][r]);
+      m = fmaxf(top, max_lane_xor<32>(m));
+      const float base = m == -INFINITY ? 0.f : -m * scale;           // a query that has seen nothing yet
+      if (__builtin_amdgcn_ballot_w64(m > top)) {
+        const float fade = __builtin_amdgcn_exp2f(fmaf(top, scale, base));
+        sum *= fade;
+#pragma unroll
+        for (int db = 0; db < DB; ++db)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) o[db][r] *= fade;
+        top = m;
+      }
+      Frag pf[KB][2];
+      float part[4] = {0.f};                    // a tile's weights first, so that few additions round the running sum
+#pragma unroll
+      for (int kb = 0; kb < KB; ++kb) {
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          s[kb][r] = __builtin_amdgcn_exp2f(fmaf(s[kb][r], scale, base));
+          part[r & 3] += s[kb][r];
+        }
+        pf[kb][0] = Operand<T>::of(s[kb], 0);
+        pf[kb][1] = Operand<T>::of(s[kb], 1);
+      }
+      sum += (part[0] + part[1]) + (part[2] + part[3]);
+#pragma unroll
+      for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+          for (int db = 0; db < DB; ++db) {
+            const Frag vf = L::transposed(vt, kb * 32, t, db, lane);
+            o[db] = Operand<T>::mma(vf, pf[kb][t], o[db]);
+            if constexpr (REST) o[db] = Operand<T>::mma(vf, Operand<T>::rest_of(s[kb], pf[kb][t], t), o[db]);
+          }
+    }
+    if (it + 1 < tiles) {
+      unsigned char *next = smem + (~it & 1) * kTile;
+      ck.store(next, tid);
+      cv.store(next + 2 * kTile, tid);
+    }
+  }
+  __syncthreads();
+  if (rows <= 0) return;
+  sum = add_lane_xor<32>(sum);
+  const bool some = sum > 0.f || sum != sum;    // (a query without keys: zeros, and -inf)
+  if (a.lse && lane < rows) {
+    const size_t at = row_value(a.s.q_start != nullptr, sq.b, sq.q_first, a.s.q_tokens, a.s.heads, head);
+    // the exponents are relative to the rounded top * scale; added up in 64 bits, rounded once
+    a.lse[at + q0 + lane] = some ? float(double(top * scale) * kLn2 + log(double(sum))) : -INFINITY;
+  }
+  const int64_t row = int64_t(sq.q_first) + q0;
+  char *op = reinterpret_cast<char *>(a.out.p + sq.b * a.out.seq + row * a.out.token + head * a.out.head);
+  char *rp = REST ? reinterpret_cast<char *>(a.rest.p + sq.b * a.rest.seq + row * a.rest.token + head * a.rest.head) : nullptr;
+  store_rows<T, DH>(o, some ? 1.f / sum : 0.f, smem + wave * (32 * L::kRow), op, a.out.token * int64_t(sizeof(T)), rows, rp,
+                    a.rest.token * int64_t(sizeof(T)), lane);
+}
+
+template <typename T, int DH, bool REST>
+hipError_t launch_attend_prompt(const AttendArgs<T> &a, hipStream_t st) {
+  constexpr int lds = 4 * kKeys<T> * Tile<T, DH>::kRow;
+  const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(&prompt_attend_kernel<T, DH, REST>),
+                                           hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+  if (e != hipSuccess) return e;
+  const long long blocks = blocks_at_most(a.s.q_start, a.s.batch, a.s.q_tokens, 128) * a.s.heads;
+  hipLaunchKernelGGL((prompt_attend_kernel<T, DH, REST>), dim3(unsigned(blocks)), dim3(256), lds, st, a);
+  return hipGetLastError();
+}
+
+// ---- the attention every key received -----------------------------------------------------------------------------
+// A workgroup takes 128 keys of a kv head, a wave 32 of them, and goes over the queries that see them, of all heads of the group:
+// S = Q K^T leaves a key's weights in two lanes, which add them up.  No atomics: the order of the sum is fixed.
+template <typename T>
+struct ScoreArgs {
+  PromptShape s;
+  Rows<const T> q, k;
+  const float *lse;
+  float *scores;
+};
+
+template <typename T>
+constexpr int kQueries = sizeof(T) == 2 ? 64 : 32;
+
+template <typename T, int DH>
+__global__ __launch_bounds__(256, 2) void prompt_scores_kernel(const ScoreArgs<T> a) {
+  constexpr int NT = 256, BK = 128, QT = kQueries<T>, QB = QT / 32, ST = DH / 16;
+  typedef Tile<T, DH> L;
+  typedef typename Operand<T>::type Frag;
+  constexpr int kTile = QT * L::kRow;
+  extern __shared__ __align__(16) unsigned char smem[];   // Q 0, Q 1
+  __shared__ __align__(16) float s_lse[2][QT];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), c = lane & 31, h = lane >> 5;
+  const int hk = blockIdx.x % a.s.kv_heads;
+  Sequence sq;
+  int block;
+  if (!find_block<BK, false>(a.s, blockIdx.x / a.s.kv_heads, sq, block)) {
+    int first;
+    const int n = tail_rows<BK>(a.s.k_start, a.s.batch, a.s.k_tokens, block, first);
+    if (tid < n) a.scores[size_t(hk) * a.s.k_tokens + first + tid] = 0.f;
+    return;
+  }
+  const int k0 = block * BK + wave * 32, off = sq.nk - sq.nq;
+  const int rows = min(32, sq.nk - k0);
+  Frag kf[ST];
+  {
+    unsigned char *own = smem + wave * (32 * L::kRow);
+    const char *kp = reinterpret_cast<const char *>(a.k.p + sq.b * a.k.seq + (int64_t(sq.k_first) + k0) * a.k.token + hk * a.k.head);
+    Carrier<T, DH, 32, 64> cc;
+    if (rows > 0) {
+      cc.template load<true>(kp, a.k.token * int64_t(sizeof(T)), 0, rows, lane);
+      cc.store(own, lane);
+    }
+    wave_lds_fence();
+#pragma unroll
+    for (int t = 0; t < ST; ++t) kf[t] = L::by_row(own, c, t, h);
+    __syncthreads();
+  }
+  const int first = max(block * BK - off, 0) / QT * QT;    // the first tile with a query that sees a key of the workgroup
+  const int per = first < sq.nq ? (sq.nq - first + QT - 1) / QT : 0, tiles = per * a.s.group;
+  const int64_t qs = a.q.token * int64_t(sizeof(T));
+  const float scale = a.s.scale_log2;
+  const bool packed = a.s.q_start != nullptr;
+  float sum = 0.f;
+  Carrier<T, DH, QT, NT> cq;
+  float row_lse = 0.f;
+  auto load = [&](int it) {
+    const int head = hk * a.s.group + it / per, q0 = first + it % per * QT;
+    const char *qp = reinterpret_cast<const char *>(a.q.p + sq.b * a.q.seq + sq.q_first * a.q.token + head * a.q.head);
+    cq.template load<false>(qp, qs, q0, sq.nq, tid);
+    if (tid < QT)
+      row_lse = q0 + tid < sq.nq ? a.lse[row_value(packed, sq.b, sq.q_first, a.s.q_tokens, a.s.heads, head) + q0 + tid] * kLog2e : INFINITY;
+  };
+  auto store = [&](int it) {
+    cq.store(smem + (it & 1) * kTile, tid);
+    if (tid < QT) s_lse[it & 1][tid] = row_lse;
+  };
+  if (tiles > 0) {
+    load(0);
+    store(0);
+  }
+  for (int it = 0; it < tiles; ++it) {
+    const unsigned char *qt = smem + (it & 1) * kTile;
+    const int q0 = first + it % per * QT;
+    __syncthreads();
+    if (it + 1 < tiles) load(it + 1);
+    float part = 0.f;
+#pragma unroll
+    for (int qb = 0; qb < QB; ++qb) {
+      if (q0 + qb * 32 + 31 + off < k0) continue;      // none of these queries sees the wave's keys
+      f32x16 s = {0.f};
+#pragma unroll
+      for (int t = 0; t < ST; ++t) s = Operand<T>::mma(L::by_row(qt, qb * 32 + c, t, h), kf[t], s);
+      const bool partly = q0 + qb * 32 + off < k0 + 31;
+#pragma unroll
+      for (int r4 = 0; r4 < 4; ++r4) {
+        const f32x4 lse = *reinterpret_cast<const f32x4 *>(&s_lse[it & 1][qb * 32 + 8 * r4 + 4 * h]);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int q = q0 + qb * 32 + 8 * r4 + 4 * h + i;
+          const float p = __builtin_amdgcn_exp2f(fmaf(s[4 * r4 + i], scale, -lse[i]));
+          part += (partly && k0 + c > q + off) ? 0.f : p;
+        }
+      }
+    }
+    sum += part;
+    if (it + 1 < tiles) store(it + 1);
+  }
+  sum = add_lane_xor<32>(sum);
+  if (lane < rows) a.scores[row_value(packed, sq.b, sq.k_first, a.s.k_tokens, a.s.kv_heads, hk) + k0 + lane] = sum;
+}
+
+template <typename T, int DH>
+hipError_t launch_scores(const ScoreArgs<T> &a, hipStream_t st) {
+  constexpr int tiles = 2 * kQueries<T> * Tile<T, DH>::kRow, keys = 128 * Tile<T, DH>::kRow, lds = tiles > keys ? tiles : keys;
+  const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(&prompt_scores_kernel<T, DH>),
+                                           hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+  if (e != hipSuccess) return e;
+  const long long blocks = blocks_at_most(a.s.k_start, a.s.batch, a.s.k_tokens, 128) * a.s.kv_heads;
+  hipLaunchKernelGGL((prompt_scores_kernel<T, DH>), dim3(unsigned(blocks)), dim3(256), lds, st, a);
+  return hipGetLastError();
+}
+
+template <typename T>
+int attend_typed(const adore_prompt_config &c, const PromptShape &s, const adore_rows *q, const adore_rows *k, const adore_rows *v,
+                 const adore_rows *out, float *lse, const adore_rows *rest, hipStream_t st) {
+  AttendArgs<T> a;
+  a.s = s;
+  a.q = rows_of<const T>(q);
+  a.k = rows_of<const T>(k);
+  a.v = rows_of<const T>(v);
+  a.out = rows_of<T>(out);
+  a.rest = rest ? rows_of<T>(rest) : Rows<T>{nullptr, 0, 0, 0};
+  a.lse = lse;
+  hipError_t e;
+  if constexpr (sizeof(T) == 2) {
+    if (rest)
+      e = c.head_dim == 128 ? launch_attend_prompt<T, 128, true>(a, st) : launch_attend_prompt<T, 64, true>(a, st);
+    else
+      e = c.head_dim == 128 ? launch_attend_prompt<T, 128, false>(a, st) : launch_attend_prompt<T, 64, false>(a, st);
+  } else {
+    e = c.head_dim == 128 ? launch_attend_prompt<T, 128, false>(a, st) : launch_attend_prompt<T, 64, false>(a, st);
+  }
+  return e == hipSuccess ? ADORE_OK : ADORE_E_HIP;
+}
+
+template <typename T>
+int scores_typed(const adore_prompt_config &c, const PromptShape &s, const adore_rows *q, const adore_rows *k, const float *lse,
+                 float *scores, hipStream_t st) {
+  ScoreArgs<T> a;
+  a.s = s;
+  a.q = rows_of<const T>(q);
+  a.k = rows_of<const T>(k);
+  a.lse = lse;
+  a.scores = scores;
+  const hipError_t e = c.head_dim == 128 ? launch_scores<T, 128>(a, st) : launch_scores<T, 64>(a, st);
+  return e == hipSuccess ? ADORE_OK : ADORE_E_HIP;
+}
+
+}  // namespace
+
+// The checks that every call on prompts makes; fills in what the kernels take.
+int prompt_shape(const adore_prompt_config *c, const int32_t *q_start, const int32_t *k_start, PromptShape *s) {
+  if (!c || (q_start == nullptr) != (k_start == nullptr)) return ADORE_E_INVALID;
+  if (c->batch <= 0 || c->heads <= 0 || c->kv_heads <= 0 || c->heads % c->kv_heads != 0 || c->q_tokens < 0 || c->k_tokens < 0 ||
+      (c->dtype != ADORE_F32 && c->dtype != ADORE_BF16) || !std::isfinite(c->scale) || c->scale < 0.f || c->head_dim <= 0)
+    return ADORE_E_INVALID;
+  if (c->head_dim != 64 && c->head_dim != 128) return ADORE_E_UNSUPPORTED;
+  // row and workgroup counts far inside 32 bits
+  constexpr int kMostTokens = 1 << 24, kMostHeads = 1 << 12, kMostBatch = 1 << 16;
+  if (c->q_tokens > kMostTokens || c->k_tokens > kMostTokens || c->heads > kMostHeads || c->batch > kMostBatch) return ADORE_E_UNSUPPORTED;
+  const long long rows = c->q_tokens > c->k_tokens ? c->q_tokens : c->k_tokens;
+  if (blocks_at_most(q_start, c->batch, int(rows), 32) * c->heads > (1ll << 24)) return ADORE_E_UNSUPPORTED;
+  s->q_start = q_start;
+  s->k_start = k_start;
+  s->batch = c->batch;
+  s->heads = c->heads;
+  s->kv_heads = c->kv_heads;
+  s->group = c->heads / c->kv_heads;
+  s->q_tokens = c->q_tokens;
+  s->k_tokens = c->k_tokens;
+  s->scale = c->scale > 0.f ? c->scale : 1.f / sqrtf(float(c->head_dim));
+  s->scale_log2 = s->scale * kLog2e;
+  return ADORE_OK;
+}
+
+// A tensor of rows: present, and every row on a 16-byte boundary.
+bool prompt_rows_ok(const adore_rows *r, int dtype) {
+  if (!r || !r->data || (reinterpret_cast<uintptr_t>(r->data) & 15)) return false;
+  const int64_t unit = dtype == ADORE_BF16 ? 8 : 4, most = int64_t(1) << 22;
+  return r->seq >= 0 && r->token >= 0 && r->head >= 0 && r->seq % unit == 0 && r->token % unit == 0 && r->head % unit == 0 && r->token <= most;
+}
+
+}  // namespace adore
+
+extern "C" {
+
+int adore_prompt_attention(const adore_prompt_config *cfg, const int32_t *q_start, const int32_t *k_start, const adore_rows *q,
+                           const adore_rows *k, const adore_rows *v, const adore_rows *out, float *lse, const adore_rows *rest,
+                           void *hip_stream) {
+  using namespace adore;
+  PromptShape s;
+  const int rc = prompt_shape(cfg, q_start, k_start, &s);
+  if (rc != ADORE_OK) return rc;
+  if (!prompt_rows_ok(q, cfg->dtype) || !prompt_rows_ok(k, cfg->dtype) || !prompt_rows_ok(v, cfg->dtype) ||
+      !prompt_rows_ok(out, cfg->dtype) || (rest && (cfg->dtype != ADORE_BF16 || !prompt_rows_ok(rest, cfg->dtype))))
+    return ADORE_E_INVALID;
+  if (s.q_tokens == 0) return ADORE_OK;
+  const hipStream_t st = static_cast<hipStream_t>(hip_stream);
+  return cfg->dtype == ADORE_BF16 ? attend_typed<bf16_t>(*cfg, s, q, k, v, out, lse, rest, st)
+                                  : attend_typed<float>(*cfg, s, q, k, v, out, lse, rest, st);
+}
+
+int adore_prompt_scores(const adore_prompt_config *cfg, const int32_t *q_start, const int32_t *k_start, const adore_rows *q,
+                        const adore_rows *k, const float *lse, float *scores, void *hip_stream) {
+  using namespace adore;
+  PromptShape s;
+  const int rc = prompt_shape(cfg, q_start, k_start, &s);
+  if (rc != ADORE_OK) return rc;
+  if (!prompt_rows_ok(q, cfg->dtype) || !prompt_rows_ok(k, cfg->dtype) || !lse || !scores) return ADORE_E_INVALID;
+  if (s.k_tokens == 0) return ADORE_OK;
+  const hipStream_t st = static_cast<hipStream_t>(hip_stream);
+  return cfg->dtype == ADORE_BF16 ? scores_typed<bf16_t>(*cfg, s, q, k, lse, scores, st) : scores_typed<float>(*cfg, s, q, k, lse, scores, st);
+}
+
+}  // extern "C"
