@@ -390,6 +390,54 @@ int adore_prompt_attention_backward(const adore_prompt_config *cfg, const int32_
 int adore_prompt_scores(const adore_prompt_config *cfg, const int32_t *q_start, const int32_t *k_start,
                         const adore_rows *q, const adore_rows *k, const float *lse, float *scores, void *hip_stream);
 
+/* ---- A cache held in 4 bits, evicted by the attention its rows received (Sec. 3.1, baseline 6: H2O) ----
+ * For prompts and answers whose cache should be small: 17/32 of a byte per element instead of 2 or 4, and `slots` rows per
+ * (sequence, kv head), of which each holds its own tokens.  Stateless calls over four buffers of the caller's (DEVICE):
+ *   cache     adore_q4_cache_bytes, 256-byte aligned: blocks of 64 slots, [batch][kv_heads][ceil(slots / 64)][68 * head_dim]
+ *             bytes, laid out as csrc/q4_cache.hip says
+ *   slot_pos  [batch][kv_heads][slots] i32: position of the token in the slot, -1 = free
+ *   score     [batch][kv_heads][slots] fp32: the attention the slot's token has received, from all query heads of the group
+ *   cursor    [batch][kv_heads][2] i32: the slot that the next token takes, its position
+ * slot_pos, score 16-byte aligned, cursor 8.  An empty cache: slot_pos -1, score 0, cursor 0.
+ * Values: 32 neighbouring elements of a row share a power of two, such that the largest of them is in (3.5, 7] of its
+ * units (exponents from -100 to 125); an element is the nearest of 0, +-0.5, 1, 1.5, 2, 3, 4, 6 units, ties to the one with the even
+ * code, larger ones to 6.  A NaN is held as 0.
+ * Eviction: the next token takes the lowest free slot; a full row's next one to go is the token with the lowest score,
+ * equal scores the lowest slot (in adore_q4_fill: position), never one of the `recent` last tokens.  (Elsewhere in this library equal
+ * scores keep the older token; here tokens that received nothing make room for newer ones.)  A NaN score counts as 0.
+ * Errors of all: E_INVALID (null, sizes, slots < 2, recent outside 1 .. slots - 1, a negative or infinite scale, misaligned
+ * buffers), E_UNSUPPORTED (head_dim not in {64,128}, slots > 2^20, batch > 2^16, heads > 2^12, batch * kv_heads * blocks > 2^23,
+ * batch * heads > 2^20), E_HIP. */
+typedef struct {
+  int32_t batch, heads, kv_heads, head_dim;
+  int32_t slots, recent;
+  int32_t dtype; /* ADORE_F32 | ADORE_BF16: q, k, v and outputs */
+  float scale;   /* 0: 1 / sqrt(head_dim) */
+} adore_q4_config;
+size_t adore_q4_cache_bytes(const adore_q4_config *cfg);     /* HOST calls; 0 for a configuration that is not taken */
+size_t adore_q4_workspace_bytes(const adore_q4_config *cfg); /* of adore_q4_step */
+
+/* Loads prompts, by the eviction rule at once: of a sequence's n tokens the last `recent` and the best slots - recent of the
+ * others stay (all if n <= slots), in slots of ascending position.  k, v as in adore_prompt_attention: packed with k_start
+ * (k_tokens rows in all), or k_tokens per sequence.  scores (may be NULL: all 0): as adore_prompt_scores wrote them. */
+int adore_q4_fill(const adore_q4_config *cfg, const int32_t *k_start, int32_t k_tokens, const adore_rows *k,
+                  const adore_rows *v, const float *scores, void *cache, int32_t *slot_pos, float *score, int32_t *cursor,
+                  void *hip_stream);
+
+/* One token: k_new, v_new [batch][kv_heads][head_dim] go into the cursor's slots (score 0), then
+ *   out[b][h][:] = sum_s softmax_s(scale q[b][h] . K[s]) V[s]   over the occupied slots, the new one as it is held,
+ * q, out [batch][heads][head_dim] storage type; every slot's score grows by the weights its group's heads gave it (fp32), and the
+ * cursor moves to the next token.  k_held, v_held [batch][kv_heads][head_dim] or NULL: the new row as it is held.
+ * bf16: products are exact, a weight times its power of two is within 2^-16; fp32: 2^-23.
+ * workspace: 256-byte aligned, at least adore_q4_workspace_bytes(cfg) bytes, free to reuse after the work enqueued here has run.
+ * Errors also: E_WORKSPACE. */
+int adore_q4_step(const adore_q4_config *cfg, const void *q, const void *k_new, const void *v_new, void *cache,
+                  int32_t *slot_pos, float *score, int32_t *cursor, void *out, void *k_held, void *v_held, void *workspace,
+                  size_t workspace_bytes, void *hip_stream);
+
+/* What the cache holds: k, v [batch][kv_heads][slots][head_dim] storage type, zeros in free slots. */
+int adore_q4_read(const adore_q4_config *cfg, const void *cache, const int32_t *slot_pos, void *k, void *v, void *hip_stream);
+
 const char *adore_strerror(int code);
 /* Debug aid for callers and tests, not a step of the method (no passage of the paper): with ADORE_GUARD_WORDS=1
  * in the environment of the process, adore_workspace_bytes and adore_create lay the workspace out with 256 bytes of

@@ -29,6 +29,8 @@ EXPORTS = [
     "adore_prompt_attention", "adore_prompt_backward_workspace_bytes", "adore_prompt_attention_backward", "adore_prompt_scores",
 ]
 
+EXPORTS_Q4 = ["adore_q4_cache_bytes", "adore_q4_workspace_bytes", "adore_q4_fill", "adore_q4_step", "adore_q4_read"]
+
 
 class AdoreConfig(ctypes.Structure):
     _fields_ = [(n, ctypes.c_int32) for n in
@@ -53,6 +55,11 @@ class AdoreForwardWeights(ctypes.Structure):
 class AdorePromptConfig(ctypes.Structure):
     _fields_ = [(n, ctypes.c_int32) for n in
                 ("batch", "heads", "kv_heads", "head_dim", "q_tokens", "k_tokens", "dtype")] + [("scale", ctypes.c_float)]
+
+
+class AdoreQ4Config(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in
+                ("batch", "heads", "kv_heads", "head_dim", "slots", "recent", "dtype")] + [("scale", ctypes.c_float)]
 
 
 class AdoreRows(ctypes.Structure):
@@ -131,6 +138,13 @@ def load_library() -> ctypes.CDLL:
     lib.adore_prompt_attention_backward.argtypes = [cfg, vp, vp] + [rows] * 6 + [vp] + [rows] * 3 + [vp, sz, vp]
     lib.adore_prompt_scores.restype = ctypes.c_int
     lib.adore_prompt_scores.argtypes = [cfg, vp, vp, rows, rows, vp, vp, vp]
+    q4 = ctypes.POINTER(AdoreQ4Config)
+    lib.adore_q4_cache_bytes.restype = lib.adore_q4_workspace_bytes.restype = sz
+    lib.adore_q4_cache_bytes.argtypes = lib.adore_q4_workspace_bytes.argtypes = [q4]
+    lib.adore_q4_fill.restype = lib.adore_q4_step.restype = lib.adore_q4_read.restype = ctypes.c_int
+    lib.adore_q4_fill.argtypes = [q4, vp, i32, rows, rows] + [vp] * 6
+    lib.adore_q4_step.argtypes = [q4] + [vp] * 11 + [sz, vp]
+    lib.adore_q4_read.argtypes = [q4] + [vp] * 5
     _lib = lib
     return lib
 
@@ -297,6 +311,82 @@ def prompt_scores(q: torch.Tensor, k: torch.Tensor, lse: torch.Tensor, *, q_star
     _check(lib, lib.adore_prompt_scores(ctypes.byref(p.cfg), *p.starts, p.rows(q, p.q_shape, "q"), p.rows(k, p.k_shape, "k"),
                                         p.values(lse, p.q_rows, "lse"), p.values(scores, p.k_rows, "scores"), p.stream))
     return scores
+
+
+class Q4Cache:
+    """A K/V cache held in 4 bits for `batch` sequences, evicted by the attention its rows received (adore_q4_* in include/adore.h):
+    its buffers, and the calls on torch's current stream.  fill() loads prompts, step() takes one token of every sequence, read()
+    gives the contents.  Buffers that are given are used as they are; others are made here, empty.
+
+      cache     uint8 [batch, kv_heads, ceil(slots / 64), 68 * head_dim]      slot_pos  int32 [batch, kv_heads, slots]
+      cursor    int32 [batch, kv_heads, 2]: next slot, next position          score     fp32 [batch, kv_heads, slots]
+
+    One stream at a time: every call works on the same buffers."""
+
+    def __init__(self, *, batch: int, heads: int, kv_heads: int, head_dim: int, slots: int, recent: int, dtype, scale: float = None,
+                 cache: torch.Tensor = None, slot_pos: torch.Tensor = None, score: torch.Tensor = None, cursor: torch.Tensor = None,
+                 device="cuda:0"):
+        self.lib = load_library()
+        code = {"f32": ADORE_F32, "bf16": ADORE_BF16}[dtype] if isinstance(dtype, str) else _CODES[dtype]
+        if scale is not None and not scale > 0.0:
+            raise ValueError("scale: expected a positive number")
+        self.cfg = AdoreQ4Config(batch, heads, kv_heads, head_dim, slots, recent, code, float(scale or 0.0))
+        self.dtype = torch.bfloat16 if code == ADORE_BF16 else torch.float32
+        need = self.lib.adore_q4_cache_bytes(ctypes.byref(self.cfg))
+        if need == 0:
+            raise AdoreError(-1, "invalid or unsupported configuration")
+        self.device = torch.device(device) if cache is None else cache.device
+        rows = (batch, kv_heads)
+        self.cache = self._buffer(cache, rows + ((slots + 63) // 64, 68 * head_dim), torch.uint8, 0, "cache", 256)
+        self.slot_pos = self._buffer(slot_pos, rows + (slots,), torch.int32, -1, "slot_pos", 16)
+        self.score = self._buffer(score, rows + (slots,), torch.float32, 0, "score", 16)
+        self.cursor = self._buffer(cursor, rows + (2,), torch.int32, 0, "cursor", 8)
+        self.workspace = torch.empty(self.lib.adore_q4_workspace_bytes(ctypes.byref(self.cfg)), dtype=torch.uint8, device=self.device)
+        self._state = [t.data_ptr() for t in (self.cache, self.slot_pos, self.score, self.cursor)]
+
+    def _buffer(self, t, shape, dtype, value, name, align):
+        if t is None:
+            return torch.full(shape, value, dtype=dtype, device=self.device)
+        return self._tensor(t, shape, dtype, name, align)
+
+    def _tensor(self, t, shape, dtype, name, align=16):
+        if not isinstance(t, torch.Tensor) or t.device != self.device or not t.is_cuda or t.dtype != dtype or tuple(t.shape) != tuple(shape) or \
+                not t.is_contiguous() or t.data_ptr() % align:
+            raise ValueError(f"{name}: expected a contiguous {dtype} tensor of shape {tuple(shape)} on {self.device}, {align}-byte aligned")
+        return t
+
+    def fill(self, k: torch.Tensor, v: torch.Tensor, scores: torch.Tensor = None, *, k_start: torch.Tensor = None):
+        """The prompts' best tokens: k, v [tokens, kv_heads, head_dim] with k_start (int32 [batch + 1]) and scores [kv_heads, tokens], or
+        [batch, kv_heads, tokens, head_dim] and [batch, kv_heads, tokens]; scores as prompt_scores gives them, or None."""
+        c = self.cfg
+        p = _Prompts(k, k, k_start, k_start, None)
+        if p.device != self.device or p.dtype != self.dtype or (p.batch, p.cfg.kv_heads, p.cfg.head_dim) != (c.batch, c.kv_heads, c.head_dim):
+            raise ValueError(f"k: expected {self.dtype} rows of {c.batch} sequences, {c.kv_heads} heads, {c.head_dim} elements on {self.device}")
+        _check(self.lib, self.lib.adore_q4_fill(ctypes.byref(c), p.starts[1], p.cfg.k_tokens, p.rows(k, p.k_shape, "k"), p.rows(v, p.k_shape, "v"),
+                                                None if scores is None else p.values(scores, p.k_rows, "scores"), *self._state, p.stream))
+
+    def step(self, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, *, out: torch.Tensor = None, held: bool = False):
+        """One token of every sequence: q [batch, heads, head_dim], k and v [batch, kv_heads, head_dim], contiguous.  Returns out
+        [batch, heads, head_dim], with held=True also the token's K and V as the cache holds them."""
+        c = self.cfg
+        mine, rows = (c.batch, c.heads, c.head_dim), (c.batch, c.kv_heads, c.head_dim)
+        if out is None:
+            out = torch.empty(mine, dtype=self.dtype, device=self.device)
+        kept = [torch.empty(rows, dtype=self.dtype, device=self.device) for _ in range(2)] if held else [None, None]
+        ptr = [self._tensor(t, s, self.dtype, n).data_ptr() for t, s, n in ((q, mine, "q"), (k, rows, "k"), (v, rows, "v"), (out, mine, "out"))]
+        _check(self.lib, self.lib.adore_q4_step(ctypes.byref(c), *ptr[:3], *self._state, ptr[3], *(None if t is None else t.data_ptr() for t in kept),
+                                                self.workspace.data_ptr(), self.workspace.numel(), torch.cuda.current_stream(self.device).cuda_stream))
+        return (out, *kept) if held else out
+
+    def read(self, k: torch.Tensor = None, v: torch.Tensor = None):
+        """What the cache holds: K and V [batch, kv_heads, slots, head_dim], zeros in free slots."""
+        c = self.cfg
+        shape = (c.batch, c.kv_heads, c.slots, c.head_dim)
+        k, v = (torch.empty(shape, dtype=self.dtype, device=self.device) if t is None else self._tensor(t, shape, self.dtype, n)
+                for t, n in ((k, "k"), (v, "v")))
+        _check(self.lib, self.lib.adore_q4_read(ctypes.byref(c), self._state[0], self._state[1], k.data_ptr(), v.data_ptr(),
+                                                torch.cuda.current_stream(self.device).cuda_stream))
+        return k, v
 
 
 class Adore:
