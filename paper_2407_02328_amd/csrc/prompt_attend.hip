@@ -36,12 +36,12 @@ constexpr int kKeys = sizeof(T) == 2 ? 64 : 32;
 // REST: P goes in as two bf16 terms (within 2^-16) and what rounding out leaves is handed out, for a backward pass whose delta is as good
 // as its other terms.
 template <typename T, int DH, bool REST>
-__global__ __launch_bounds__(256, 2) void prompt_attend_kernel(const AttendArgs<T> a) {
+__global__ __launch_bounds__(256) ADORE_WAVES(sizeof(T) == 4 ? 1 : DH == 128 ? 2 : REST ? 3 : 4) void prompt_attend_kernel(const AttendArgs<T> a) {
   constexpr int NT = 256, BQ = 128, KT = kKeys<T>, KB = KT / 32, DB = DH / 32, ST = DH / 16;
   typedef Tile<T, DH> L;
   typedef typename Operand<T>::type Frag;
   constexpr int kTile = KT * L::kRow;
-  extern __shared__ __align__(16) unsigned char smem[];   // K 0, K 1, V 0, V 1; at the end the outputs
+  extern __shared__ __align__(16) unsigned char smem[];   // two stages of K and V; at the end the outputs
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), c = lane & 31, h = lane >> 5;
   // kv head fastest: with a multiple of eight of them a head's workgroups share an XCD and its L2
   const int hk = blockIdx.x % a.s.kv_heads, item = blockIdx.x / a.s.kv_heads, head = hk * a.s.group + item % a.s.group;
@@ -60,56 +60,60 @@ __global__ __launch_bounds__(256, 2) void prompt_attend_kernel(const AttendArgs<
   const int rows = min(32, sq.nq - q0);        // may be <= 0
   const char *kp = reinterpret_cast<const char *>(a.k.p + sq.b * a.k.seq + sq.k_first * a.k.token + hk * a.k.head);
   const char *vp = reinterpret_cast<const char *>(a.v.p + sq.b * a.v.seq + sq.k_first * a.v.token + hk * a.v.head);
-  const int64_t ks = a.k.token * int64_t(sizeof(T)), vs = a.v.token * int64_t(sizeof(T));
 
-  // the query operand, through the wave's own quarter of LDS (4 x 32 rows: 16 KB, or 32, of the 64)
-  Frag qf[ST];
-  {
-    unsigned char *own = smem + wave * (32 * L::kRow);
-    const char *qp = reinterpret_cast<const char *>(a.q.p + sq.b * a.q.seq + (int64_t(sq.q_first) + q0) * a.q.token + head * a.q.head);
-    Carrier<T, DH, 32, 64> cq;
-    if (rows > 0) {
-      cq.template load<true>(qp, a.q.token * int64_t(sizeof(T)), 0, rows, lane);
-      cq.store(own, lane);
-    }
-    wave_lds_fence();
-#pragma unroll
-    for (int t = 0; t < ST; ++t) qf[t] = L::by_row(own, c, t, h);
-    __syncthreads();
-  }
-
-  f32x16 o[DB];
-#pragma unroll
-  for (int db = 0; db < DB; ++db) o[db] = f32x16{0.f};
-  float top = -INFINITY, sum = 0.f;             // of the lane's query: running maximum of the products, sum of its share of the keys
   const int last = min(block * BQ + BQ, sq.nq) - 1 + off;             // the last key that a query of the workgroup sees
   const int tiles = last < 0 ? 0 : last / KT + 1;
   const int mine = rows > 0 ? q0 + rows - 1 + off : -1;               // ... of the wave
   const int seen = q0 + c + off;                                      // ... of the lane
   const float scale = a.s.scale_log2;
-  Carrier<T, DH, KT, NT> ck, cv;
+  const uint32_t base0 = __builtin_amdgcn_readfirstlane(lds_offset(smem)), share = base0 + uint32_t(wave) * 1024u;
+  const int64_t ks = KT * a.k.token * int64_t(sizeof(T)), vs = KT * a.v.token * int64_t(sizeof(T));   // from tile to tile
+  const TileLoad<T, DH, KT, NT> lk(a.k.token * int64_t(sizeof(T)), tid), lv(a.v.token * int64_t(sizeof(T)), tid);
   if (tiles > 0) {
-    ck.template load<false>(kp, ks, 0, sq.nk, tid);
-    cv.template load<true>(vp, vs, 0, sq.nk, tid);
-    ck.store(smem, tid);
-    cv.store(smem + 2 * kTile, tid);
+    lk(kp, sq.nk, share);
+    lv(vp, sq.nk, share + kTile);
   }
+  Reader<T, DH> read(base0, lane);
+  // the query operand, through the wave's share of the second stage
+  Frag qf[ST];
+  operand_rows<T, DH, false>(qf, read, reinterpret_cast<const char *>(a.q.p + sq.b * a.q.seq + (int64_t(sq.q_first) + q0) * a.q.token + head * a.q.head),
+                      a.q.token * int64_t(sizeof(T)), rows, smem + 2 * kTile + wave * (32 * L::kRow), 2 * kTile + wave * (32 * L::kRow), lane);
+
+  f32x16 o[DB];
+#pragma unroll
+  for (int db = 0; db < DB; ++db) o[db] = f32x16{0.f};
+  float top = -INFINITY, sum = 0.f;             // of the lane's query: running maximum of the products, sum of its share of the keys
   for (int it = 0; it < tiles; ++it) {
-    const unsigned char *kt = smem + (it & 1) * kTile, *vt = kt + 2 * kTile;
     const int k0 = it * KT;
+    arrived();
     __syncthreads();
     if (it + 1 < tiles) {
-      ck.template load<false>(kp, ks, k0 + KT, sq.nk, tid);
-      cv.template load<true>(vp, vs, k0 + KT, sq.nk, tid);
+      const uint32_t next = share + uint32_t(~it & 1) * uint32_t(2 * kTile);
+      kp += ks;
+      vp += vs;
+      lk(kp, sq.nk - k0 - KT, next);
+      lv(vp, sq.nk - k0 - KT, next + kTile);
     }
     if (k0 <= mine) {
+      // Operands are on their way from LDS ahead of the products that take them, and arithmetic stands between products: a wave issues in
+      // order, and left to itself the compiler reads, waits and multiplies in turn.
+      Frag x[ST], v[DB];
       f32x16 s[KB];
+#pragma unroll
+      for (int t = 0; t < ST; ++t) x[t] = read.by_row(0, 0, t);
+      float m = -INFINITY;
 #pragma unroll
       for (int kb = 0; kb < KB; ++kb) {
         s[kb] = f32x16{0.f};
 #pragma unroll
-        for (int t = 0; t < ST; ++t) s[kb] = Operand<T>::mma(L::by_row(kt, kb * 32 + c, t, h), qf[t], s[kb]);
+        for (int t = 0; t < ST; ++t) {
+          pin();
+          s[kb] = Operand<T>::mma(x[t], qf[t], s[kb]);
+          if (kb + 1 < KB) x[t] = read.by_row(0, kb * 32 + 32, t);
+          if (kb + 1 == KB && t >= ST - DB) v[t - ST + DB] = read.transposed(kTile, 0, 0, t - ST + DB);
+        }
       }
+      pin();
       if (k0 + KT - 1 > q0 + off) {             // some of the wave's queries do not see all of the tile
 #pragma unroll
         for (int kb = 0; kb < KB; ++kb)
@@ -117,7 +121,6 @@ __global__ __launch_bounds__(256, 2) void prompt_attend_kernel(const AttendArgs<
           for (int r = 0; r < 16; ++r)
             if (k0 + kb * 32 + 8 * (r >> 2) + 4 * h + (r & 3) > seen) s[kb][r] = -INFINITY;
       }
-      float m = s[0][0];
 #pragma unroll
       for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
@@ -133,35 +136,36 @@ __global__ __launch_bounds__(256, 2) void prompt_attend_kernel(const AttendArgs<
           for (int r = 0; r < 16; ++r) o[db][r] *= fade;
         top = m;
       }
-      Frag pf[KB][2];
       float part[4] = {0.f};                    // a tile's weights first, so that few additions round the running sum
+      auto weights = [&](int kb, int r0, int n) {
 #pragma unroll
-      for (int kb = 0; kb < KB; ++kb) {
-#pragma unroll
-        for (int r = 0; r < 16; ++r) {
+        for (int r = r0; r < r0 + n; ++r) {
           s[kb][r] = __builtin_amdgcn_exp2f(fmaf(s[kb][r], scale, base));
           part[r & 3] += s[kb][r];
         }
-        pf[kb][0] = Operand<T>::of(s[kb], 0);
-        pf[kb][1] = Operand<T>::of(s[kb], 1);
+      };
+      Frag pf[2];
+      weights(0, 0, 16);
+      pf[0] = Operand<T>::of(s[0], 0);
+      pf[1] = Operand<T>::of(s[0], 1);
+#pragma unroll
+      for (int i = 0; i < 2 * KB; ++i) {        // 16 keys a step
+        const Frag p = pf[i & 1];
+        Frag left;
+        if constexpr (REST) left = Operand<T>::rest_of(s[i >> 1], p, i & 1);
+#pragma unroll
+        for (int db = 0; db < DB; ++db) {
+          pin();
+          o[db] = Operand<T>::mma(v[db], p, o[db]);
+          if constexpr (REST) o[db] = Operand<T>::mma(v[db], left, o[db]);
+          if (i + 1 < 2 * KB) v[db] = read.transposed(kTile, (i + 1) / 2 * 32, (i + 1) & 1, db);
+          if (i + 2 < 2 * KB) weights((i + 2) >> 1, 8 * (i & 1) + db * (8 / DB), 8 / DB);   // those of the step after the next one
+        }
+        if (i + 2 < 2 * KB) pf[i & 1] = Operand<T>::of(s[(i + 2) >> 1], i & 1);
       }
       sum += (part[0] + part[1]) + (part[2] + part[3]);
-#pragma unroll
-      for (int kb = 0; kb < KB; ++kb)
-#pragma unroll
-        for (int t = 0; t < 2; ++t)
-#pragma unroll
-          for (int db = 0; db < DB; ++db) {
-            const Frag vf = L::transposed(vt, kb * 32, t, db, lane);
-            o[db] = Operand<T>::mma(vf, pf[kb][t], o[db]);
-            if constexpr (REST) o[db] = Operand<T>::mma(vf, Operand<T>::rest_of(s[kb], pf[kb][t], t), o[db]);
-          }
     }
-    if (it + 1 < tiles) {
-      unsigned char *next = smem + (~it & 1) * kTile;
-      ck.store(next, tid);
-      cv.store(next + 2 * kTile, tid);
-    }
+    read.move(it & 1 ? uint32_t(-2 * kTile) : uint32_t(2 * kTile));
   }
   __syncthreads();
   if (rows <= 0) return;
@@ -181,7 +185,8 @@ __global__ __launch_bounds__(256, 2) void prompt_attend_kernel(const AttendArgs<
 
 template <typename T, int DH, bool REST>
 hipError_t launch_attend_prompt(const AttendArgs<T> &a, hipStream_t st) {
-  constexpr int lds = 4 * kKeys<T> * Tile<T, DH>::kRow;
+  // a stage, and behind it another one or the waves' 32 queries each
+  constexpr int stage = 2 * kKeys<T> * Tile<T, DH>::kRow, waves = 4 * 32 * Tile<T, DH>::kRow, lds = stage + (stage > waves ? stage : waves);
   const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(&prompt_attend_kernel<T, DH, REST>),
                                            hipFuncAttributeMaxDynamicSharedMemorySize, lds);
   if (e != hipSuccess) return e;
@@ -205,7 +210,7 @@ template <typename T>
 constexpr int kQueries = sizeof(T) == 2 ? 64 : 32;
 
 template <typename T, int DH>
-__global__ __launch_bounds__(256, 2) void prompt_scores_kernel(const ScoreArgs<T> a) {
+__global__ __launch_bounds__(256) void prompt_scores_kernel(const ScoreArgs<T> a) {
   constexpr int NT = 256, BK = 128, QT = kQueries<T>, QB = QT / 32, ST = DH / 16;
   typedef Tile<T, DH> L;
   typedef typename Operand<T>::type Frag;
@@ -224,69 +229,79 @@ __global__ __launch_bounds__(256, 2) void prompt_scores_kernel(const ScoreArgs<T
   }
   const int k0 = block * BK + wave * 32, off = sq.nk - sq.nq;
   const int rows = min(32, sq.nk - k0);
-  Frag kf[ST];
-  {
-    unsigned char *own = smem + wave * (32 * L::kRow);
-    const char *kp = reinterpret_cast<const char *>(a.k.p + sq.b * a.k.seq + (int64_t(sq.k_first) + k0) * a.k.token + hk * a.k.head);
-    Carrier<T, DH, 32, 64> cc;
-    if (rows > 0) {
-      cc.template load<true>(kp, a.k.token * int64_t(sizeof(T)), 0, rows, lane);
-      cc.store(own, lane);
-    }
-    wave_lds_fence();
-#pragma unroll
-    for (int t = 0; t < ST; ++t) kf[t] = L::by_row(own, c, t, h);
-    __syncthreads();
-  }
   const int first = max(block * BK - off, 0) / QT * QT;    // the first tile with a query that sees a key of the workgroup
   const int per = first < sq.nq ? (sq.nq - first + QT - 1) / QT : 0, tiles = per * a.s.group;
-  const int64_t qs = a.q.token * int64_t(sizeof(T));
   const float scale = a.s.scale_log2;
   const bool packed = a.s.q_start != nullptr;
-  float sum = 0.f;
-  Carrier<T, DH, QT, NT> cq;
+  const uint32_t base0 = __builtin_amdgcn_readfirstlane(lds_offset(smem)), share = base0 + uint32_t(wave) * 1024u;
+  const int64_t qs = a.q.token * int64_t(sizeof(T));
+  const TileLoad<T, DH, QT, NT> lq(a.q.token * int64_t(sizeof(T)), tid);
+  // the tile after the last one loaded: its head's rows and log-sum-exps, its first query
+  const char *qp = reinterpret_cast<const char *>(a.q.p + sq.b * a.q.seq + sq.q_first * a.q.token + hk * a.s.group * a.q.head);
+  const float *lp = a.lse + row_value(packed, sq.b, sq.q_first, a.s.q_tokens, a.s.heads, hk * a.s.group);
+  int next = first;
   float row_lse = 0.f;
-  auto load = [&](int it) {
-    const int head = hk * a.s.group + it / per, q0 = first + it % per * QT;
-    const char *qp = reinterpret_cast<const char *>(a.q.p + sq.b * a.q.seq + sq.q_first * a.q.token + head * a.q.head);
-    cq.template load<false>(qp, qs, q0, sq.nq, tid);
-    if (tid < QT)
-      row_lse = q0 + tid < sq.nq ? a.lse[row_value(packed, sq.b, sq.q_first, a.s.q_tokens, a.s.heads, head) + q0 + tid] * kLog2e : INFINITY;
+  auto load = [&](int stage) {
+    lq(qp + next * qs, sq.nq - next, share + uint32_t(stage * kTile));
+    if (tid < QT) row_lse = next + tid < sq.nq ? subtrahend(lp[next + tid]) : INFINITY;
+    next += QT;
+    if (next >= sq.nq) {
+      next = first;
+      qp += a.q.head * int64_t(sizeof(T));
+      lp += a.s.q_tokens;
+    }
   };
-  auto store = [&](int it) {
-    cq.store(smem + (it & 1) * kTile, tid);
-    if (tid < QT) s_lse[it & 1][tid] = row_lse;
-  };
-  if (tiles > 0) {
-    load(0);
-    store(0);
-  }
+  Reader<T, DH> read(base0, lane);
+  Frag kf[ST];                                              // through the wave's quarter of LDS
+  operand_rows<T, DH, false>(kf, read, reinterpret_cast<const char *>(a.k.p + sq.b * a.k.seq + (int64_t(sq.k_first) + k0) * a.k.token + hk * a.k.head),
+                      a.k.token * int64_t(sizeof(T)), rows, smem + wave * (32 * L::kRow), wave * (32 * L::kRow), lane);
+  __syncthreads();
+  if (tiles > 0) load(0);
+  if (tid < QT) s_lse[0][tid] = row_lse;
+  float sum = 0.f;
+  int q0 = first - QT;
   for (int it = 0; it < tiles; ++it) {
-    const unsigned char *qt = smem + (it & 1) * kTile;
-    const int q0 = first + it % per * QT;
+    q0 += QT;
+    if (q0 >= sq.nq) q0 = first;
+    arrived();
     __syncthreads();
-    if (it + 1 < tiles) load(it + 1);
-    float part = 0.f;
+    if (it + 1 < tiles) load(~it & 1);
+    Frag x[ST];
+#pragma unroll
+    for (int t = 0; t < ST; ++t) x[t] = read.by_row(0, 0, t);
+    f32x16 s[QB];
+    float part[4] = {0.f};
+    auto weights = [&](int qb, int r4) {
+      const f32x4 lse = *reinterpret_cast<const f32x4 *>(&s_lse[it & 1][qb * 32 + 8 * r4 + 4 * h]);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) part[i] += __builtin_amdgcn_exp2f(fmaf(s[qb][4 * r4 + i], scale, -lse[i]));
+    };
+    auto hide = [&](int qb) {
+      const int qf = q0 + qb * 32 + off;
+      if (qf < k0 + 31) {                              // some of these queries do not see some of the wave's keys
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+          if (k0 + c > qf + 8 * (r >> 2) + 4 * h + (r & 3)) s[qb][r] = -INFINITY;
+      }
+    };
 #pragma unroll
     for (int qb = 0; qb < QB; ++qb) {
-      if (q0 + qb * 32 + 31 + off < k0) continue;      // none of these queries sees the wave's keys
-      f32x16 s = {0.f};
+      s[qb] = f32x16{0.f};
 #pragma unroll
-      for (int t = 0; t < ST; ++t) s = Operand<T>::mma(L::by_row(qt, qb * 32 + c, t, h), kf[t], s);
-      const bool partly = q0 + qb * 32 + off < k0 + 31;
-#pragma unroll
-      for (int r4 = 0; r4 < 4; ++r4) {
-        const f32x4 lse = *reinterpret_cast<const f32x4 *>(&s_lse[it & 1][qb * 32 + 8 * r4 + 4 * h]);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int q = q0 + qb * 32 + 8 * r4 + 4 * h + i;
-          const float p = __builtin_amdgcn_exp2f(fmaf(s[4 * r4 + i], scale, -lse[i]));
-          part += (partly && k0 + c > q + off) ? 0.f : p;
-        }
+      for (int t = 0; t < ST; ++t) {
+        pin();
+        s[qb] = Operand<T>::mma(x[t], kf[t], s[qb]);
+        if (qb + 1 < QB) x[t] = read.by_row(0, qb * 32 + 32, t);
+        if (qb > 0 && t % (ST / 4) == ST / 4 - 1) weights(qb - 1, t / (ST / 4));   // the block before under this one's products
       }
+      pin();
+      hide(qb);
     }
-    sum += part;
-    if (it + 1 < tiles) store(it + 1);
+#pragma unroll
+    for (int r4 = 0; r4 < 4; ++r4) weights(QB - 1, r4);
+    sum += (part[0] + part[1]) + (part[2] + part[3]);
+    if (it + 1 < tiles && tid < QT) s_lse[~it & 1][tid] = row_lse;
+    read.move(it & 1 ? uint32_t(-kTile) : uint32_t(kTile));
   }
   sum = add_lane_xor<32>(sum);
   if (lane < rows) a.scores[row_value(packed, sq.b, sq.k_first, a.s.k_tokens, a.s.kv_heads, hk) + k0 + lane] = sum;

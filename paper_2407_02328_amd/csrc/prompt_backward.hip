@@ -16,8 +16,6 @@ namespace adore {
 
 namespace {
 
-constexpr float kLog2e = 1.4426950408889634f;
-
 template <typename T>
 struct BackwardArgs {
   PromptShape s;
@@ -50,32 +48,17 @@ __global__ __launch_bounds__(256) void prompt_delta_kernel(const BackwardArgs<T>
   if (sub == 0) a.delta[row_value(packed, b, 0, a.s.q_tokens, a.s.heads, head) + t] = sum;
 }
 
-// 32 rows from `base` (zeros beyond `rows`) as an operand, through the wave's own LDS.
-template <typename T, int DH>
-__device__ __forceinline__ void operand_rows(typename Operand<T>::type (&f)[DH / 16], const char *base, int64_t stride, int rows,
-                                             unsigned char *own, int lane) {
-  Carrier<T, DH, 32, 64> carry;
-  wave_lds_fence();
-  if (rows > 0) {
-    carry.template load<true>(base, stride, 0, rows, lane);
-    carry.store(own, lane);
-  }
-  wave_lds_fence();
-#pragma unroll
-  for (int t = 0; t < DH / 16; ++t) f[t] = Tile<T, DH>::by_row(own, lane & 31, t, lane >> 5);
-}
-
 // ---- dq: 128 queries a workgroup, 32 a wave ----
 template <typename T>
 constexpr int kDqKeys = sizeof(T) == 2 ? 64 : 32;
 
 template <typename T, int DH>
-__global__ __launch_bounds__(256, 2) void prompt_dq_kernel(const BackwardArgs<T> a) {
+__global__ __launch_bounds__(256) ADORE_WAVES(sizeof(T) == 4 ? 1 : DH == 128 ? 2 : 3) void prompt_dq_kernel(const BackwardArgs<T> a) {
   constexpr int NT = 256, BQ = 128, KT = kDqKeys<T>, KB = KT / 32, DB = DH / 32, ST = DH / 16;
   typedef Tile<T, DH> L;
   typedef typename Operand<T>::type Frag;
   constexpr int kTile = KT * L::kRow;
-  extern __shared__ __align__(16) unsigned char smem[];   // K 0, K 1, V 0, V 1
+  extern __shared__ __align__(16) unsigned char smem[];   // two stages of K and V
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), c = lane & 31, h = lane >> 5;
   const int hk = blockIdx.x % a.s.kv_heads, item = blockIdx.x / a.s.kv_heads, head = hk * a.s.group + item % a.s.group;
   Sequence sq;
@@ -92,65 +75,97 @@ __global__ __launch_bounds__(256, 2) void prompt_dq_kernel(const BackwardArgs<T>
   const int64_t row = int64_t(sq.q_first) + q0, es = int64_t(sizeof(T));
   const char *kp = reinterpret_cast<const char *>(a.k.p + sq.b * a.k.seq + sq.k_first * a.k.token + hk * a.k.head);
   const char *vp = reinterpret_cast<const char *>(a.v.p + sq.b * a.v.seq + sq.k_first * a.v.token + hk * a.v.head);
-  unsigned char *own = smem + wave * (32 * L::kRow);
+  const int last = min(block * BQ + BQ, sq.nq) - 1 + off, tiles = last < 0 ? 0 : last / KT + 1;
+  const int mine = rows > 0 ? q0 + rows - 1 + off : -1, seen = q0 + c + off;
+  const float scale = a.s.scale_log2;
+  const uint32_t base0 = __builtin_amdgcn_readfirstlane(lds_offset(smem)), share = base0 + uint32_t(wave) * 1024u;
+  Reader<T, DH> read(base0, lane);
+  const TileLoad<T, DH, KT, NT> lk(a.k.token * es, tid), lv(a.v.token * es, tid);
+  if (tiles > 0) {
+    lk(kp, sq.nk, share);
+    lv(vp, sq.nk, share + kTile);
+  }
+  unsigned char *own = smem + 2 * kTile + wave * (32 * L::kRow);    // the wave's share of the second stage
   Frag qf[ST], df[ST];
-  operand_rows<T, DH>(qf, reinterpret_cast<const char *>(a.q.p + sq.b * a.q.seq + row * a.q.token + head * a.q.head), a.q.token * es, rows, own, lane);
-  operand_rows<T, DH>(df, reinterpret_cast<const char *>(a.d_out.p + sq.b * a.d_out.seq + row * a.d_out.token + head * a.d_out.head),
-                      a.d_out.token * es, rows, own, lane);
-  __syncthreads();
+  operand_rows<T, DH, false>(qf, read, reinterpret_cast<const char *>(a.q.p + sq.b * a.q.seq + row * a.q.token + head * a.q.head), a.q.token * es, rows, own, 2 * kTile + wave * (32 * L::kRow), lane);
+  operand_rows<T, DH, false>(df, read, reinterpret_cast<const char *>(a.d_out.p + sq.b * a.d_out.seq + row * a.d_out.token + head * a.d_out.head),
+                      a.d_out.token * es, rows, own, 2 * kTile + wave * (32 * L::kRow), lane);
   float lse = INFINITY, delta = 0.f;            // of the lane's query; weights of a query that is not there are 0
   if (c < rows) {
     const size_t at = row_value(a.s.q_start != nullptr, sq.b, sq.q_first, a.s.q_tokens, a.s.heads, head) + q0 + c;
-    lse = a.lse[at] * kLog2e;
+    lse = subtrahend(a.lse[at]);
     delta = a.delta[at];
   }
   f32x16 dq[DB];
 #pragma unroll
   for (int db = 0; db < DB; ++db) dq[db] = f32x16{0.f};
-  const int last = min(block * BQ + BQ, sq.nq) - 1 + off, tiles = last < 0 ? 0 : last / KT + 1;
-  const int mine = rows > 0 ? q0 + rows - 1 + off : -1, seen = q0 + c + off;
-  const float scale = a.s.scale_log2;
-  Carrier<T, DH, KT, NT> ck, cv;
-  auto load = [&](int k0) {
-    ck.template load<true>(kp, a.k.token * es, k0, sq.nk, tid);
-    cv.template load<true>(vp, a.v.token * es, k0, sq.nk, tid);
-  };
-  auto store = [&](unsigned char *to) {
-    ck.store(to, tid);
-    cv.store(to + 2 * kTile, tid);
-  };
-  if (tiles > 0) {
-    load(0);
-    store(smem);
-  }
   for (int it = 0; it < tiles; ++it) {
-    const unsigned char *kt = smem + (it & 1) * kTile, *vt = kt + 2 * kTile;
     const int k0 = it * KT;
+    arrived();
     __syncthreads();
-    if (it + 1 < tiles) load(k0 + KT);
+    if (it + 1 < tiles) {
+      const uint32_t next = share + uint32_t(~it & 1) * uint32_t(2 * kTile);
+      kp += KT * a.k.token * es;
+      vp += KT * a.v.token * es;
+      lk(kp, sq.nk - k0 - KT, next);
+      lv(vp, sq.nk - k0 - KT, next + kTile);
+    }
+    if (k0 > mine) {
+      read.move(it & 1 ? uint32_t(-2 * kTile) : uint32_t(2 * kTile));
+      continue;
+    }
+    // Operands on their way ahead of their products, arithmetic between products (a wave issues in order).
+    Frag x[ST], y[DB];
+#pragma unroll
+    for (int t = 0; t < ST; ++t) x[t] = read.by_row(0, 0, t);
 #pragma unroll
     for (int kb = 0; kb < KB; ++kb) {
-      const int kf = k0 + kb * 32;
-      if (kf > mine) continue;
       f32x16 s = {0.f}, g = {0.f};
 #pragma unroll
-      for (int t = 0; t < ST; ++t) s = Operand<T>::mma(L::by_row(kt, kb * 32 + c, t, h), qf[t], s);
+      for (int t = 0; t < ST; ++t) {
+        pin();
+        s = Operand<T>::mma(x[t], qf[t], s);
+        x[t] = read.by_row(kTile, kb * 32, t);
+      }
+      pin();
+      if (k0 + kb * 32 + 31 > q0 + off) {         // some of the wave's queries do not see some of these keys
 #pragma unroll
-      for (int t = 0; t < ST; ++t) g = Operand<T>::mma(L::by_row(vt, kb * 32 + c, t, h), df[t], g);
-      const bool partly = kf + 31 > q0 + off;
-#pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        const float p = __builtin_amdgcn_exp2f(fmaf(s[r], scale, -lse));
-        g[r] = (partly && kf + 8 * (r >> 2) + 4 * h + (r & 3) > seen) ? 0.f : p * (g[r] - delta);
+        for (int r = 0; r < 16; ++r)
+          if (k0 + kb * 32 + 8 * (r >> 2) + 4 * h + (r & 3) > seen) s[r] = -INFINITY;
       }
 #pragma unroll
-      for (int t = 0; t < 2; ++t) {
-        const Frag gf = Operand<T>::of(g, t);
+      for (int t = 0; t < ST; ++t) {
+        pin();
+        g = Operand<T>::mma(x[t], df[t], g);
+        if (t >= ST - DB) y[t - ST + DB] = read.transposed(0, kb * 32, 0, t - ST + DB);
 #pragma unroll
-        for (int db = 0; db < DB; ++db) dq[db] = Operand<T>::mma(L::transposed(kt, kb * 32, t, db, lane), gf, dq[db]);
+        for (int r = t * (16 / ST); r < (t + 1) * (16 / ST); ++r) s[r] = __builtin_amdgcn_exp2f(fmaf(s[r], scale, -lse));
       }
+      pin();
+#pragma unroll
+      for (int r = 0; r < 8; ++r) g[r] = s[r] * (g[r] - delta);
+      Frag gf = Operand<T>::of(g, 0);
+#pragma unroll
+      for (int db = 0; db < DB; ++db) {
+        pin();
+        dq[db] = Operand<T>::mma(y[db], gf, dq[db]);
+        y[db] = read.transposed(0, kb * 32, 1, db);
+#pragma unroll
+        for (int r = 8 + db * (8 / DB); r < 8 + (db + 1) * (8 / DB); ++r) g[r] = s[r] * (g[r] - delta);
+      }
+      gf = Operand<T>::of(g, 1);
+#pragma unroll
+      for (int db = 0; db < DB; ++db) {
+        pin();
+        dq[db] = Operand<T>::mma(y[db], gf, dq[db]);
+        if (kb + 1 < KB) {
+#pragma unroll
+          for (int t = db * (ST / DB); t < (db + 1) * (ST / DB); ++t) x[t] = read.by_row(0, kb * 32 + 32, t);
+        }
+      }
+      pin();
     }
-    if (it + 1 < tiles) store(smem + (~it & 1) * kTile);
+    read.move(it & 1 ? uint32_t(-2 * kTile) : uint32_t(2 * kTile));
   }
   __syncthreads();
   if (rows <= 0) return;
@@ -159,17 +174,19 @@ __global__ __launch_bounds__(256, 2) void prompt_dq_kernel(const BackwardArgs<T>
 }
 
 // ---- dk and dv: 128 keys a workgroup, 32 a wave ----
+// At 128 elements a wave's K, V and their gradients would be 192 registers, and with the rest more than two waves a SIMD leave room for:
+// V stays in LDS (a spilled register in the loop costs a wait for the next tile: loads return in order).
 template <typename T>
 constexpr int kDkvQueries = 32;
 
 template <typename T, int DH>
-__global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void prompt_dkv_kernel(const BackwardArgs<T> a) {
-  constexpr int NT = 256, BK = 128, QT = kDkvQueries<T>, QB = QT / 32, DB = DH / 32, ST = DH / 16;
+__global__ __launch_bounds__(256) ADORE_WAVES(sizeof(T) == 2 ? 2 : 1) void prompt_dkv_kernel(const BackwardArgs<T> a) {
+  constexpr int NT = 256, BK = 128, QT = kDkvQueries<T>, DB = DH / 32, ST = DH / 16;
   typedef Tile<T, DH> L;
   typedef typename Operand<T>::type Frag;
-  constexpr int kTile = QT * L::kRow;
-  extern __shared__ __align__(16) unsigned char smem[];   // Q 0, Q 1, dO 0, dO 1
-  __shared__ __align__(16) float s_lse[2][QT], s_delta[2][QT];
+  constexpr int kTile = QT * L::kRow, kWave = 32 * L::kRow;
+  extern __shared__ __align__(16) unsigned char smem[];   // two stages of Q and dO (32 rows a wave besides), the workgroup's V
+  float *const s_lse = reinterpret_cast<float *>(smem + 8 * kTile), *const s_delta = s_lse + 2 * QT;   // [stage][QT] each, behind V
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), c = lane & 31, h = lane >> 5;
   const int hk = blockIdx.x % a.s.kv_heads;
   Sequence sq;
@@ -184,83 +201,137 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void prompt_dkv_kernel
   const int k0 = block * BK + wave * 32, off = sq.nk - sq.nq;
   const int rows = min(32, sq.nk - k0);
   const int64_t row = int64_t(sq.k_first) + k0, es = int64_t(sizeof(T));
-  unsigned char *own = smem + wave * (32 * L::kRow);
-  Frag kf[ST], vf[ST];
-  operand_rows<T, DH>(kf, reinterpret_cast<const char *>(a.k.p + sq.b * a.k.seq + row * a.k.token + hk * a.k.head), a.k.token * es, rows, own, lane);
-  operand_rows<T, DH>(vf, reinterpret_cast<const char *>(a.v.p + sq.b * a.v.seq + row * a.v.token + hk * a.v.head), a.v.token * es, rows, own, lane);
-  __syncthreads();
-  f32x16 dk[DB], dv[DB];
-#pragma unroll
-  for (int db = 0; db < DB; ++db) dk[db] = dv[db] = f32x16{0.f};
   const int first = max(block * BK - off, 0) / QT * QT;
   const int per = first < sq.nq ? (sq.nq - first + QT - 1) / QT : 0, tiles = per * a.s.group;
   const float scale = a.s.scale_log2;
   const bool packed = a.s.q_start != nullptr;
-  Carrier<T, DH, QT, NT> cq, cd;
+  const uint32_t base0 = __builtin_amdgcn_readfirstlane(lds_offset(smem)), share = base0 + uint32_t(wave) * 1024u;
+  Reader<T, DH, sizeof(T) == 2> read(base0, lane);
+  const TileLoad<T, DH, QT, NT> lq(a.q.token * es, tid), ld(a.d_out.token * es, tid);
+  // The tile after the last one loaded: its head's rows, its first query.  From the last query back to the diagonal: the workgroups of
+  // a head start with the same tiles, one reads what the others find in the L2.
+  const int final = first + (per - 1) * QT;
+  const char *qp = reinterpret_cast<const char *>(a.q.p + sq.b * a.q.seq + sq.q_first * a.q.token + hk * a.s.group * a.q.head);
+  const char *dp = reinterpret_cast<const char *>(a.d_out.p + sq.b * a.d_out.seq + sq.q_first * a.d_out.token + hk * a.s.group * a.d_out.head);
+  size_t at = row_value(packed, sq.b, sq.q_first, a.s.q_tokens, a.s.heads, hk * a.s.group);
+  int next = final;
   float row_lse = 0.f, row_delta = 0.f;
-  auto load = [&](int it) {
-    const int head = hk * a.s.group + it / per, q0 = first + it % per * QT;
-    cq.template load<true>(reinterpret_cast<const char *>(a.q.p + sq.b * a.q.seq + sq.q_first * a.q.token + head * a.q.head), a.q.token * es, q0, sq.nq, tid);
-    cd.template load<true>(reinterpret_cast<const char *>(a.d_out.p + sq.b * a.d_out.seq + sq.q_first * a.d_out.token + head * a.d_out.head),
-                           a.d_out.token * es, q0, sq.nq, tid);
+  auto load = [&](int stage) {
+    lq(qp + next * (a.q.token * es), sq.nq - next, share + uint32_t(stage * 2 * kTile));
+    ld(dp + next * (a.d_out.token * es), sq.nq - next, share + uint32_t(stage * 2 * kTile + kTile));
     if (tid < QT) {
-      const bool there = q0 + tid < sq.nq;
-      const size_t at = row_value(packed, sq.b, sq.q_first, a.s.q_tokens, a.s.heads, head) + q0 + tid;
-      row_lse = there ? a.lse[at] * kLog2e : INFINITY;
-      row_delta = there ? a.delta[at] : 0.f;
+      const bool there = next + tid < sq.nq;
+      row_lse = there ? subtrahend(a.lse[at + next + tid]) : INFINITY;
+      row_delta = there ? a.delta[at + next + tid] : 0.f;
+    }
+    next -= QT;
+    if (next < first) {
+      next = final;
+      qp += a.q.head * es;
+      dp += a.d_out.head * es;
+      at += a.s.q_tokens;
     }
   };
-  auto store = [&](int it) {
-    unsigned char *to = smem + (it & 1) * kTile;
-    cq.store(to, tid);
-    cd.store(to + 2 * kTile, tid);
+  auto hand_over = [&](int stage) {
     if (tid < QT) {
-      s_lse[it & 1][tid] = row_lse;
-      s_delta[it & 1][tid] = row_delta;
+      s_lse[stage * QT + tid] = row_lse;
+      s_delta[stage * QT + tid] = row_delta;
     }
   };
-  if (tiles > 0) {
-    load(0);
-    store(0);
-  }
+  unsigned char *own = smem + wave * kWave;
+  constexpr int kVAt = 4 * kTile;                          // = four waves' 32 rows: a stage is 64 of them
+  static_assert(4 * kTile == 4 * kWave, "the waves' own rows end where V begins");
+  Frag kf[ST];
+  operand_rows<T, DH, sizeof(T) == 2>(kf, read, reinterpret_cast<const char *>(a.k.p + sq.b * a.k.seq + row * a.k.token + hk * a.k.head), a.k.token * es, rows, own,
+                      wave * kWave, lane);
+  if (rows > 0)
+    carry_rows<T, DH>(reinterpret_cast<const char *>(a.v.p + sq.b * a.v.seq + row * a.v.token + hk * a.v.head), a.v.token * es, rows,
+                      own + kVAt, lane);
+  __syncthreads();
+  if (tiles > 0) load(0);
+  hand_over(0);
+  const uint32_t v_ahead = kVAt + uint32_t(wave) * kWave;  // of the reader at stage 0
+  f32x16 dk[DB], dv[DB];
+#pragma unroll
+  for (int db = 0; db < DB; ++db) dk[db] = dv[db] = f32x16{0.f};
+  int q0 = final + QT;
   for (int it = 0; it < tiles; ++it) {
-    const unsigned char *qt = smem + (it & 1) * kTile, *dt = qt + 2 * kTile;
-    const int q0 = first + it % per * QT;
+    q0 -= QT;
+    if (q0 < first) q0 = final;
+    arrived();
     __syncthreads();
-    if (it + 1 < tiles) load(it + 1);
+    if (it + 1 < tiles) load(~it & 1);
+    // Operands on their way ahead of their products, arithmetic between products (a wave issues in order).  A tile that none of the wave's
+    // keys is seen from is worked on like any other: its weights are zeros.
+    const uint32_t va = v_ahead - uint32_t((it & 1) * 2 * kTile);
+    const float *const rows_lse = s_lse + (it & 1) * QT + 4 * h, *const rows_delta = s_delta + (it & 1) * QT + 4 * h;
+    Frag x[4], y[4];                                        // rings, four products deep
+    f32x16 s = {0.f}, g = {0.f};
 #pragma unroll
-    for (int qb = 0; qb < QB; ++qb) {
-      const int qf = q0 + qb * 32;
-      if (qf + 31 + off < k0) continue;
-      f32x16 s = {0.f}, g = {0.f};
+    for (int t = 0; t < 4; ++t) x[t] = read.by_row(0, 0, t);
 #pragma unroll
-      for (int t = 0; t < ST; ++t) s = Operand<T>::mma(L::by_row(qt, qb * 32 + c, t, h), kf[t], s);
+    for (int t = 0; t < ST; ++t) {
+      pin();
+      s = Operand<T>::mma(x[t & 3], kf[t], s);
+      x[t & 3] = t + 4 < ST ? read.by_row(0, 0, t + 4) : read.by_row(kTile, 0, t + 4 - ST);
+      if (t >= ST - 4) y[t - ST + 4] = read.by_row(va, 0, t - ST + 4);
+    }
+    pin();
+    if (q0 + off < k0 + 31) {                               // some of the queries do not see some of the wave's keys
 #pragma unroll
-      for (int t = 0; t < ST; ++t) g = Operand<T>::mma(L::by_row(dt, qb * 32 + c, t, h), vf[t], g);
-      const bool partly = qf + off < k0 + 31;
+      for (int r = 0; r < 16; ++r)
+        if (k0 + c > q0 + 8 * (r >> 2) + 4 * h + (r & 3) + off) s[r] = -INFINITY;
+    }
+    auto next_of = [&](int i) {                             // columns in the order of the last four groups of products
+      const int db = i % DB, t = i / DB;
+      return t < 2 ? read.transposed(kTile, 0, t, db) : read.transposed(0, 0, t - 2, db);
+    };
 #pragma unroll
-      for (int r4 = 0; r4 < 4; ++r4) {
-        const f32x4 lse = *reinterpret_cast<const f32x4 *>(&s_lse[it & 1][qb * 32 + 8 * r4 + 4 * h]);
-        const f32x4 delta = *reinterpret_cast<const f32x4 *>(&s_delta[it & 1][qb * 32 + 8 * r4 + 4 * h]);
+    for (int t = 0; t < ST; ++t) {
+      pin();
+      g = Operand<T>::mma(x[t & 3], y[t & 3], g);
+      x[t & 3] = t + 4 < ST ? read.by_row(kTile, 0, t + 4) : next_of(t + 4 - ST);
+      if (t + 4 < ST) y[t & 3] = read.by_row(va, 0, t + 4);
+      if (t % (ST / 4) == 0) {
+        const int r4 = t / (ST / 4);
+        const f32x4 lse = *reinterpret_cast<const f32x4 *>(rows_lse + 8 * r4);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int r = 4 * r4 + i;
-          const bool hidden = partly && k0 + c > qf + 8 * r4 + 4 * h + i + off;
-          const float p = __builtin_amdgcn_exp2f(fmaf(s[r], scale, -lse[i]));
-          s[r] = hidden ? 0.f : p;
-          g[r] = hidden ? 0.f : p * (g[r] - delta[i]);
-        }
-      }
-#pragma unroll
-      for (int t = 0; t < 2; ++t) {
-        const Frag pf = Operand<T>::of(s, t), gf = Operand<T>::of(g, t);
-#pragma unroll
-        for (int db = 0; db < DB; ++db) dv[db] = Operand<T>::mma(L::transposed(dt, qb * 32, t, db, lane), pf, dv[db]);
-#pragma unroll
-        for (int db = 0; db < DB; ++db) dk[db] = Operand<T>::mma(L::transposed(qt, qb * 32, t, db, lane), gf, dk[db]);
+        for (int i = 0; i < 4; ++i) s[4 * r4 + i] = __builtin_amdgcn_exp2f(fmaf(s[4 * r4 + i], scale, -lse[i]));
       }
     }
-    if (it + 1 < tiles) store(it + 1);
+    pin();
+    // dv takes p; meanwhile g becomes p (g - delta)
+    auto scaled = [&](int r4) {
+      const f32x4 delta = *reinterpret_cast<const f32x4 *>(rows_delta + 8 * r4);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) g[4 * r4 + i] = s[4 * r4 + i] * (g[4 * r4 + i] - delta[i]);
+    };
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      const Frag pf = Operand<T>::of(s, t);
+#pragma unroll
+      for (int db = 0; db < DB; ++db) {
+        const int i = t * DB + db;
+        pin();
+        dv[db] = Operand<T>::mma(x[i & 3], pf, dv[db]);
+        x[i & 3] = next_of(i + 4);
+        if (db % (DB / 2) == 0) scaled(2 * t + db / (DB / 2));
+      }
+    }
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      const Frag gf = Operand<T>::of(g, t);
+#pragma unroll
+      for (int db = 0; db < DB; ++db) {
+        const int i = (2 + t) * DB + db;
+        pin();
+        dk[db] = Operand<T>::mma(x[i & 3], gf, dk[db]);
+        if (i + 4 < 4 * DB) x[i & 3] = next_of(i + 4);
+      }
+    }
+    pin();
+    if (it + 1 < tiles) hand_over(~it & 1);
+    read.move(it & 1 ? uint32_t(-2 * kTile) : uint32_t(2 * kTile));
   }
   __syncthreads();
   if (rows <= 0) return;
@@ -277,9 +348,9 @@ hipError_t allow_lds(F *kernel, int bytes) {
 
 template <typename T, int DH>
 hipError_t launch_backward(const BackwardArgs<T> &a, hipStream_t st) {
-  constexpr int row = Tile<T, DH>::kRow, waves = 4 * 32 * row;         // every wave's own 32 rows at the beginning and the end
-  constexpr int dq_tiles = 4 * kDqKeys<T> * row, dkv_tiles = 4 * kDkvQueries<T> * row;
-  constexpr int dq_lds = dq_tiles > waves ? dq_tiles : waves, dkv_lds = dkv_tiles > waves ? dkv_tiles : waves;
+  // a stage, and behind it another one or every wave's own 32 rows, for the operands at the beginning and the results at the end
+  constexpr int row = Tile<T, DH>::kRow, waves = 4 * 32 * row, dq_stage = 2 * kDqKeys<T> * row;
+  constexpr int dq_lds = dq_stage + (dq_stage > waves ? dq_stage : waves), dkv_lds = 4 * kDkvQueries<T> * row + waves + 4 * kDkvQueries<T> * 4;
   hipError_t e = allow_lds(&prompt_dq_kernel<T, DH>, dq_lds);
   if (e == hipSuccess) e = allow_lds(&prompt_dkv_kernel<T, DH>, dkv_lds);
   if (e != hipSuccess) return e;

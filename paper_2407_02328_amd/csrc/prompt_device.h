@@ -131,6 +131,14 @@ __device__ __forceinline__ size_t row_value(bool packed, int b, int first, int t
   return packed ? size_t(h) * tokens + first : (size_t(b) * heads + h) * tokens;
 }
 
+// A kernel that is to have N waves a SIMD, no more: the compiler then uses the registers that leaves.
+#define ADORE_WAVES(N) __attribute__((amdgpu_waves_per_eu(N, N)))
+// What stands before it is issued before what stands behind it.
+__device__ __forceinline__ void pin() { __builtin_amdgcn_sched_barrier(0); }
+
+// A row's log-sum-exp as the subtrahend of exponents in base 2: +inf for a row that sees nothing, whose weights are then 0 and not NaN.
+__device__ __forceinline__ float subtrahend(float lse) { return lse == -INFINITY ? INFINITY : lse * 1.4426950408889634f; }
+
 // ---- matrix products ------------------------------------------------------------------------------------------
 __device__ __forceinline__ uint32_t pair_bf16(float a, float b) {   // rounded to nearest, ties to even
   return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{a, b}, bf16x2));
@@ -174,82 +182,158 @@ struct Operand<float> {
 };
 
 // ---- tiles in LDS -----------------------------------------------------------------------------------------------
-// R rows of DH elements, in 16-byte chunks that are permuted within their row so that neither 8 rows x 1 chunk (an operand by rows) nor 4
-// rows x 2 neighbouring chunks (transposed) meet in a bank.
+// R rows of DH elements, in 16-byte chunks that are permuted within their row (an exclusive or with a number that goes by the row) so
+// that neither the rows of an operand at one chunk nor 4 rows x 2 neighbouring chunks (transposed) meet in a bank.
 template <typename T, int DH>
 struct Tile {
   static constexpr int kRow = DH * int(sizeof(T));
   static constexpr int kChunks = kRow / 16;
-  __device__ static __forceinline__ int chunk_at(int r, int ch) {
-    if constexpr (sizeof(T) == 4) return r * kRow + ((ch ^ (r & 15)) << 4);
+  static constexpr int kPeriod = sizeof(T) == 2 && DH == 128 ? 16 : 8;
+  __device__ static __forceinline__ int turn(int r) {
+    if constexpr (sizeof(T) == 4) return r & 7;
     const int x = (r & 3) << 1 | ((r >> 2) & 1);
-    return DH == 128 ? r * kRow + ((ch ^ (x | (r & 8))) << 4) : r * kRow + ((ch ^ x) << 4);
+    return DH == 128 ? x | (r & 8) : x;
   }
-  // Row r, elements 16 t + 8 h .. + 7.
-  __device__ static __forceinline__ typename Operand<T>::type by_row(const unsigned char *tile, int r, int t, int h) {
-    if constexpr (sizeof(T) == 4) {
-      const f32x4 lo = *reinterpret_cast<const f32x4 *>(tile + chunk_at(r, 4 * t + 2 * h));
-      const f32x4 hi = *reinterpret_cast<const f32x4 *>(tile + chunk_at(r, 4 * t + 2 * h + 1));
+  __device__ static __forceinline__ int chunk_at(int r, int ch) { return r * kRow + ((ch ^ turn(r)) << 4); }
+};
+
+typedef const __attribute__((address_space(3))) char *LdsPtr;
+__device__ __forceinline__ uint32_t lds_offset(const void *p) { return uint32_t(uintptr_t((LdsPtr)(const char *)p)); }
+template <typename V>
+__device__ __forceinline__ V lds_read(uint32_t at) {
+  return *(const __attribute__((address_space(3))) V *)(LdsPtr)uintptr_t(at);
+}
+
+// A lane's operands out of tiles.  Everything that goes by the lane is in a few registers made once and moved from stage to stage;
+// constant rows and steps are offsets of the instructions (an exclusive or per read would be a third of the vector instructions).
+//   by_row(add, r0, t)          row r0 + c, elements 16 t + 8 h .. + 7
+//   transposed(add, r0, t, db)  column 32 db + c, rows r0 + 16 t + 8 (e / 4) + 4 h + e % 4, e = 0 .. 7
+// of the tile `add` bytes behind the place the reader is at; r0: a multiple of 32.
+// FEW: one register for the rows instead of one per step, at an exclusive or a read (tiles then start at multiples of a row).
+template <typename T, int DH, bool FEW = false>
+struct Reader {
+  typedef Tile<T, DH> L;
+  typedef typename Operand<T>::type Frag;
+  static constexpr bool F32 = sizeof(T) == 4;
+  static constexpr int NR = F32 ? 4 : FEW ? 1 : DH / 16, NC = F32 ? 4 : DH / 32;
+  uint32_t row[NR], col[NC];
+  __device__ __forceinline__ void move(uint32_t by) {
+#pragma unroll
+    for (int i = 0; i < NR; ++i) row[i] += by;
+#pragma unroll
+    for (int i = 0; i < NC; ++i) col[i] += by;
+  }
+  __device__ __forceinline__ Reader(uint32_t place, int lane) {
+    const int c = lane & 31, h = lane >> 5;
+    if constexpr (F32) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        row[i] = uint32_t(L::chunk_at(c, 4 * (i >> 1) + 2 * h + (i & 1)));
+        col[i] = uint32_t(L::chunk_at(4 * h + i, c >> 2) + (c & 3) * 4);
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < NR; ++i) row[i] = uint32_t(L::chunk_at(c, 2 * i + h));
+      // 16 lanes read 4 rows x 16 columns, and each gets 4 rows of its column
+      const int grp = lane >> 4, r = 4 * (grp >> 1) + ((lane & 15) >> 2), x = (grp & 1) * 16 + (lane & 3) * 4;
+#pragma unroll
+      for (int i = 0; i < NC; ++i) col[i] = uint32_t(L::chunk_at(r, (32 * i + x) >> 3) + (x & 4) * 2);
+    }
+    move(place);
+  }
+  __device__ __forceinline__ Frag by_row(uint32_t ahead, int r0, int t) const {
+    if constexpr (F32) {
+      const uint32_t add = ahead + uint32_t(r0 * L::kRow + (t >> 1) * 128);
+      const f32x4 lo = lds_read<f32x4>(row[2 * (t & 1)] + add), hi = lds_read<f32x4>(row[2 * (t & 1) + 1] + add);
       return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
     } else {
-      return *reinterpret_cast<const bf16x8 *>(tile + chunk_at(r, 2 * t + h));
+      // (step t is bits 1 .. 3 of the chunk, which the permutation turns over one by one)
+      return lds_read<bf16x8>((FEW ? row[0] ^ uint32_t(t << 5) : row[FEW ? 0 : t]) + (ahead + uint32_t(r0 * L::kRow)));
     }
   }
-  // Column 32 db + c, rows r0 + 16 t + 8 (e / 4) + 4 h + e % 4, e = 0 .. 7 (r0 a multiple of 32).
-  __device__ static __forceinline__ typename Operand<T>::type transposed(const unsigned char *tile, int r0, int t, int db, int lane) {
-    const int c = lane & 31, h = lane >> 5;
-    if constexpr (sizeof(T) == 4) {
+  __device__ __forceinline__ Frag transposed(uint32_t ahead, int r0, int t, int db) const {
+    if constexpr (F32) {
       f32x8 v;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const int r = r0 + 16 * t + 8 * (e / 4) + 4 * h + e % 4;
-        v[e] = *reinterpret_cast<const float *>(tile + chunk_at(r, (32 * db + c) >> 2) + (c & 3) * 4);
-      }
+      for (int e = 0; e < 8; ++e) v[e] = lds_read<float>(col[e & 3] + (ahead + uint32_t((r0 + 16 * t + 8 * (e >> 2)) * L::kRow + 128 * db)));
       return v;
     } else {
-      // 16 lanes read 4 rows x 16 columns, and each gets 4 rows of its column
-      const int grp = lane >> 4, row = 4 * (grp >> 1) + ((lane & 15) >> 2), col = 32 * db + (grp & 1) * 16 + (lane & 3) * 4;
       union {
         s16x4 q[2];
         bf16x8 v;
       } u;
 #pragma unroll
-      for (int e4 = 0; e4 < 2; ++e4) {
-        const int at = chunk_at(r0 + 16 * t + 8 * e4 + row, col >> 3) + (col & 4) * 2;
-        u.q[e4] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)(tile + at));
+      for (int e4 = 0; e4 < 2; ++e4) {       // rows 8 further on: the other half of the permutation at 128 elements
+        const uint32_t at = col[DH == 128 ? db ^ (2 * e4) : db] + (ahead + uint32_t((r0 + 16 * t + 8 * e4) * L::kRow));
+        u.q[e4] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)(LdsPtr)uintptr_t(at));
       }
       return u.v;
     }
   }
 };
 
-// A tile's way from memory to LDS: NT threads carry R rows of DH elements, 16 bytes at a time, in registers in between.
-template <typename T, int DH, int R, int NT>
-struct Carrier {
+// 32 rows' way from memory to the wave's own LDS, 16 bytes at a time; rows from `rows` on are zeros.
+template <typename T, int DH>
+__device__ __forceinline__ void carry_rows(const char *base, int64_t stride, int rows, unsigned char *own, int lane) {
   typedef Tile<T, DH> L;
-  static constexpr int N = R * L::kChunks / NT;
-  static_assert(N * NT == R * L::kChunks, "whole chunks per thread");
+  constexpr int N = 32 * L::kChunks / 64;
+  const int row = lane / L::kChunks, ch = lane % L::kChunks;
   u32x4 r[N];
-  // Rows first .. first + R - 1 of the row array at `base` (row stride in bytes); rows from `end` on read as row end - 1, or as zeros.
-  template <bool ZEROS>
-  __device__ __forceinline__ void load(const char *base, int64_t stride, int first, int end, int tid) {
-    const char *at = base + int64_t(first) * stride;
-    const int row = tid / L::kChunks, col = tid % L::kChunks * 16;
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-      const int mine = row + i * (NT / L::kChunks);
-      const int there = min(mine, end - 1 - first);
-      r[i] = *reinterpret_cast<const u32x4 *>(at + (uint32_t(there) * uint32_t(stride) + uint32_t(col)));
-      if (ZEROS && mine != there) r[i] = u32x4{0, 0, 0, 0};
+  for (int i = 0; i < N; ++i) {
+    const int mine = row + i * (64 / L::kChunks);
+    r[i] = *reinterpret_cast<const u32x4 *>(base + int64_t(min(mine, rows - 1)) * stride + ch * 16);
+    if (mine >= rows) r[i] = u32x4{0, 0, 0, 0};
+  }
+#pragma unroll
+  for (int i = 0; i < N; ++i) *reinterpret_cast<u32x4 *>(own + L::chunk_at(row + i * (64 / L::kChunks), ch)) = r[i];
+}
+
+// 32 rows from `base` (zeros from `rows` on) as an operand, through the wave's own LDS, `ahead` of the reader.
+template <typename T, int DH, bool FEW>
+__device__ __forceinline__ void operand_rows(typename Operand<T>::type (&f)[DH / 16], const Reader<T, DH, FEW> &read, const char *base,
+                                             int64_t stride, int rows, unsigned char *own, uint32_t ahead, int lane) {
+  wave_lds_fence();
+  if (rows > 0) carry_rows<T, DH>(base, stride, rows, own, lane);
+  wave_lds_fence();
+#pragma unroll
+  for (int t = 0; t < DH / 16; ++t) f[t] = read.by_row(ahead, 0, t);
+}
+
+// A tile's way from memory straight to LDS (no registers): R rows of DH elements, NT threads.  A wave's load fills 1 KB of LDS in lane
+// order, so the lanes read the chunks that the tile's permutation wants there.  Rows from `end` on read as row end - 1.
+// `arrived()` behind the loads and ahead of the barrier that hands the tile over: what the compiler does not count.
+template <typename T, int DH, int R, int NT>
+struct TileLoad {
+  typedef Tile<T, DH> L;
+  static constexpr int kPer = NT / L::kChunks, N = R / kPer;    // rows of a load of the workgroup's
+  static_assert(N * kPer == R && kPer % L::kPeriod == 0, "a thread's chunk has the same place in all of its rows");
+  uint32_t at, pitch;        // bytes from the tile's first row to the thread's chunk, from row to row
+  int64_t step;              // bytes from one load of the workgroup's to the next
+  __device__ __forceinline__ TileLoad(int64_t stride, int tid) : pitch(uint32_t(stride)), step(stride * kPer) {
+    at = uint32_t(tid / L::kChunks) * pitch + col_of(tid);
+  }
+  __device__ static __forceinline__ uint32_t col_of(int tid) { return uint32_t(((tid % L::kChunks) ^ L::turn(tid / L::kChunks)) << 4); }
+  // p: the tile's first row; left: rows from there on, at least one; lds: the tile's byte offset in LDS plus the wave's share of a
+  // load (wave * 1024)
+  __device__ __forceinline__ void operator()(const char *p, int left, uint32_t lds) const {
+    if (left >= R) {
+#pragma unroll
+      for (int i = 0; i < N; ++i, p += step) to_lds(p, at, lds + uint32_t(i * NT * 16));
+    } else {
+      int tid = threadIdx.x;
+      asm("" : "+v"(tid));   // what only a sequence's last tile needs is worked out there, not kept in registers
+      const int row = tid / L::kChunks;
+#pragma unroll
+      for (int i = 0; i < N; ++i) to_lds(p, uint32_t(min(row + i * kPer, left - 1)) * pitch + col_of(tid), lds + uint32_t(i * NT * 16));
     }
   }
-  __device__ __forceinline__ void store(unsigned char *tile, int tid) const {
-    const int row = tid / L::kChunks, ch = tid % L::kChunks;
-#pragma unroll
-    for (int i = 0; i < N; ++i) *reinterpret_cast<u32x4 *>(tile + L::chunk_at(row + i * (NT / L::kChunks), ch)) = r[i];
+  // (m0: nothing else in these kernels uses it.  As a builtin, the compiler would wait for the load ahead of every LDS read.)
+  __device__ static __forceinline__ void to_lds(const char *base, uint32_t off, uint32_t lds) {
+    asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(off), "s"(base) : "memory");
   }
 };
-
+__device__ __forceinline__ void arrived() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
 // The wave's transposed result o[db] (row = element 32 db + .., column = row c of 32) to the rows of `to`, through LDS of the wave's
 // own (32 rows of DH elements), for whole 16-byte stores.  rest, if given, takes what rounding to bf16 left, rounded.
 template <typename T, int DH>
