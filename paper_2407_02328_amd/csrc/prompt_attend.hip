@@ -27,6 +27,7 @@ struct AttendArgs {
   Rows<const T> q, k, v;
   Rows<T> out, rest;      // rest.p may be null
   float *lse;             // or null
+  bool by_work;
 };
 
 // Keys of a tile: 16 KB of K and as much of V at head dimension 128.
@@ -47,7 +48,7 @@ __global__ __launch_bounds__(256) ADORE_WAVES(sizeof(T) == 4 ? 1 : DH == 128 ? 2
   const int hk = blockIdx.x % a.s.kv_heads, item = blockIdx.x / a.s.kv_heads, head = hk * a.s.group + item % a.s.group;
   Sequence sq;
   int block;
-  if (!find_block<BQ, true>(a.s, item / a.s.group, sq, block)) {
+  if (!find_block<BQ, true>(a.s, item / a.s.group, a.by_work, sq, block)) {
     int first;
     const int n = tail_rows<BQ>(a.s.q_start, a.s.batch, a.s.q_tokens, block, first);
     zero_rows<T, DH>(a.out, head, first, n, tid, NT);
@@ -55,7 +56,6 @@ __global__ __launch_bounds__(256) ADORE_WAVES(sizeof(T) == 4 ? 1 : DH == 128 ? 2
     if (a.lse && tid < n) a.lse[size_t(head) * a.s.q_tokens + first + tid] = -INFINITY;
     return;
   }
-  block = (sq.nq + BQ - 1) / BQ - 1 - block;   // the longest first
   const int q0 = block * BQ + wave * 32, off = sq.nk - sq.nq;
   const int rows = min(32, sq.nq - q0);        // may be <= 0
   const char *kp = reinterpret_cast<const char *>(a.k.p + sq.b * a.k.seq + sq.k_first * a.k.token + hk * a.k.head);
@@ -184,13 +184,14 @@ __global__ __launch_bounds__(256) ADORE_WAVES(sizeof(T) == 4 ? 1 : DH == 128 ? 2
 }
 
 template <typename T, int DH, bool REST>
-hipError_t launch_attend_prompt(const AttendArgs<T> &a, hipStream_t st) {
+hipError_t launch_attend_prompt(AttendArgs<T> a, hipStream_t st) {
   // a stage, and behind it another one or the waves' 32 queries each
   constexpr int stage = 2 * kKeys<T> * Tile<T, DH>::kRow, waves = 4 * 32 * Tile<T, DH>::kRow, lds = stage + (stage > waves ? stage : waves);
   const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(&prompt_attend_kernel<T, DH, REST>),
                                            hipFuncAttributeMaxDynamicSharedMemorySize, lds);
   if (e != hipSuccess) return e;
   const long long blocks = blocks_at_most(a.s.q_start, a.s.batch, a.s.q_tokens, 128) * a.s.heads;
+  a.by_work = blocks < 1024;      // two for each place: beyond, what a sequence's blocks share counts for more (4096: 198 / 229 us)
   hipLaunchKernelGGL((prompt_attend_kernel<T, DH, REST>), dim3(unsigned(blocks)), dim3(256), lds, st, a);
   return hipGetLastError();
 }
@@ -204,6 +205,7 @@ struct ScoreArgs {
   Rows<const T> q, k;
   const float *lse;
   float *scores;
+  bool by_work;
 };
 
 template <typename T>
@@ -221,7 +223,7 @@ __global__ __launch_bounds__(256) void prompt_scores_kernel(const ScoreArgs<T> a
   const int hk = blockIdx.x % a.s.kv_heads;
   Sequence sq;
   int block;
-  if (!find_block<BK, false>(a.s, blockIdx.x / a.s.kv_heads, sq, block)) {
+  if (!find_block<BK, false>(a.s, blockIdx.x / a.s.kv_heads, a.by_work, sq, block)) {
     int first;
     const int n = tail_rows<BK>(a.s.k_start, a.s.batch, a.s.k_tokens, block, first);
     if (tid < n) a.scores[size_t(hk) * a.s.k_tokens + first + tid] = 0.f;
@@ -308,12 +310,13 @@ __global__ __launch_bounds__(256) void prompt_scores_kernel(const ScoreArgs<T> a
 }
 
 template <typename T, int DH>
-hipError_t launch_scores(const ScoreArgs<T> &a, hipStream_t st) {
+hipError_t launch_scores(ScoreArgs<T> a, hipStream_t st) {
   constexpr int tiles = 2 * kQueries<T> * Tile<T, DH>::kRow, keys = 128 * Tile<T, DH>::kRow, lds = tiles > keys ? tiles : keys;
   const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(&prompt_scores_kernel<T, DH>),
                                            hipFuncAttributeMaxDynamicSharedMemorySize, lds);
   if (e != hipSuccess) return e;
   const long long blocks = blocks_at_most(a.s.k_start, a.s.batch, a.s.k_tokens, 128) * a.s.kv_heads;
+  a.by_work = blocks < 1024;      // (as above; 1512: 177 / 197 us)
   hipLaunchKernelGGL((prompt_scores_kernel<T, DH>), dim3(unsigned(blocks)), dim3(256), lds, st, a);
   return hipGetLastError();
 }

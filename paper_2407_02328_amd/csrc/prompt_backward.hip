@@ -23,6 +23,7 @@ struct BackwardArgs {
   Rows<T> dq, dk, dv;
   const float *lse;
   float *delta;                              // laid out like lse
+  bool by_work;
 };
 
 // ---- delta: DH / EPL lanes a row, 16 bytes each ----
@@ -63,13 +64,12 @@ __global__ __launch_bounds__(256) ADORE_WAVES(sizeof(T) == 4 ? 1 : DH == 128 ? 2
   const int hk = blockIdx.x % a.s.kv_heads, item = blockIdx.x / a.s.kv_heads, head = hk * a.s.group + item % a.s.group;
   Sequence sq;
   int block;
-  if (!find_block<BQ, true>(a.s, item / a.s.group, sq, block)) {
+  if (!find_block<BQ, true>(a.s, item / a.s.group, a.by_work, sq, block)) {
     int first;
     const int n = tail_rows<BQ>(a.s.q_start, a.s.batch, a.s.q_tokens, block, first);
     zero_rows<T, DH>(a.dq, head, first, n, tid, NT);
     return;
   }
-  block = (sq.nq + BQ - 1) / BQ - 1 - block;
   const int q0 = block * BQ + wave * 32, off = sq.nk - sq.nq;
   const int rows = min(32, sq.nq - q0);
   const int64_t row = int64_t(sq.q_first) + q0, es = int64_t(sizeof(T));
@@ -191,7 +191,7 @@ __global__ __launch_bounds__(256) ADORE_WAVES(sizeof(T) == 2 ? 2 : 1) void promp
   const int hk = blockIdx.x % a.s.kv_heads;
   Sequence sq;
   int block;
-  if (!find_block<BK, false>(a.s, blockIdx.x / a.s.kv_heads, sq, block)) {
+  if (!find_block<BK, false>(a.s, blockIdx.x / a.s.kv_heads, a.by_work, sq, block)) {
     int first;
     const int n = tail_rows<BK>(a.s.k_start, a.s.batch, a.s.k_tokens, block, first);
     zero_rows<T, DH>(a.dk, hk, first, n, tid, NT);
@@ -347,7 +347,7 @@ hipError_t allow_lds(F *kernel, int bytes) {
 }
 
 template <typename T, int DH>
-hipError_t launch_backward(const BackwardArgs<T> &a, hipStream_t st) {
+hipError_t launch_backward(BackwardArgs<T> a, hipStream_t st) {
   // a stage, and behind it another one or every wave's own 32 rows, for the operands at the beginning and the results at the end
   constexpr int row = Tile<T, DH>::kRow, waves = 4 * 32 * row, dq_stage = 2 * kDqKeys<T> * row;
   constexpr int dq_lds = dq_stage + (dq_stage > waves ? dq_stage : waves), dkv_lds = 4 * kDkvQueries<T> * row + waves + 4 * kDkvQueries<T> * 4;
@@ -359,13 +359,16 @@ hipError_t launch_backward(const BackwardArgs<T> &a, hipStream_t st) {
     const long long blocks = ((long long)rows * a.s.heads + per - 1) / per;
     hipLaunchKernelGGL((prompt_delta_kernel<T, DH>), dim3(unsigned(blocks)), dim3(256), 0, st, a, rows);
     if ((e = hipGetLastError()) != hipSuccess) return e;
-    hipLaunchKernelGGL((prompt_dq_kernel<T, DH>), dim3(unsigned(blocks_at_most(a.s.q_start, a.s.batch, a.s.q_tokens, 128) * a.s.heads)), dim3(256),
-                       dq_lds, st, a);
+    const long long query_blocks = blocks_at_most(a.s.q_start, a.s.batch, a.s.q_tokens, 128) * a.s.heads;
+    a.by_work = query_blocks < 1024;
+    hipLaunchKernelGGL((prompt_dq_kernel<T, DH>), dim3(unsigned(query_blocks)), dim3(256), dq_lds, st, a);
     if ((e = hipGetLastError()) != hipSuccess) return e;
   }
-  if (a.s.k_tokens > 0)
-    hipLaunchKernelGGL((prompt_dkv_kernel<T, DH>), dim3(unsigned(blocks_at_most(a.s.k_start, a.s.batch, a.s.k_tokens, 128) * a.s.kv_heads)),
-                       dim3(256), dkv_lds, st, a);
+  if (a.s.k_tokens > 0) {
+    const long long key_blocks = blocks_at_most(a.s.k_start, a.s.batch, a.s.k_tokens, 128) * a.s.kv_heads;
+    a.by_work = key_blocks < 2048;   // 1024, with 4 to 64 tiles of 4 heads each: 796 -> 610 us
+    hipLaunchKernelGGL((prompt_dkv_kernel<T, DH>), dim3(unsigned(key_blocks)), dim3(256), dkv_lds, st, a);
+  }
   return hipGetLastError();
 }
 

@@ -79,28 +79,59 @@ inline long long blocks_at_most(const int32_t *start, int batch, int tokens, int
   return start ? (long long)tokens / rows + batch + 1 : (long long)batch * ((tokens + rows - 1) / rows);
 }
 
-// Block `item` of the sequences' blocks of ROWS rows (of q, or of k), one sequence behind the other.  False: none, and `block` is that
-// much behind the last one (tail_rows).  All 64 lanes of a wave call it together.
+// Block `item` of the sequences' blocks of ROWS rows of q (whose work grows with their index: they see all keys before them) or of k
+// (whose work falls).  The order: one sequence behind the other, each with its longest block first, so that what
+// one sequence's workgroups share stays in the L2; by_work: the longest of all sequences first, so that a launch of few workgroups
+// ends with short ones.  False: there is no such block, and `block` is how far behind the last one (tail_rows).  All 64 lanes of a wave
+// call it together.
 template <int ROWS, bool OF_Q>
-__device__ __forceinline__ bool find_block(const PromptShape &a, int item, Sequence &s, int &block) {
+__device__ __forceinline__ bool find_block(const PromptShape &a, int item, bool by_work, Sequence &s, int &block) {
   const int32_t *start = OF_Q ? a.q_start : a.k_start;
   const int tokens = OF_Q ? a.q_tokens : a.k_tokens;
   if (!start) {
-    const int per = (tokens + ROWS - 1) / ROWS, b = item / per;
-    block = item - b * per;
+    const int per = (tokens + ROWS - 1) / ROWS, b = by_work ? item % a.batch : item / per, i = by_work ? item / a.batch : item - b * per;
+    block = OF_Q ? per - 1 - i : i;
     s = sequence_at(a, b);
     return true;
   }
   const int lane = threadIdx.x & 63;
+  auto blocks_at = [&](int b) {
+    int n = 0, first;
+    if (b < a.batch) span(start, b, tokens, first, n);
+    return (n + ROWS - 1) / ROWS;
+  };
+  // by_work: the blocks with more than w in front of them (counted from the sequence's light end) are fewer than or as many as item
+  int w = 0;
+  if (by_work) {
+    auto heavier = [&](int than) {
+      int sum = 0;
+      for (int b0 = 0; b0 < a.batch; b0 += 64) sum += __builtin_amdgcn_readlane(wave_scan(max(0, blocks_at(b0 + lane) - than)), 63);
+      return sum;
+    };
+    const int all = heavier(0);
+    if (item >= all) {
+      block = item - all;
+      return false;
+    }
+    int hi = (tokens + ROWS - 1) / ROWS;      // heavier(hi) = 0 <= item < heavier(w)
+    while (hi - w > 1) {
+      const int mid = (w + hi) >> 1;
+      if (heavier(mid) <= item)
+        hi = mid;
+      else
+        w = mid;
+    }
+    item -= heavier(hi);                      // among the sequences with hi blocks or more, one block each
+    w = hi;
+  }
   int before = 0;
   for (int b0 = 0; b0 < a.batch; b0 += 64) {
-    int n = 0, first;
-    if (b0 + lane < a.batch) span(start, b0 + lane, tokens, first, n);
-    const int own = (n + ROWS - 1) / ROWS, upto = before + wave_scan(own);
+    const int n = blocks_at(b0 + lane), own = by_work ? (n >= w ? 1 : 0) : n, upto = before + wave_scan(own);
     const uint64_t beyond = __builtin_amdgcn_ballot_w64(upto > item);
     if (beyond) {
-      const int at = __builtin_ctzll(beyond);
-      block = item - __builtin_amdgcn_readlane(upto - own, at);
+      const int at = __builtin_ctzll(beyond), blocks = __builtin_amdgcn_readlane(n, at);
+      const int i = by_work ? blocks - w : item - __builtin_amdgcn_readlane(upto - own, at);
+      block = OF_Q ? blocks - 1 - i : i;
       s = sequence_at(a, __builtin_amdgcn_readfirstlane(b0 + at));
       return true;
     }

@@ -286,7 +286,7 @@ struct ReadArgs {
 template <typename T, int DH>
 __global__ __launch_bounds__(256) void q4_read_kernel(const ReadArgs<T> a) {
   typedef Block<DH> L;
-  constexpr int G = L::kGroups, EPL = Vec16<T>::EPL;
+  constexpr int EPL = Vec16<T>::EPL;
   __shared__ __align__(16) uint32_t s_v[DH][9];                          // 32 bytes an element, and a word that spreads the banks
   const int row = blockIdx.x / a.s.blocks, block = blockIdx.x % a.s.blocks, tid = threadIdx.x;
   const unsigned char *in = a.cache + (size_t(row) * a.s.blocks + block) * L::kBytes;
@@ -296,12 +296,12 @@ __global__ __launch_bounds__(256) void q4_read_kernel(const ReadArgs<T> a) {
     for (int j = 0; j < 4; ++j) s_v[i >> 1][(i & 1) * 4 + j] = u[j];
   }
   __syncthreads();
-  auto put = [&](T *to, const uint32_t (&c)[4], float unit) {
-    float x[32];
+  // eight elements a thread: whole lines
+  auto put = [&](T *to, uint32_t c, float unit) {
+    float x[8];
+    values_of(c, unit, x);
 #pragma unroll
-    for (int w = 0; w < 4; ++w) values_of(c[w], unit, x + 8 * w);
-#pragma unroll
-    for (int i = 0; i < 32 / EPL; ++i) {
+    for (int i = 0; i < 8 / EPL; ++i) {
       typename Vec16<T>::Raw r;
       T *e = reinterpret_cast<T *>(&r);
 #pragma unroll
@@ -309,24 +309,17 @@ __global__ __launch_bounds__(256) void q4_read_kernel(const ReadArgs<T> a) {
       Vec16<T>::store_raw(to + i * EPL, r);
     }
   };
-  for (int i = tid; i < kSlots * G; i += 256) {
-    const int slot = i / G, g = i % G, at = block * kSlots + slot;
+  for (int i = tid; i < kSlots * (DH / 8); i += 256) {
+    const int slot = i / (DH / 8), part = i % (DH / 8), g = part / 4, at = block * kSlots + slot;
     if (at >= a.s.slots) continue;
     const bool there = a.slot_pos[size_t(row) * a.s.slots + at] >= 0;
-    const size_t to = (size_t(row) * a.s.slots + at) * DH + 32 * g;
-    const u32x4 kc = *reinterpret_cast<const u32x4 *>(in + ((slot & 3) * 16 + (slot >> 2)) * (DH / 2) + g * 16);
-    uint32_t c[4];
+    const size_t to = (size_t(row) * a.s.slots + at) * DH + 8 * part;
+    const uint32_t kc = *reinterpret_cast<const uint32_t *>(in + ((slot & 3) * 16 + (slot >> 2)) * (DH / 2) + part * 4);
+    uint32_t vc = 0;
 #pragma unroll
-    for (int w = 0; w < 4; ++w) c[w] = there ? kc[w] : 0u;
-    put(a.k + to, c, power(in[L::kKScale + g * kSlots + slot]));
-#pragma unroll
-    for (int w = 0; w < 4; ++w) {
-      c[w] = 0;
-#pragma unroll
-      for (int j = 0; j < 8; ++j) c[w] |= (s_v[32 * g + 8 * w + j][slot >> 3] >> (4 * (slot & 7)) & 15u) << (4 * j);
-      c[w] = there ? c[w] : 0u;
-    }
-    put(a.v + to, c, power(in[L::kVScale + g * kSlots + slot]));
+    for (int j = 0; j < 8; ++j) vc |= (s_v[8 * part + j][slot >> 3] >> (4 * (slot & 7)) & 15u) << (4 * j);
+    put(a.k + to, there ? kc : 0u, there ? power(in[L::kKScale + g * kSlots + slot]) : 1.f);
+    put(a.v + to, there ? vc : 0u, there ? power(in[L::kVScale + g * kSlots + slot]) : 1.f);
   }
 }
 
@@ -343,12 +336,13 @@ struct StepArgs {
   float *part_o;                   // several workgroups a row: [row][pass][split][16][DH] unscaled sums,
   float *part_ml;                  // [row][pass][split][16][2] their maximum and sum,
   float *logit;                    // [row][group][64 blocks] the weights' exponents,
+  float *part_new;                 // [row][group] the new token's,
   uint64_t *part_key;              // [row][finishing workgroup] and the row's counter
   int32_t *arrived;
 };
 
 constexpr int kPassHeads = 16;     // heads of a pass
-constexpr int kFinishSlots = 2048; // slots of a finishing workgroup
+constexpr int kFinishSlots = 1024; // slots of a finishing workgroup
 
 // The token's place and position.  Whatever the cursor holds, the slot is one of the row's.
 __device__ __forceinline__ void cursor_of(const int32_t *cursor, int row, int slots, int &slot, int &n) {
@@ -391,22 +385,22 @@ __device__ __forceinline__ void terms_of(float (&x)[8], bf16x8 (&t)[N]) {
 // 16 / groups) a column is a (head, group): a lane scales its weights once, and of the products with all elements keeps its group's.
 // With more (WIDE) a column is a head, and a lane makes as many operands as there are groups.
 template <typename T, int DH, bool WIDE>
-__global__ __launch_bounds__(512) void q4_step_kernel(const StepArgs<T> a) {
+__global__ __launch_bounds__(576) void q4_step_kernel(const StepArgs<T> a) {
   typedef Block<DH> L;
   constexpr int G = L::kGroups, KW = DH / 32, NT = DH / 16, OG = WIDE ? G : 1;   // KW: code words of a lane and tile; NT: tiles of V
   constexpr int HEADS = WIDE ? kPassHeads : 16 / G;
   constexpr int QN = kQTerms<T>, PN = kPTerms<T>;
-  extern __shared__ __align__(16) float s_dyn[];    // [waves][HEADS][DH] sums, [waves][HEADS][2]; one workgroup a row: [HEADS][64 blocks] exponents
-  __shared__ uint64_t s_key[8];
+  extern __shared__ __align__(16) float s_dyn[];    // [waves + 1][HEADS][DH] sums, [waves + 1][HEADS][2]; one workgroup a row: [group][64 blocks] exponents
+  __shared__ uint64_t s_key[9];
   __shared__ float s_total[kPassHeads][2];
-  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), waves = blockDim.x >> 6;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), waves = (blockDim.x >> 6) - 1;
   const int c = lane & 15, quarter = lane >> 4;
   const bool alone = a.splits == 1 && a.passes == 1;
   const int row = blockIdx.x / a.splits, split = blockIdx.x % a.splits, pass = blockIdx.y, b = row / a.s.kv_heads, hk = row % a.s.kv_heads;
   const int K = a.s.slots, KP = a.s.blocks * kSlots;
   const int head0 = pass * kPassHeads, heads = min(HEADS, a.s.group - head0);    // (WIDE false: one pass)
   const int head = WIDE ? c : c / G, mygroup = WIDE ? 0 : c % G;
-  float *s_o = s_dyn, *s_ml = s_dyn + waves * HEADS * DH, *s_logit = s_ml + waves * HEADS * 2;
+  float *s_o = s_dyn, *s_ml = s_dyn + (waves + 1) * HEADS * DH, *s_logit = s_ml + (waves + 1) * HEADS * 2;
   int slot, n;
   cursor_of(a.cursor, row, K, slot, n);
   if (!alone && split == 0 && pass == 0 && tid == 0) a.arrived[row] = 0;
@@ -437,11 +431,11 @@ __global__ __launch_bounds__(512) void q4_step_kernel(const StepArgs<T> a) {
   struct Raw {
     uint32_t k[4][KW], kscale, v[NT][2];
     u32x4 vscale[OG];
-    int pos[16];
+    int pos;                         // of the lane's slot
   };
   unsigned char *cache = a.cache + size_t(row) * a.s.blocks * L::kBytes;
   const int32_t *pos = a.slot_pos + size_t(row) * K;
-  auto load = [&](int block, Raw &r) {
+  auto load_k = [&](int block, Raw &r) {
     const unsigned char *in = cache + size_t(block) * L::kBytes;
 #pragma unroll
     for (int t = 0; t < 4; ++t) {
@@ -457,6 +451,10 @@ __global__ __launch_bounds__(512) void q4_step_kernel(const StepArgs<T> a) {
       }
     }
     r.kscale = *reinterpret_cast<const uint32_t *>(in + L::kKScale + quarter * G / 4 * kSlots + 4 * c);
+    r.pos = block * kSlots + lane < K ? pos[block * kSlots + lane] : -1;
+  };
+  auto load_v = [&](int block, Raw &r) {
+    const unsigned char *in = cache + size_t(block) * L::kBytes;
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
       const u32x2 u = *reinterpret_cast<const u32x2 *>(in + L::kV + (16 * t + c) * 32 + quarter * 8);
@@ -465,108 +463,10 @@ __global__ __launch_bounds__(512) void q4_step_kernel(const StepArgs<T> a) {
     }
 #pragma unroll
     for (int g = 0; g < OG; ++g) r.vscale[g] = *reinterpret_cast<const u32x4 *>(in + L::kVScale + (WIDE ? g : mygroup) * kSlots + quarter * 16);
-    const int at = block * kSlots + quarter * 16;
-#pragma unroll
-    for (int i = 0; i < 16; ++i) r.pos[i] = at + i < K ? pos[at + i] : -1;
   };
 
-  // The new token's row, into the loaded block and into the cache.
-  auto insert = [&](int block, Raw &r) {
-    const int in = slot & 63, c0 = in >> 2, t0 = in & 3, q0 = in >> 4, j0 = in & 15;
-    unsigned char *to = cache + size_t(block) * L::kBytes;
-    float x[32];
-    auto group_of = [&](const T *src, int g) {
-      float big = 0.f;
-#pragma unroll
-      for (int i = 0; i < 32 / Vec16<T>::EPL; ++i) {
-        float y[Vec16<T>::EPL];
-        Vec16<T>::load(src + 32 * g + i * Vec16<T>::EPL, y);
-#pragma unroll
-        for (int e = 0; e < Vec16<T>::EPL; ++e) {
-          x[i * Vec16<T>::EPL + e] = number(y[e]);
-          big = fmaxf(big, fabsf(x[i * Vec16<T>::EPL + e]));
-        }
-      }
-      return scale_of(big);
-    };
-    const size_t src = (size_t(b) * a.s.kv_heads + hk) * DH;
-    const bool writes = pass == 0;
-    {
-      const int g = quarter * G / 4;
-      const uint32_t scale = group_of(a.k_new + src, g);
-      uint32_t code[KW];
-#pragma unroll
-      for (int s = 0; s < KW; ++s) {
-        float y[8];          // (half a group a lane where there are two groups only)
-#pragma unroll
-        for (int e = 0; e < 8; ++e) y[e] = G == 4 ? x[8 * s + e] : (quarter & 1 ? x[16 + (8 * s & 15) + e] : x[(8 * s & 15) + e]);
-        code[s] = codes_of(y, power(scale));
-      }
-      const bool mine = c == c0;
-#pragma unroll
-      for (int t = 0; t < 4; ++t)
-#pragma unroll
-        for (int s = 0; s < KW; ++s) r.k[t][s] = mine && t == t0 ? code[s] : r.k[t][s];
-      r.kscale = mine ? (r.kscale & ~(255u << (8 * t0))) | scale << (8 * t0) : r.kscale;
-      if (mine && writes) {
-        uint32_t *p = reinterpret_cast<uint32_t *>(to + (16 * t0 + c0) * (DH / 2) + quarter * (DH / 8));
-#pragma unroll
-        for (int s = 0; s < KW; ++s) p[s] = code[s];
-        to[L::kKScale + g * kSlots + in] = uint8_t(scale);
-        if (a.k_held) {
-#pragma unroll
-          for (int s = 0; s < KW; ++s) {
-            float y[8];
-            values_of(code[s], power(scale), y);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) store_elem(a.k_held + src + quarter * (DH / 4) + 8 * s + e, y[e]);
-          }
-        }
-      }
-    }
-    uint32_t scales[G];
-#pragma unroll
-    for (int g = 0; g < G; ++g) scales[g] = group_of(a.v_new + src, g);
-    const bool mine = quarter == q0;
-#pragma unroll
-    for (int t = 0; t < NT; ++t) {
-      const int e = 16 * t + c;
-      const float y = number(to_float(a.v_new[src + e])), unit = power(scales[t / 2]);
-      const uint32_t code = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(0u, y, 0.f, unit, 0) & 15u;
-      const int sh = 4 * (j0 & 7);
-#pragma unroll
-      for (int u = 0; u < 2; ++u)
-        if (mine && (j0 >> 3) == u) {
-          r.v[t][u] = (r.v[t][u] & ~(15u << sh)) | code << sh;
-          if (writes) *reinterpret_cast<uint32_t *>(to + L::kV + e * 32 + quarter * 8 + u * 4) = r.v[t][u];
-        }
-      if (mine && writes && a.v_held) store_elem(a.v_held + src + e, __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(code, unit, 0)[0]);
-    }
-    if (mine) {
-#pragma unroll
-      for (int g = 0; g < OG; ++g) {
-        uint32_t scale = scales[g];
-        if constexpr (!WIDE) {
-#pragma unroll
-          for (int i = 1; i < G; ++i) scale = mygroup == i ? scales[i] : scale;
-        }
-#pragma unroll
-        for (int w = 0; w < 4; ++w)
-          if ((j0 >> 2) == w) r.vscale[g][w] = (r.vscale[g][w] & ~(255u << (8 * (j0 & 3)))) | scale << (8 * (j0 & 3));
-      }
-#pragma unroll
-      for (int i = 0; i < 16; ++i) r.pos[i] = i == j0 ? n : r.pos[i];
-      if (writes && c < G) {
-        uint32_t scale = scales[0];
-#pragma unroll
-        for (int i = 1; i < G; ++i) scale = c == i ? scales[i] : scale;
-        to[L::kVScale + c * kSlots + in] = uint8_t(scale);
-      }
-    }
-  };
-
-  float *logits = alone ? s_logit : a.logit + (size_t(row) * a.s.group + head0) * KP;
-  auto attend = [&](int block, const Raw &r) {
+  // The wave's next block takes the registers of this one's K as soon as they are free, then those of V.
+  auto attend = [&](int block, int next, Raw &r) {
     f32x4 s[4];
 #pragma unroll
     for (int t = 0; t < 4; ++t) {
@@ -578,18 +478,29 @@ __global__ __launch_bounds__(512) void q4_step_kernel(const StepArgs<T> a) {
 #pragma unroll
         for (int i = QN - 1; i >= 0; --i) s[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[w][i], s[t], 0, 0, 0);
       }
+      pin();                                       // operands are made as they are needed: all at once they would take 64 registers
     }
     float m = -INFINITY;
+    uint64_t there = __builtin_amdgcn_ballot_w64(r.pos >= 0);
+    if (next < a.s.blocks) load_k(next, r);
+    if (block == slot >> 6) there &= ~(uint64_t(1) << (slot & 63));   // what it held goes; the new token comes in with the sums
+    const uint32_t mine = uint32_t((quarter & 2 ? there >> 32 : there) >> (quarter & 1 ? 16 : 0));
 #pragma unroll
     for (int i = 0; i < 16; ++i) {                 // slot 16 quarter + i is row i / 4 of tile i % 4
-      const float x = r.pos[i] < 0 ? -INFINITY : s[i & 3][i >> 2] * a.s.scale_log2;
+      const float x = mine >> i & 1 ? s[i & 3][i >> 2] * a.s.scale_log2 : -INFINITY;
       s[i & 3][i >> 2] = x;
       m = fmaxf(m, x);
     }
     if ((WIDE || mygroup == 0) && head < heads) {
-      float *to = logits + size_t(head) * KP + block * kSlots + quarter * 16;
+      const size_t at = size_t(head) * KP + block * kSlots + quarter * 16;
+      if (alone) {
 #pragma unroll
-      for (int j = 0; j < 4; ++j) *reinterpret_cast<f32x4 *>(to + 4 * j) = f32x4{s[0][j], s[1][j], s[2][j], s[3][j]};
+        for (int j = 0; j < 4; ++j) *reinterpret_cast<f32x4 *>(s_logit + at + 4 * j) = f32x4{s[0][j], s[1][j], s[2][j], s[3][j]};
+      } else {
+        float *to = a.logit + (size_t(row) * a.s.group + head0) * KP + at;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) *reinterpret_cast<f32x4 *>(to + 4 * j) = f32x4{s[0][j], s[1][j], s[2][j], s[3][j]};
+      }
     }
     m = fmaxf(top, max_lane_xor<32>(max_lane_xor<16>(m)));
     const float base = m == -INFINITY ? 0.f : m;
@@ -613,7 +524,8 @@ __global__ __launch_bounds__(512) void q4_step_kernel(const StepArgs<T> a) {
       for (int g = 0; g < OG; ++g) {
         float x[8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) x[i] = p[8 * u + i] * power(r.vscale[g][2 * u + (i >> 2)] >> (8 * (i & 3)) & 255u);
+        for (int i = 0; i < 8; ++i)            // (0 stays 0 whatever a free slot's scale is, which a product with infinity would not)
+          x[i] = __builtin_ldexpf(p[8 * u + i], int(r.vscale[g][2 * u + (i >> 2)] >> (8 * (i & 3)) & 255u) - 127);
         terms_of<PN>(x, pf[g]);
       }
 #pragma unroll
@@ -621,21 +533,81 @@ __global__ __launch_bounds__(512) void q4_step_kernel(const StepArgs<T> a) {
         const bf16x8 vf = operand_of(r.v[t][u], 1.f);
 #pragma unroll
         for (int i = PN - 1; i >= 0; --i) o[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[WIDE ? t / 2 : 0][i], o[t], 0, 0, 0);
+        if (t % 2) pin();
       }
     }
+    if (next < a.s.blocks) load_v(next, r);
   };
 
-  const int stride = a.splits * waves;
-  for (int block = split * waves + wave; block < a.s.blocks; block += stride) {
+  const bool mine = wave < waves;                            // else the wave of the new token
+  if (mine) {
+    int block = split * waves + wave;
     Raw r;
-    load(block, r);
-    if (block == slot >> 6) insert(block, r);
-    attend(block, r);
+    if (block < a.s.blocks) {
+      load_k(block, r);
+      load_v(block, r);
+    }
+    for (const int stride = a.splits * waves; block < a.s.blocks; block += stride) attend(block, block + stride, r);
   }
 
   // ---- the waves' sums together ----
+  // what the end wants of the first slots is on its way meanwhile
+  const bool early = alone && tid < K;
+  const float early_score = early ? a.score[size_t(row) * K + tid] : 0.f;
+  const int early_pos = early ? pos[tid] : -1;
+  // The new token is one more wave's sums: its exponent, 1, its V as it is held.  Its codes go to memory meanwhile: what the block's own
+  // wave reads of them counts for nothing.
+  if (!mine) {
+    const bool here = (slot >> 6) / waves % a.splits == split, in = lane < DH / 2;
+    const size_t src = (size_t(b) * a.s.kv_heads + hk) * DH + 2 * (in ? lane : 0);   // two neighbouring elements a lane (DH = 64: 32 lanes)
+    f32x2 held[2] = {f32x2{0.f, 0.f}, f32x2{0.f, 0.f}};
+    if (here) {
+      unsigned char *to = cache + size_t(slot >> 6) * L::kBytes;
+      const int at = slot & 63;
+#pragma unroll
+      for (int kv = 0; kv < 2; ++kv) {
+        const T *from = (kv ? a.v_new : a.k_new) + src;
+        const float x0 = number(to_float(from[0])), x1 = number(to_float(from[1]));
+        float big = fmaxf(fabsf(x0), fabsf(x1));              // of 16 lanes: 32 elements
+        big = fmaxf(big, __shfl_xor(big, 1, 64));
+        big = fmaxf(big, __shfl_xor(big, 2, 64));
+        big = fmaxf(big, __shfl_xor(big, 4, 64));
+        big = fmaxf(big, __shfl_xor(big, 8, 64));
+        const uint32_t scale = scale_of(big);
+        const uint32_t code = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(0u, x0, x1, power(scale), 0) & 255u;
+        held[kv] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(code, power(scale), 0);
+        if (in && pass == 0) {
+          if (kv == 0) {
+            to[((at & 3) * 16 + (at >> 2)) * (DH / 2) + lane] = uint8_t(code);
+          } else {
+            unsigned char *v = to + L::kV + 64 * lane + at / 2;
+            const int sh = 4 * (at & 1);
+            v[0] = uint8_t((v[0] & ~(15u << sh)) | (code & 15u) << sh);
+            v[32] = uint8_t((v[32] & ~(15u << sh)) | code >> 4 << sh);
+          }
+          if ((lane & 15) == 0) to[(kv ? L::kVScale : L::kKScale) + (lane >> 4) * kSlots + at] = uint8_t(scale);
+          T *out = kv ? a.v_held : a.k_held;
+          if (out) {
+            store_elem(out + src, held[kv][0]);
+            store_elem(out + src + 1, held[kv][1]);
+          }
+        }
+      }
+    }
+    for (int j = 0; j < heads; ++j) {
+      const T *q = a.q + (size_t(b) * a.s.heads + hk * a.s.group + head0 + j) * DH + 2 * (in ? lane : 0);
+      float x = in ? fmaf(to_float(q[0]), held[0][0], to_float(q[1]) * held[0][1]) : 0.f;
+      x = here ? wave_sum(x) * a.s.scale_log2 : -INFINITY;
+      if (lane == 0) {
+        s_ml[(waves * HEADS + j) * 2] = x;
+        s_ml[(waves * HEADS + j) * 2 + 1] = here ? 1.f : 0.f;
+        if (here && !alone) a.part_new[size_t(row) * a.s.group + head0 + j] = x;
+      }
+      if (in) *reinterpret_cast<f32x2 *>(&s_o[(waves * HEADS + j) * DH + 2 * lane]) = held[1];
+    }
+  }
   sum = add_lane_xor<32>(add_lane_xor<16>(sum));
-  if (head < heads) {
+  if (mine && head < heads) {
     if (quarter == 0 && (WIDE || mygroup == 0)) {
       s_ml[(wave * HEADS + head) * 2] = top;
       s_ml[(wave * HEADS + head) * 2 + 1] = sum;
@@ -647,9 +619,9 @@ __global__ __launch_bounds__(512) void q4_step_kernel(const StepArgs<T> a) {
   __syncthreads();
   if (tid < heads) {
     float m = -INFINITY, l = 0.f;
-    for (int w = 0; w < waves; ++w) m = fmaxf(m, s_ml[(w * HEADS + tid) * 2]);
+    for (int w = 0; w <= waves; ++w) m = fmaxf(m, s_ml[(w * HEADS + tid) * 2]);
     const float base = m == -INFINITY ? 0.f : m;
-    for (int w = 0; w < waves; ++w) l += s_ml[(w * HEADS + tid) * 2 + 1] * __builtin_amdgcn_exp2f(s_ml[(w * HEADS + tid) * 2] - base);
+    for (int w = 0; w <= waves; ++w) l += s_ml[(w * HEADS + tid) * 2 + 1] * __builtin_amdgcn_exp2f(s_ml[(w * HEADS + tid) * 2] - base);
     s_total[tid][0] = base;
     s_total[tid][1] = l;
     if (!alone) {
@@ -663,7 +635,7 @@ __global__ __launch_bounds__(512) void q4_step_kernel(const StepArgs<T> a) {
     const int j = i / DH, e = i % DH;
     const float base = s_total[j][0];
     float x = 0.f;
-    for (int w = 0; w < waves; ++w) x += s_o[(w * HEADS + j) * DH + e] * __builtin_amdgcn_exp2f(s_ml[(w * HEADS + j) * 2] - base);
+    for (int w = 0; w <= waves; ++w) x += s_o[(w * HEADS + j) * DH + e] * __builtin_amdgcn_exp2f(s_ml[(w * HEADS + j) * 2] - base);
     if (alone)
       store_elem(a.out + (size_t(b) * a.s.heads + hk * a.s.group + head0 + j) * DH + e, x / s_total[j][1]);
     else
@@ -673,10 +645,11 @@ __global__ __launch_bounds__(512) void q4_step_kernel(const StepArgs<T> a) {
   // ---- what the row's slots received, and the next one to go ----
   uint64_t key = ~uint64_t(0);
   for (int i = tid; i < K; i += blockDim.x) {
-    float x = i == slot ? 0.f : a.score[size_t(row) * K + i];
-    const int at = i == slot ? n : pos[i];
+    float x = i == slot ? 0.f : i == tid ? early_score : a.score[size_t(row) * K + i];
+    const int at = i == slot ? n : i == tid ? early_pos : pos[i];
     float p = 0.f;
-    for (int j = 0; j < heads; ++j) p += __builtin_amdgcn_exp2f(s_logit[size_t(j) * KP + i] - s_total[j][0]) / s_total[j][1];
+    for (int j = 0; j < heads; ++j)
+      p += __builtin_amdgcn_exp2f((i == slot ? s_ml[(waves * HEADS + j) * 2] : s_logit[size_t(j) * KP + i]) - s_total[j][0]) / s_total[j][1];
     x += p;
     if (at >= 0) a.score[size_t(row) * K + i] = x;
     if (i == slot) a.slot_pos[size_t(row) * K + i] = n;
@@ -693,45 +666,73 @@ __global__ __launch_bounds__(512) void q4_step_kernel(const StepArgs<T> a) {
 // arrive looks for the smallest key; keys and the counter go past the L2 (agent scope), nothing else is handed over.
 template <typename T, int DH>
 __global__ __launch_bounds__(256) void q4_finish_kernel(const StepArgs<T> a, int parts) {
-  extern __shared__ __align__(16) float s_dyn[];    // [group][2]
+  extern __shared__ __align__(16) float s_dyn[];    // [group][2] maximum and 1 / sum, [group][splits] factor of each workgroup's sums
   __shared__ uint64_t s_key[4];
   __shared__ int s_last;
   const int row = blockIdx.x / parts, part = blockIdx.x % parts, b = row / a.s.kv_heads, hk = row % a.s.kv_heads, tid = threadIdx.x;
-  const int K = a.s.slots, KP = a.s.blocks * kSlots;
+  const int K = a.s.slots, KP = a.s.blocks * kSlots, group = a.s.group;
+  float *s_factor = s_dyn + 2 * group;
   int slot, n;
   cursor_of(a.cursor, row, K, slot, n);
-  auto ml_of = [&](int j, int split) {
-    return a.part_ml + (((size_t(row) * a.passes + j / kPassHeads) * a.splits + split) * kPassHeads + j % kPassHeads) * 2;
-  };
-  for (int j = tid; j < a.s.group; j += 256) {
+  // the slots' part is on its way while the heads' sums are put together
+  constexpr int kOwn = kFinishSlots / 256, kEarly = 4;
+  const int first = part * kFinishSlots + tid;
+  auto exponent = [&](int i, int j) { return i == slot ? a.part_new[size_t(row) * group + j] : a.logit[(size_t(row) * group + j) * KP + i]; };
+  float score[kOwn], early[kOwn][kEarly];
+  int at[kOwn];
+#pragma unroll
+  for (int u = 0; u < kOwn; ++u) {
+    const int i = first + u * 256;
+    const bool there = i < K;
+    score[u] = there && i != slot ? a.score[size_t(row) * K + i] : 0.f;
+    at[u] = i == slot ? n : there ? a.slot_pos[size_t(row) * K + i] : -1;
+#pragma unroll
+    for (int j = 0; j < kEarly; ++j) early[u][j] = there && j < group ? exponent(i, j) : 0.f;
+  }
+  // a wave a head
+  for (int j = tid >> 6; j < group; j += 4) {
+    const int lane = tid & 63;
+    const float2 *ml = reinterpret_cast<const float2 *>(a.part_ml) + ((size_t(row) * a.passes + j / kPassHeads) * a.splits) * kPassHeads + j % kPassHeads;
     float m = -INFINITY, l = 0.f;
-    for (int s = 0; s < a.splits; ++s) m = fmaxf(m, ml_of(j, s)[0]);
+    for (int s = lane; s < a.splits; s += 64) m = fmaxf(m, ml[size_t(s) * kPassHeads].x);
+    for (int o = 32; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o, 64));
     const float base = m == -INFINITY ? 0.f : m;
-    for (int s = 0; s < a.splits; ++s) l += ml_of(j, s)[1] * __builtin_amdgcn_exp2f(ml_of(j, s)[0] - base);
-    s_dyn[2 * j] = base;
-    s_dyn[2 * j + 1] = 1.f / l;
+    for (int s = lane; s < a.splits; s += 64) {
+      const float2 x = ml[size_t(s) * kPassHeads];
+      const float f = __builtin_amdgcn_exp2f(x.x - base);
+      s_factor[j * a.splits + s] = f;
+      l = fmaf(x.y, f, l);
+    }
+    l = wave_sum(l);
+    if (lane == 0) {
+      s_dyn[2 * j] = base;
+      s_dyn[2 * j + 1] = 1.f / l;
+    }
   }
   __syncthreads();
-  for (int i = tid + part * 256; i < a.s.group * DH; i += parts * 256) {
+  for (int i = tid + part * 256; i < group * DH; i += parts * 256) {
     const int j = i / DH, e = i % DH;
+    const float *o = a.part_o + ((size_t(row) * a.passes + j / kPassHeads) * a.splits * kPassHeads + j % kPassHeads) * DH + e;
     float x = 0.f;
-    for (int s = 0; s < a.splits; ++s)
-      x += a.part_o[(((size_t(row) * a.passes + j / kPassHeads) * a.splits + s) * kPassHeads + j % kPassHeads) * DH + e] *
-           __builtin_amdgcn_exp2f(ml_of(j, s)[0] - s_dyn[2 * j]);
-    store_elem(a.out + (size_t(b) * a.s.heads + hk * a.s.group + j) * DH + e, x * s_dyn[2 * j + 1]);
+#pragma unroll 8
+    for (int s = 0; s < a.splits; ++s) x = fmaf(o[size_t(s) * (kPassHeads * DH)], s_factor[j * a.splits + s], x);
+    store_elem(a.out + (size_t(b) * a.s.heads + hk * group + j) * DH + e, x * s_dyn[2 * j + 1]);
   }
   uint64_t key = ~uint64_t(0);
-  const int end = min(K, (part + 1) * kFinishSlots);
-  for (int i = part * kFinishSlots + tid; i < end; i += 256) {
-    float x = i == slot ? 0.f : a.score[size_t(row) * K + i];
-    const int at = i == slot ? n : a.slot_pos[size_t(row) * K + i];
+#pragma unroll
+  for (int u = 0; u < kOwn; ++u) {
+    const int i = first + u * 256;
+    if (i >= K) break;
     float p = 0.f;
-    for (int j = 0; j < a.s.group; ++j)
-      p += __builtin_amdgcn_exp2f(a.logit[(size_t(row) * a.s.group + j) * KP + i] - s_dyn[2 * j]) * s_dyn[2 * j + 1];
-    x += p;
-    if (at >= 0) a.score[size_t(row) * K + i] = x;
+#pragma unroll
+    for (int j = 0; j < kEarly; ++j)
+      if (j < group) p += __builtin_amdgcn_exp2f(early[u][j] - s_dyn[2 * j]) * s_dyn[2 * j + 1];
+#pragma unroll 4
+    for (int j = kEarly; j < group; ++j) p += __builtin_amdgcn_exp2f(exponent(i, j) - s_dyn[2 * j]) * s_dyn[2 * j + 1];
+    const float x = score[u] + p;
+    if (at[u] >= 0) a.score[size_t(row) * K + i] = x;
     if (i == slot) a.slot_pos[size_t(row) * K + i] = n;
-    key = min_key(key, eviction_key(at, x, i, n + 1, a.s.recent));
+    key = min_key(key, eviction_key(at[u], x, i, n + 1, a.s.recent));
   }
   key = workgroup_min(key, s_key);
   if (tid == 0) {
@@ -779,7 +780,7 @@ constexpr int kMaxLds = 128 * 1024;
 int step_lds(const Q4Shape &s, int head_dim, const StepPlan &p) {
   const int heads = p.wide ? kPassHeads : 16 / (head_dim / 32);
   const long long logits = p.splits == 1 && p.passes == 1 ? (long long)s.group * s.blocks * kSlots : 0;
-  const long long bytes = ((long long)p.waves * heads * (head_dim + 2) + logits) * 4;
+  const long long bytes = ((long long)(p.waves + 1) * heads * (head_dim + 2) + logits) * 4;
   return bytes > kMaxLds ? kMaxLds + 1 : int(bytes);
 }
 StepPlan plan_step(const Q4Shape &s, int head_dim) {
@@ -795,6 +796,8 @@ StepPlan plan_step(const Q4Shape &s, int head_dim) {
     const long long want = (1024 + rows * p.passes - 1) / (rows * p.passes), able = (s.blocks + p.waves - 1) / p.waves;
     p.splits = int(want < able ? want : able);
     if (p.splits > 64) p.splits = 64;
+    const int most = 8192 / s.group;      // factors in the finishing workgroups' LDS
+    if (p.splits > most) p.splits = most > 1 ? most : 1;
   }
   if (p.splits == 1 && step_lds(s, head_dim, p) > kMaxLds) {   // the exponents of all slots are too many for LDS
     p.waves = 4;
@@ -806,7 +809,7 @@ StepPlan plan_step(const Q4Shape &s, int head_dim) {
 bool alone(const StepPlan &p) { return p.splits == 1 && p.passes == 1; }
 
 struct StepSpace {
-  size_t part_o, part_ml, logit, part_key, arrived, total;
+  size_t part_o, part_ml, logit, part_new, part_key, arrived, total;
 };
 StepSpace step_space(const Q4Shape &s, int head_dim, const StepPlan &p) {
   StepSpace w = {};
@@ -824,6 +827,7 @@ StepSpace step_space(const Q4Shape &s, int head_dim, const StepPlan &p) {
   w.part_o = take(parts * head_dim * 4);
   w.part_ml = take(parts * 8);
   w.logit = take(rows * s.group * s.blocks * kSlots * 4);
+  w.part_new = take(rows * s.group * 4);
   w.part_key = take(rows * p.parts * 8);
   w.arrived = take(rows * 4);
   w.total = at;
@@ -836,9 +840,9 @@ hipError_t launch_step(const StepArgs<T> &a, const StepPlan &p, hipStream_t st) 
   hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(&q4_step_kernel<T, DH, WIDE>), hipFuncAttributeMaxDynamicSharedMemorySize, kMaxLds);
   if (e != hipSuccess) return e;
   const unsigned rows = unsigned(a.s.batch) * unsigned(a.s.kv_heads);
-  hipLaunchKernelGGL((q4_step_kernel<T, DH, WIDE>), dim3(rows * unsigned(p.splits), unsigned(p.passes)), dim3(64 * p.waves), lds, st, a);
+  hipLaunchKernelGGL((q4_step_kernel<T, DH, WIDE>), dim3(rows * unsigned(p.splits), unsigned(p.passes)), dim3(64 * (p.waves + 1)), lds, st, a);
   if ((e = hipGetLastError()) != hipSuccess || alone(p)) return e;
-  hipLaunchKernelGGL((q4_finish_kernel<T, DH>), dim3(rows * unsigned(p.parts)), dim3(256), a.s.group * 8, st, a, p.parts);
+  hipLaunchKernelGGL((q4_finish_kernel<T, DH>), dim3(rows * unsigned(p.parts)), dim3(256), a.s.group * (2 + p.splits) * 4, st, a, p.parts);
   return hipGetLastError();
 }
 
@@ -865,6 +869,7 @@ int step_typed(const Q4Shape &s, int head_dim, const void *q, const void *k_new,
   a.part_o = reinterpret_cast<float *>(ws + w.part_o);
   a.part_ml = reinterpret_cast<float *>(ws + w.part_ml);
   a.logit = reinterpret_cast<float *>(ws + w.logit);
+  a.part_new = reinterpret_cast<float *>(ws + w.part_new);
   a.part_key = reinterpret_cast<uint64_t *>(ws + w.part_key);
   a.arrived = reinterpret_cast<int32_t *>(ws + w.arrived);
   hipError_t e;

@@ -295,3 +295,17 @@ def test_a_cursor_that_is_out_of_range_stays_within_its_row():
         assert bool((rows[0] == 7).all()) and bool((rows[2] == 7).all())
         slot = 0 if bad < 0 else 39
         assert int(cache.slot_pos[0, 0, slot]) == 3
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_what_free_slots_hold_does_not_matter(dtype):
+    """Any bytes in the cache's free slots, scales of 0 and 255 among them (a buffer that nobody has cleared)."""
+    torch, P = _mods()
+    dt = types()[dtype]
+    for H, K, byte in ((2, 100, 255), (2, 100, 0), (24, 70, 255), (8, 2000, 255)):
+        cache = P.Q4Cache(batch=1, heads=H, kv_heads=1, head_dim=128, slots=K, recent=3, dtype=dt)
+        cache.cache.fill_(byte)
+        m = Model(1, H, 1, 128, K, 3)
+        for i in range(3):
+            take_step(torch, cache, m, dt, 10 * i, f"H {H} K {K} byte {byte} step {i}")
+        compare(torch, cache, m, f"byte {byte}")
