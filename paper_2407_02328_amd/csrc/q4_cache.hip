@@ -75,14 +75,21 @@ struct Q4Shape {
 };
 
 __device__ __forceinline__ uint64_t min_key(uint64_t a, uint64_t b) { return a < b ? a : b; }
-// Smallest key of the workgroup, in thread 0 (at least); s: one word per wave.
+__device__ __forceinline__ uint32_t wave_min(uint32_t x) {
+  // a lane's neighbours come with the instruction (the row before where there is one, else itself); lane 63 has the result
+  auto take = [&](uint32_t y) { x = x < y ? x : y; };
+  take(uint32_t(__builtin_amdgcn_update_dpp(int(x), int(x), 0x111, 0xf, 0xf, false)));   // row_shr:1, 2, 4, 8
+  take(uint32_t(__builtin_amdgcn_update_dpp(int(x), int(x), 0x112, 0xf, 0xf, false)));
+  take(uint32_t(__builtin_amdgcn_update_dpp(int(x), int(x), 0x114, 0xf, 0xf, false)));
+  take(uint32_t(__builtin_amdgcn_update_dpp(int(x), int(x), 0x118, 0xf, 0xf, false)));
+  take(uint32_t(__builtin_amdgcn_update_dpp(int(x), int(x), 0x142, 0xa, 0xf, false)));   // row_bcast:15 into rows 1 and 3
+  take(uint32_t(__builtin_amdgcn_update_dpp(int(x), int(x), 0x143, 0xc, 0xf, false)));   // row_bcast:31 into rows 2 and 3
+  return uint32_t(__builtin_amdgcn_readlane(int(x), 63));
+}
+// Smallest key of the workgroup, in thread 0 (at least); s: one word per wave.  All threads call it.
 __device__ __forceinline__ uint64_t workgroup_min(uint64_t key, uint64_t *s) {
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) {
-    const uint32_t lo = __shfl_xor(uint32_t(key), o, 64), hi = __shfl_xor(uint32_t(key >> 32), o, 64);
-    key = min_key(key, uint64_t(hi) << 32 | lo);
-  }
-  __syncthreads();
+  const uint32_t high = wave_min(uint32_t(key >> 32)), low = wave_min(uint32_t(key >> 32) == high ? uint32_t(key) : ~0u);
+  key = uint64_t(high) << 32 | low;
   if ((threadIdx.x & 63) == 0) s[threadIdx.x >> 6] = key;
   __syncthreads();
   if (threadIdx.x == 0)
@@ -333,6 +340,7 @@ struct StepArgs {
   float *score;
   T *out, *k_held, *v_held;        // the latter two or null
   int splits, passes;              // workgroups that share a row's blocks, and passes over its heads (16 at a time at most)
+  int extra;                       // 1: a wave of its own for the new token
   float *part_o;                   // several workgroups a row: [row][pass][split][16][DH] unscaled sums,
   float *part_ml;                  // [row][pass][split][16][2] their maximum and sum,
   float *logit;                    // [row][group][64 blocks] the weights' exponents,
@@ -342,7 +350,7 @@ struct StepArgs {
 };
 
 constexpr int kPassHeads = 16;     // heads of a pass
-constexpr int kFinishSlots = 1024; // slots of a finishing workgroup
+constexpr int kFinishThreads = 1024, kFinishSlots = 4 * kFinishThreads;   // of a finishing workgroup
 
 // The token's place and position.  Whatever the cursor holds, the slot is one of the row's.
 __device__ __forceinline__ void cursor_of(const int32_t *cursor, int row, int slots, int &slot, int &n) {
@@ -385,15 +393,15 @@ __device__ __forceinline__ void terms_of(float (&x)[8], bf16x8 (&t)[N]) {
 // 16 / groups) a column is a (head, group): a lane scales its weights once, and of the products with all elements keeps its group's.
 // With more (WIDE) a column is a head, and a lane makes as many operands as there are groups.
 template <typename T, int DH, bool WIDE>
-__global__ __launch_bounds__(576) void q4_step_kernel(const StepArgs<T> a) {
+__global__ __launch_bounds__(512) void q4_step_kernel(const StepArgs<T> a) {
   typedef Block<DH> L;
   constexpr int G = L::kGroups, KW = DH / 32, NT = DH / 16, OG = WIDE ? G : 1;   // KW: code words of a lane and tile; NT: tiles of V
   constexpr int HEADS = WIDE ? kPassHeads : 16 / G;
   constexpr int QN = kQTerms<T>, PN = kPTerms<T>;
   extern __shared__ __align__(16) float s_dyn[];    // [waves + 1][HEADS][DH] sums, [waves + 1][HEADS][2]; one workgroup a row: [group][64 blocks] exponents
-  __shared__ uint64_t s_key[9];
+  __shared__ uint64_t s_key[8];
   __shared__ float s_total[kPassHeads][2];
-  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), waves = (blockDim.x >> 6) - 1;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), waves = int(blockDim.x >> 6) - a.extra;
   const int c = lane & 15, quarter = lane >> 4;
   const bool alone = a.splits == 1 && a.passes == 1;
   const int row = blockIdx.x / a.splits, split = blockIdx.x % a.splits, pass = blockIdx.y, b = row / a.s.kv_heads, hk = row % a.s.kv_heads;
@@ -539,35 +547,23 @@ __global__ __launch_bounds__(576) void q4_step_kernel(const StepArgs<T> a) {
     if (next < a.s.blocks) load_v(next, r);
   };
 
-  const bool mine = wave < waves;                            // else the wave of the new token
-  if (mine) {
-    int block = split * waves + wave;
-    Raw r;
-    if (block < a.s.blocks) {
-      load_k(block, r);
-      load_v(block, r);
-    }
-    for (const int stride = a.splits * waves; block < a.s.blocks; block += stride) attend(block, block + stride, r);
-  }
-
-  // ---- the waves' sums together ----
-  // what the end wants of the first slots is on its way meanwhile
-  const bool early = alone && tid < K;
-  const float early_score = early ? a.score[size_t(row) * K + tid] : 0.f;
-  const int early_pos = early ? pos[tid] : -1;
-  // The new token is one more wave's sums: its exponent, 1, its V as it is held.  Its codes go to memory meanwhile: what the block's own
-  // wave reads of them counts for nothing.
-  if (!mine) {
+  // The new token comes in with the waves' sums, as one more of them: its exponent, 1, its V as it is held.  Its codes go to memory
+  // meanwhile; what the block's own wave reads of them counts for nothing.  The last wave does it, while its first block is on
+  // its way or with nothing else to do.
+  auto new_token = [&]() {
     const bool here = (slot >> 6) / waves % a.splits == split, in = lane < DH / 2;
     const size_t src = (size_t(b) * a.s.kv_heads + hk) * DH + 2 * (in ? lane : 0);   // two neighbouring elements a lane (DH = 64: 32 lanes)
     f32x2 held[2] = {f32x2{0.f, 0.f}, f32x2{0.f, 0.f}};
     if (here) {
       unsigned char *to = cache + size_t(slot >> 6) * L::kBytes;
       const int at = slot & 63;
+      unsigned char *v = to + L::kV + 64 * (in ? lane : 0) + at / 2;
+      // all that it reads at once: a trip to memory takes as long as an attention wave's products
+      const T k0 = a.k_new[src], k1 = a.k_new[src + 1], v0 = a.v_new[src], v1 = a.v_new[src + 1];
+      const uint32_t old0 = v[0], old1 = v[32];
 #pragma unroll
       for (int kv = 0; kv < 2; ++kv) {
-        const T *from = (kv ? a.v_new : a.k_new) + src;
-        const float x0 = number(to_float(from[0])), x1 = number(to_float(from[1]));
+        const float x0 = number(to_float(kv ? v0 : k0)), x1 = number(to_float(kv ? v1 : k1));
         float big = fmaxf(fabsf(x0), fabsf(x1));              // of 16 lanes: 32 elements
         big = fmaxf(big, __shfl_xor(big, 1, 64));
         big = fmaxf(big, __shfl_xor(big, 2, 64));
@@ -580,10 +576,9 @@ __global__ __launch_bounds__(576) void q4_step_kernel(const StepArgs<T> a) {
           if (kv == 0) {
             to[((at & 3) * 16 + (at >> 2)) * (DH / 2) + lane] = uint8_t(code);
           } else {
-            unsigned char *v = to + L::kV + 64 * lane + at / 2;
             const int sh = 4 * (at & 1);
-            v[0] = uint8_t((v[0] & ~(15u << sh)) | (code & 15u) << sh);
-            v[32] = uint8_t((v[32] & ~(15u << sh)) | code >> 4 << sh);
+            v[0] = uint8_t((old0 & ~(15u << sh)) | (code & 15u) << sh);
+            v[32] = uint8_t((old1 & ~(15u << sh)) | code >> 4 << sh);
           }
           if ((lane & 15) == 0) to[(kv ? L::kVScale : L::kKScale) + (lane >> 4) * kSlots + at] = uint8_t(scale);
           T *out = kv ? a.v_held : a.k_held;
@@ -605,9 +600,25 @@ __global__ __launch_bounds__(576) void q4_step_kernel(const StepArgs<T> a) {
       }
       if (in) *reinterpret_cast<f32x2 *>(&s_o[(waves * HEADS + j) * DH + 2 * lane]) = held[1];
     }
+  };
+  {
+    int block = wave < waves ? split * waves + wave : a.s.blocks;
+    Raw r;
+    if (block < a.s.blocks) {
+      load_k(block, r);
+      load_v(block, r);
+    }
+    if (wave == waves - 1 + a.extra) new_token();
+    for (const int stride = a.splits * waves; block < a.s.blocks; block += stride) attend(block, block + stride, r);
   }
+
+  // ---- the waves' sums together ----
+  // what the end wants of the first slots is on its way meanwhile
+  const bool early = alone && tid < K;
+  const float early_score = early ? a.score[size_t(row) * K + tid] : 0.f;
+  const int early_pos = early ? pos[tid] : -1;
   sum = add_lane_xor<32>(add_lane_xor<16>(sum));
-  if (mine && head < heads) {
+  if (wave < waves && head < heads) {
     if (quarter == 0 && (WIDE || mygroup == 0)) {
       s_ml[(wave * HEADS + head) * 2] = top;
       s_ml[(wave * HEADS + head) * 2 + 1] = sum;
@@ -617,31 +628,36 @@ __global__ __launch_bounds__(576) void q4_step_kernel(const StepArgs<T> a) {
       if (WIDE || t / 2 == mygroup) *reinterpret_cast<f32x4 *>(&s_o[(wave * HEADS + head) * DH + 16 * t + 4 * quarter]) = o[t];
   }
   __syncthreads();
+  auto total = [&](int j, float &m, float &base, float &l) {
+    m = -INFINITY;
+    l = 0.f;
+    for (int w = 0; w <= waves; ++w) m = fmaxf(m, s_ml[(w * HEADS + j) * 2]);
+    base = m == -INFINITY ? 0.f : m;
+    for (int w = 0; w <= waves; ++w) l += s_ml[(w * HEADS + j) * 2 + 1] * __builtin_amdgcn_exp2f(s_ml[(w * HEADS + j) * 2] - base);
+  };
   if (tid < heads) {
-    float m = -INFINITY, l = 0.f;
-    for (int w = 0; w <= waves; ++w) m = fmaxf(m, s_ml[(w * HEADS + tid) * 2]);
-    const float base = m == -INFINITY ? 0.f : m;
-    for (int w = 0; w <= waves; ++w) l += s_ml[(w * HEADS + tid) * 2 + 1] * __builtin_amdgcn_exp2f(s_ml[(w * HEADS + tid) * 2] - base);
+    float m, base, l;
+    total(tid, m, base, l);
     s_total[tid][0] = base;
-    s_total[tid][1] = l;
+    s_total[tid][1] = 1.f / l;
     if (!alone) {
       float *ml = a.part_ml + (((size_t(row) * a.passes + pass) * a.splits + split) * kPassHeads + tid) * 2;
       ml[0] = m;
       ml[1] = l;
     }
   }
-  __syncthreads();
   for (int i = tid; i < heads * DH; i += blockDim.x) {
     const int j = i / DH, e = i % DH;
-    const float base = s_total[j][0];
-    float x = 0.f;
+    float m, base, l, x = 0.f;
+    total(j, m, base, l);
     for (int w = 0; w <= waves; ++w) x += s_o[(w * HEADS + j) * DH + e] * __builtin_amdgcn_exp2f(s_ml[(w * HEADS + j) * 2] - base);
     if (alone)
-      store_elem(a.out + (size_t(b) * a.s.heads + hk * a.s.group + head0 + j) * DH + e, x / s_total[j][1]);
+      store_elem(a.out + (size_t(b) * a.s.heads + hk * a.s.group + head0 + j) * DH + e, x / l);
     else
       a.part_o[(((size_t(row) * a.passes + pass) * a.splits + split) * kPassHeads + j) * DH + e] = x;
   }
   if (!alone) return;
+  __syncthreads();
   // ---- what the row's slots received, and the next one to go ----
   uint64_t key = ~uint64_t(0);
   for (int i = tid; i < K; i += blockDim.x) {
@@ -649,7 +665,7 @@ __global__ __launch_bounds__(576) void q4_step_kernel(const StepArgs<T> a) {
     const int at = i == slot ? n : i == tid ? early_pos : pos[i];
     float p = 0.f;
     for (int j = 0; j < heads; ++j)
-      p += __builtin_amdgcn_exp2f((i == slot ? s_ml[(waves * HEADS + j) * 2] : s_logit[size_t(j) * KP + i]) - s_total[j][0]) / s_total[j][1];
+      p += __builtin_amdgcn_exp2f((i == slot ? s_ml[(waves * HEADS + j) * 2] : s_logit[size_t(j) * KP + i]) - s_total[j][0]) * s_total[j][1];
     x += p;
     if (at >= 0) a.score[size_t(row) * K + i] = x;
     if (i == slot) a.slot_pos[size_t(row) * K + i] = n;
@@ -665,9 +681,9 @@ __global__ __launch_bounds__(576) void q4_step_kernel(const StepArgs<T> a) {
 // Several workgroups a row: their sums together, and the slots' share of the attention, kFinishSlots to a workgroup.  The last one to
 // arrive looks for the smallest key; keys and the counter go past the L2 (agent scope), nothing else is handed over.
 template <typename T, int DH>
-__global__ __launch_bounds__(256) void q4_finish_kernel(const StepArgs<T> a, int parts) {
+__global__ __launch_bounds__(kFinishThreads) void q4_finish_kernel(const StepArgs<T> a, int parts) {
   extern __shared__ __align__(16) float s_dyn[];    // [group][2] maximum and 1 / sum, [group][splits] factor of each workgroup's sums
-  __shared__ uint64_t s_key[4];
+  __shared__ uint64_t s_key[kFinishThreads / 64];
   __shared__ int s_last;
   const int row = blockIdx.x / parts, part = blockIdx.x % parts, b = row / a.s.kv_heads, hk = row % a.s.kv_heads, tid = threadIdx.x;
   const int K = a.s.slots, KP = a.s.blocks * kSlots, group = a.s.group;
@@ -675,14 +691,14 @@ __global__ __launch_bounds__(256) void q4_finish_kernel(const StepArgs<T> a, int
   int slot, n;
   cursor_of(a.cursor, row, K, slot, n);
   // the slots' part is on its way while the heads' sums are put together
-  constexpr int kOwn = kFinishSlots / 256, kEarly = 4;
+  constexpr int kOwn = kFinishSlots / kFinishThreads, kEarly = 4;
   const int first = part * kFinishSlots + tid;
   auto exponent = [&](int i, int j) { return i == slot ? a.part_new[size_t(row) * group + j] : a.logit[(size_t(row) * group + j) * KP + i]; };
   float score[kOwn], early[kOwn][kEarly];
   int at[kOwn];
 #pragma unroll
   for (int u = 0; u < kOwn; ++u) {
-    const int i = first + u * 256;
+    const int i = first + u * kFinishThreads;
     const bool there = i < K;
     score[u] = there && i != slot ? a.score[size_t(row) * K + i] : 0.f;
     at[u] = i == slot ? n : there ? a.slot_pos[size_t(row) * K + i] : -1;
@@ -690,7 +706,7 @@ __global__ __launch_bounds__(256) void q4_finish_kernel(const StepArgs<T> a, int
     for (int j = 0; j < kEarly; ++j) early[u][j] = there && j < group ? exponent(i, j) : 0.f;
   }
   // a wave a head
-  for (int j = tid >> 6; j < group; j += 4) {
+  for (int j = tid >> 6; j < group; j += kFinishThreads / 64) {
     const int lane = tid & 63;
     const float2 *ml = reinterpret_cast<const float2 *>(a.part_ml) + ((size_t(row) * a.passes + j / kPassHeads) * a.splits) * kPassHeads + j % kPassHeads;
     float m = -INFINITY, l = 0.f;
@@ -710,7 +726,7 @@ __global__ __launch_bounds__(256) void q4_finish_kernel(const StepArgs<T> a, int
     }
   }
   __syncthreads();
-  for (int i = tid + part * 256; i < group * DH; i += parts * 256) {
+  for (int i = tid + part * kFinishThreads; i < group * DH; i += parts * kFinishThreads) {
     const int j = i / DH, e = i % DH;
     const float *o = a.part_o + ((size_t(row) * a.passes + j / kPassHeads) * a.splits * kPassHeads + j % kPassHeads) * DH + e;
     float x = 0.f;
@@ -721,7 +737,7 @@ __global__ __launch_bounds__(256) void q4_finish_kernel(const StepArgs<T> a, int
   uint64_t key = ~uint64_t(0);
 #pragma unroll
   for (int u = 0; u < kOwn; ++u) {
-    const int i = first + u * 256;
+    const int i = first + u * kFinishThreads;
     if (i >= K) break;
     float p = 0.f;
 #pragma unroll
@@ -735,6 +751,13 @@ __global__ __launch_bounds__(256) void q4_finish_kernel(const StepArgs<T> a, int
     key = min_key(key, eviction_key(at[u], x, i, n + 1, a.s.recent));
   }
   key = workgroup_min(key, s_key);
+  if (parts == 1) {
+    if (tid == 0) {
+      a.cursor[2 * row] = int(uint32_t(key));
+      a.cursor[2 * row + 1] = n + 1;
+    }
+    return;
+  }
   if (tid == 0) {
     __hip_atomic_store(a.part_key + size_t(row) * parts + part, key, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");                 // the key is where the last one will look for it
@@ -743,7 +766,7 @@ __global__ __launch_bounds__(256) void q4_finish_kernel(const StepArgs<T> a, int
   __syncthreads();
   if (!s_last) return;
   key = ~uint64_t(0);
-  for (int i = tid; i < parts; i += 256)
+  for (int i = tid; i < parts; i += kFinishThreads)
     key = min_key(key, __hip_atomic_load(a.part_key + size_t(row) * parts + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT));
   key = workgroup_min(key, s_key);
   if (tid == 0) {
@@ -774,7 +797,7 @@ int q4_shape(const adore_q4_config *c, Q4Shape *s) {
 // How a step's work is cut.
 struct StepPlan {
   bool wide;
-  int passes, splits, waves, parts;
+  int passes, splits, waves, extra, parts;
 };
 constexpr int kMaxLds = 128 * 1024;
 int step_lds(const Q4Shape &s, int head_dim, const StepPlan &p) {
@@ -788,17 +811,22 @@ StepPlan plan_step(const Q4Shape &s, int head_dim) {
   p.wide = s.group > 16 / (head_dim / 32);
   p.passes = (s.group + kPassHeads - 1) / kPassHeads;
   const long long rows = (long long)s.batch * s.kv_heads;
-  p.waves = s.blocks >= 8 ? 8 : s.blocks >= 4 ? 4 : s.blocks;
-  // One workgroup a row wherever that fills the chip, or a wave has few blocks: no second launch.
+  // One workgroup a row wherever that fills the chip, or a wave has few blocks: no second launch.  Few large workgroups, whose waves have
+  // their next block on its way, rather than many small ones (4 sequences, 8 kv heads, 16384 slots: 256 workgroups of 8 waves 18 us,
+  // 512 20, 1024 28; of 4 waves 22, 25, 30).  With a row for every place (16 x 32 rows of 512 slots) 4 waves each 14 us, 3 15, 8 18.
+  // The new token has a wave of its own where a place has waves to spare (long rows 18 us / 20, a single row 5.4 / 6.2; 512 rows 14.9 / 14.0).
   p.splits = 1;
-  if (s.blocks > 16 && rows * p.passes < 512) {
-    p.waves = 4;
-    const long long want = (1024 + rows * p.passes - 1) / (rows * p.passes), able = (s.blocks + p.waves - 1) / p.waves;
+  const long long groups = rows * p.passes;
+  p.waves = groups >= 512 ? 4 : 7;
+  p.extra = groups >= 512 ? 0 : 1;
+  if (s.blocks > 16 && groups < 256) {
+    const long long want = (256 + groups - 1) / groups, able = (s.blocks + p.waves - 1) / p.waves;
     p.splits = int(want < able ? want : able);
     if (p.splits > 64) p.splits = 64;
     const int most = 8192 / s.group;      // factors in the finishing workgroups' LDS
     if (p.splits > most) p.splits = most > 1 ? most : 1;
   }
+  if (p.waves > s.blocks) p.waves = s.blocks;
   if (p.splits == 1 && step_lds(s, head_dim, p) > kMaxLds) {   // the exponents of all slots are too many for LDS
     p.waves = 4;
     p.splits = 2;
@@ -840,9 +868,9 @@ hipError_t launch_step(const StepArgs<T> &a, const StepPlan &p, hipStream_t st) 
   hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(&q4_step_kernel<T, DH, WIDE>), hipFuncAttributeMaxDynamicSharedMemorySize, kMaxLds);
   if (e != hipSuccess) return e;
   const unsigned rows = unsigned(a.s.batch) * unsigned(a.s.kv_heads);
-  hipLaunchKernelGGL((q4_step_kernel<T, DH, WIDE>), dim3(rows * unsigned(p.splits), unsigned(p.passes)), dim3(64 * (p.waves + 1)), lds, st, a);
+  hipLaunchKernelGGL((q4_step_kernel<T, DH, WIDE>), dim3(rows * unsigned(p.splits), unsigned(p.passes)), dim3(64 * (p.waves + p.extra)), lds, st, a);
   if ((e = hipGetLastError()) != hipSuccess || alone(p)) return e;
-  hipLaunchKernelGGL((q4_finish_kernel<T, DH>), dim3(rows * unsigned(p.parts)), dim3(256), a.s.group * (2 + p.splits) * 4, st, a, p.parts);
+  hipLaunchKernelGGL((q4_finish_kernel<T, DH>), dim3(rows * unsigned(p.parts)), dim3(kFinishThreads), a.s.group * (2 + p.splits) * 4, st, a, p.parts);
   return hipGetLastError();
 }
 
@@ -866,6 +894,7 @@ int step_typed(const Q4Shape &s, int head_dim, const void *q, const void *k_new,
   a.v_held = static_cast<T *>(v_held);
   a.splits = p.splits;
   a.passes = p.passes;
+  a.extra = p.extra;
   a.part_o = reinterpret_cast<float *>(ws + w.part_o);
   a.part_ml = reinterpret_cast<float *>(ws + w.part_ml);
   a.logit = reinterpret_cast<float *>(ws + w.logit);
