@@ -208,55 +208,61 @@ class _Prompts:
     The last dimension is dense, the others may have any strides that keep every row on a 16-byte boundary."""
 
     def __init__(self, q: torch.Tensor, k: torch.Tensor, q_start, k_start, scale):
+        # (once or twice a call, rows() up to twelve times: what short prompts take the GPU is not much more)
         if (q_start is None) != (k_start is None):
             raise ValueError("q_start and k_start: both or neither")
-        self.packed, self.device, self.dtype = q_start is not None, q.device, q.dtype
-        if q.dtype not in _CODES or not q.is_cuda:
+        code = _CODES.get(q.dtype)
+        index = q.get_device()
+        if code is None or index < 0:
             raise ValueError(f"q: expected a bf16 or fp32 GPU tensor, got {q.device} {q.dtype}")
-        dims = 3 if self.packed else 4
-        if q.dim() != dims or k.dim() != dims:
+        self.device, self.index, self.dtype = q.device, index, q.dtype
+        self.q_shape, self.k_shape = qs, ks = q.shape, k.shape
+        self.packed = packed = q_start is not None
+        if len(qs) != (3 if packed else 4) or len(ks) != len(qs):
             raise ValueError("q, k: expected [tokens, heads, head_dim] with starts, [batch, heads, tokens, head_dim] without")
-        heads, tokens = (1, 0) if self.packed else (1, 2)
-        self.starts = []
-        for name, t in (("q_start", q_start), ("k_start", k_start)):
-            if t is None:
-                self.starts.append(None)
-            elif t.dtype != torch.int32 or t.device != q.device or t.dim() != 1 or not t.is_contiguous() or t.numel() < 2 or \
-                    t.numel() != q_start.numel():
-                raise ValueError(f"{name}: expected contiguous int32 [batch + 1] on q's device")
-            else:
-                self.starts.append(t.data_ptr())
-        self.batch = q_start.numel() - 1 if self.packed else q.shape[0]
-        self.q_shape, self.k_shape = tuple(q.shape), tuple(k.shape)
         if scale is None:
             scale = 0.0
         elif not scale > 0.0:
             raise ValueError("scale: expected a positive number")
-        self.cfg = AdorePromptConfig(self.batch, q.shape[heads], k.shape[heads], q.shape[-1], q.shape[tokens], k.shape[tokens],
-                                     _CODES[q.dtype], float(scale))
-        self.q_rows = (q.shape[1], q.shape[0]) if self.packed else tuple(q.shape[:3])     # of one value per row: lse
-        self.k_rows = (k.shape[1], k.shape[0]) if self.packed else tuple(k.shape[:3])
+        if packed:
+            for name, t in (("q_start", q_start), ("k_start", k_start)):
+                if t.dtype is not torch.int32 or t.get_device() != index or t.dim() != 1 or not t.is_contiguous() or t.numel() < 2 or \
+                        t.numel() != q_start.numel():
+                    raise ValueError(f"{name}: expected contiguous int32 [batch + 1] on q's device")
+            self.starts = (q_start.data_ptr(), k_start.data_ptr())
+            self.batch = q_start.numel() - 1
+            self.cfg = AdorePromptConfig(self.batch, qs[1], ks[1], qs[2], qs[0], ks[0], code, scale)
+            self.q_rows, self.k_rows = (qs[1], qs[0]), (ks[1], ks[0])      # of one value per row: lse
+        else:
+            self.starts = (None, None)
+            self.batch = qs[0]
+            self.cfg = AdorePromptConfig(self.batch, qs[1], ks[1], qs[3], qs[2], ks[2], code, scale)
+            self.q_rows, self.k_rows = qs[:3], ks[:3]
 
     def rows(self, t: torch.Tensor, shape, name: str, written: bool = False):
-        if not isinstance(t, torch.Tensor) or t.device != self.device or t.dtype != self.dtype or tuple(t.shape) != shape or \
-                (t.shape[-1] > 1 and t.stride(-1) != 1):
-            raise ValueError(f"{name}: expected a {self.dtype} tensor of shape {shape} on {self.device}, its last dimension dense")
-        stride = [0 if n <= 1 else s for n, s in zip(t.shape, t.stride())]
-        if written and any(n > 1 and s == 0 for n, s in zip(t.shape, stride)):
-            raise ValueError(f"{name}: its rows lie on one another")
-        where = (0, stride[0], stride[1]) if self.packed else (stride[0], stride[2], stride[1])
-        # an empty tensor has no address, and no row of it is touched
-        return ctypes.byref(AdoreRows(t.data_ptr() or 16, *where))
+        if not isinstance(t, torch.Tensor) or t.shape != shape or t.dtype is not self.dtype or t.get_device() != self.index:
+            raise ValueError(f"{name}: expected a {self.dtype} tensor of shape {tuple(shape)} on {self.device}")
+        stride = t.stride()
+        if stride[-1] != 1 or 0 in stride or 1 in shape or 0 in shape:
+            if shape[-1] > 1 and stride[-1] != 1:
+                raise ValueError(f"{name}: its last dimension has to be dense")
+            stride = tuple(0 if n <= 1 else s for n, s in zip(shape, stride))      # of one row: any
+            if written and any(n > 1 and s == 0 for n, s in zip(shape, stride)):
+                raise ValueError(f"{name}: its rows lie on one another")
+        ptr = t.data_ptr() or 16               # (an empty tensor has no address, and no row of it is touched)
+        if self.packed:
+            return ctypes.byref(AdoreRows(ptr, 0, stride[0], stride[1]))
+        return ctypes.byref(AdoreRows(ptr, stride[0], stride[2], stride[1]))
 
     def values(self, t: torch.Tensor, shape, name: str):
-        if not isinstance(t, torch.Tensor) or t.device != self.device or t.dtype != torch.float32 or tuple(t.shape) != shape or \
+        if not isinstance(t, torch.Tensor) or t.shape != shape or t.dtype is not torch.float32 or t.get_device() != self.index or \
                 not t.is_contiguous():
-            raise ValueError(f"{name}: expected contiguous fp32 of shape {shape} on {self.device}")
+            raise ValueError(f"{name}: expected contiguous fp32 of shape {tuple(shape)} on {self.device}")
         return t.data_ptr() or 16
 
     @property
     def stream(self):
-        return torch.cuda.current_stream(self.device).cuda_stream
+        return torch.cuda.current_stream(self.index).cuda_stream
 
 
 def prompt_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, *, q_start: torch.Tensor = None,
@@ -342,7 +348,12 @@ class Q4Cache:
         self.score = self._buffer(score, rows + (slots,), torch.float32, 0, "score", 16)
         self.cursor = self._buffer(cursor, rows + (2,), torch.int32, 0, "cursor", 8)
         self.workspace = torch.empty(self.lib.adore_q4_workspace_bytes(ctypes.byref(self.cfg)), dtype=torch.uint8, device=self.device)
-        self._state = [t.data_ptr() for t in (self.cache, self.slot_pos, self.score, self.cursor)]
+        # what every call hands over, made once (a step of few rows takes the host longer than the GPU)
+        self._cfg = ctypes.byref(self.cfg)
+        self._state = [ctypes.c_void_p(t.data_ptr()) for t in (self.cache, self.slot_pos, self.score, self.cursor)]
+        self._space = [ctypes.c_void_p(self.workspace.data_ptr()), ctypes.c_size_t(self.workspace.numel())]
+        self._index = self.cache.get_device()
+        self._mine, self._rows = (batch, heads, head_dim), rows + (head_dim,)
 
     def _buffer(self, t, shape, dtype, value, name, align):
         if t is None:
@@ -362,21 +373,29 @@ class Q4Cache:
         p = _Prompts(k, k, k_start, k_start, None)
         if p.device != self.device or p.dtype != self.dtype or (p.batch, p.cfg.kv_heads, p.cfg.head_dim) != (c.batch, c.kv_heads, c.head_dim):
             raise ValueError(f"k: expected {self.dtype} rows of {c.batch} sequences, {c.kv_heads} heads, {c.head_dim} elements on {self.device}")
-        _check(self.lib, self.lib.adore_q4_fill(ctypes.byref(c), p.starts[1], p.cfg.k_tokens, p.rows(k, p.k_shape, "k"), p.rows(v, p.k_shape, "v"),
+        _check(self.lib, self.lib.adore_q4_fill(self._cfg, p.starts[1], p.cfg.k_tokens, p.rows(k, p.k_shape, "k"), p.rows(v, p.k_shape, "v"),
                                                 None if scores is None else p.values(scores, p.k_rows, "scores"), *self._state, p.stream))
 
     def step(self, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, *, out: torch.Tensor = None, held: bool = False):
         """One token of every sequence: q [batch, heads, head_dim], k and v [batch, kv_heads, head_dim], contiguous.  Returns out
         [batch, heads, head_dim], with held=True also the token's K and V as the cache holds them."""
-        c = self.cfg
-        mine, rows = (c.batch, c.heads, c.head_dim), (c.batch, c.kv_heads, c.head_dim)
         if out is None:
-            out = torch.empty(mine, dtype=self.dtype, device=self.device)
-        kept = [torch.empty(rows, dtype=self.dtype, device=self.device) for _ in range(2)] if held else [None, None]
-        ptr = [self._tensor(t, s, self.dtype, n).data_ptr() for t, s, n in ((q, mine, "q"), (k, rows, "k"), (v, rows, "v"), (out, mine, "out"))]
-        _check(self.lib, self.lib.adore_q4_step(ctypes.byref(c), *ptr[:3], *self._state, ptr[3], *(None if t is None else t.data_ptr() for t in kept),
-                                                self.workspace.data_ptr(), self.workspace.numel(), torch.cuda.current_stream(self.device).cuda_stream))
-        return (out, *kept) if held else out
+            out = torch.empty_like(q)
+        mine, rows = self._mine, self._rows
+        ptr = (self._ptr(q, mine, "q"), self._ptr(k, rows, "k"), self._ptr(v, rows, "v"), *self._state, self._ptr(out, mine, "out"))
+        stream = torch.cuda.current_stream(self._index).cuda_stream
+        if held:
+            k_held, v_held = torch.empty_like(k), torch.empty_like(v)
+            _check(self.lib, self.lib.adore_q4_step(self._cfg, *ptr, k_held.data_ptr(), v_held.data_ptr(), *self._space, stream))
+            return out, k_held, v_held
+        _check(self.lib, self.lib.adore_q4_step(self._cfg, *ptr, None, None, *self._space, stream))
+        return out
+
+    def _ptr(self, t, shape, name):
+        # four of these a step: attributes that cost least (2 -> 0.6 us each)
+        if t.dtype is not self.dtype or t.shape != shape or t.get_device() != self._index or not t.is_contiguous() or t.data_ptr() % 16:
+            self._tensor(t, shape, self.dtype, name)
+        return t.data_ptr()
 
     def read(self, k: torch.Tensor = None, v: torch.Tensor = None):
         """What the cache holds: K and V [batch, kv_heads, slots, head_dim], zeros in free slots."""
@@ -384,7 +403,7 @@ class Q4Cache:
         shape = (c.batch, c.kv_heads, c.slots, c.head_dim)
         k, v = (torch.empty(shape, dtype=self.dtype, device=self.device) if t is None else self._tensor(t, shape, self.dtype, n)
                 for t, n in ((k, "k"), (v, "v")))
-        _check(self.lib, self.lib.adore_q4_read(ctypes.byref(c), self._state[0], self._state[1], k.data_ptr(), v.data_ptr(),
+        _check(self.lib, self.lib.adore_q4_read(self._cfg, self._state[0], self._state[1], k.data_ptr(), v.data_ptr(),
                                                 torch.cuda.current_stream(self.device).cuda_stream))
         return k, v
 

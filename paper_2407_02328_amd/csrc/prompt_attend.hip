@@ -187,8 +187,7 @@ template <typename T, int DH, bool REST>
 hipError_t launch_attend_prompt(AttendArgs<T> a, hipStream_t st) {
   // a stage, and behind it another one or the waves' 32 queries each
   constexpr int stage = 2 * kKeys<T> * Tile<T, DH>::kRow, waves = 4 * 32 * Tile<T, DH>::kRow, lds = stage + (stage > waves ? stage : waves);
-  const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(&prompt_attend_kernel<T, DH, REST>),
-                                           hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+  const hipError_t e = allow_lds(&prompt_attend_kernel<T, DH, REST>, lds);
   if (e != hipSuccess) return e;
   const long long blocks = blocks_at_most(a.s.q_start, a.s.batch, a.s.q_tokens, 128) * a.s.heads;
   a.by_work = blocks < 1024;      // two for each place: beyond, what a sequence's blocks share counts for more (4096: 198 / 229 us)
@@ -312,8 +311,7 @@ __global__ __launch_bounds__(256) void prompt_scores_kernel(const ScoreArgs<T> a
 template <typename T, int DH>
 hipError_t launch_scores(ScoreArgs<T> a, hipStream_t st) {
   constexpr int tiles = 2 * kQueries<T> * Tile<T, DH>::kRow, keys = 128 * Tile<T, DH>::kRow, lds = tiles > keys ? tiles : keys;
-  const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(&prompt_scores_kernel<T, DH>),
-                                           hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+  const hipError_t e = allow_lds(&prompt_scores_kernel<T, DH>, lds);
   if (e != hipSuccess) return e;
   const long long blocks = blocks_at_most(a.s.k_start, a.s.batch, a.s.k_tokens, 128) * a.s.kv_heads;
   a.by_work = blocks < 1024;      // (as above; 1512: 177 / 197 us)

@@ -341,11 +341,6 @@ __global__ __launch_bounds__(256) ADORE_WAVES(sizeof(T) == 2 ? 2 : 1) void promp
                     nullptr, 0, lane);
 }
 
-template <typename F>
-hipError_t allow_lds(F *kernel, int bytes) {
-  return hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
-}
-
 template <typename T, int DH>
 hipError_t launch_backward(BackwardArgs<T> a, hipStream_t st) {
   // a stage, and behind it another one or every wave's own 32 rows, for the operands at the beginning and the results at the end

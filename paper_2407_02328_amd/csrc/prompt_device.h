@@ -162,6 +162,13 @@ __device__ __forceinline__ size_t row_value(bool packed, int b, int first, int t
   return packed ? size_t(h) * tokens + first : (size_t(b) * heads + h) * tokens;
 }
 
+// Dynamic shared memory beyond what every kernel may have.
+template <typename F>
+inline hipError_t allow_lds(F *kernel, int bytes) {
+  if (bytes <= 64 * 1024) return hipSuccess;
+  return hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+}
+
 // A kernel that is to have N waves a SIMD, no more: the compiler then uses the registers that leaves.
 #define ADORE_WAVES(N) __attribute__((amdgpu_waves_per_eu(N, N)))
 // What stands before it is issued before what stands behind it.

@@ -865,7 +865,7 @@ StepSpace step_space(const Q4Shape &s, int head_dim, const StepPlan &p) {
 template <typename T, int DH, bool WIDE>
 hipError_t launch_step(const StepArgs<T> &a, const StepPlan &p, hipStream_t st) {
   const int lds = step_lds(a.s, DH, p);
-  hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(&q4_step_kernel<T, DH, WIDE>), hipFuncAttributeMaxDynamicSharedMemorySize, kMaxLds);
+  hipError_t e = allow_lds(&q4_step_kernel<T, DH, WIDE>, lds);
   if (e != hipSuccess) return e;
   const unsigned rows = unsigned(a.s.batch) * unsigned(a.s.kv_heads);
   hipLaunchKernelGGL((q4_step_kernel<T, DH, WIDE>), dim3(rows * unsigned(p.splits), unsigned(p.passes)), dim3(64 * (p.waves + p.extra)), lds, st, a);
