@@ -83,6 +83,7 @@ __global__ __launch_bounds__(256) ADORE_WAVES(sizeof(T) == 4 ? 1 : DH == 128 ? 2
 #pragma unroll
   for (int db = 0; db < DB; ++db) o[db] = f32x16{0.f};
   float top = -INFINITY, sum = 0.f;             // of the lane's query: running maximum of the products, sum of its share of the keys
+  const float slack = 8.f / scale;
   for (int it = 0; it < tiles; ++it) {
     const int k0 = it * KT;
     arrived();
@@ -125,10 +126,11 @@ __global__ __launch_bounds__(256) ADORE_WAVES(sizeof(T) == 4 ? 1 : DH == 128 ? 2
       for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
         for (int r = 0; r < 16; ++r) m = fmaxf(m, s[kb][r]);
+      // The maximum moves only where some query's has grown by 8 in the exponent: until then its weights are up to 2^8 and not 1, which
+      // neither fp32 sums nor bf16 operands mind, and the outputs need not be scaled at every tile.
       m = fmaxf(top, max_lane_xor<32>(m));
-      const float base = m == -INFINITY ? 0.f : -m * scale;           // a query that has seen nothing yet
-      if (__builtin_amdgcn_ballot_w64(m > top)) {
-        const float fade = __builtin_amdgcn_exp2f(fmaf(top, scale, base));
+      if (__builtin_amdgcn_ballot_w64(m > top + slack)) {
+        const float fade = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((top - m) * scale);
         sum *= fade;
 #pragma unroll
         for (int db = 0; db < DB; ++db)
@@ -136,6 +138,7 @@ __global__ __launch_bounds__(256) ADORE_WAVES(sizeof(T) == 4 ? 1 : DH == 128 ? 2
           for (int r = 0; r < 16; ++r) o[db][r] *= fade;
         top = m;
       }
+      const float base = top == -INFINITY ? 0.f : -top * scale;       // (a query that has seen nothing yet)
       float part[4] = {0.f};                    // a tile's weights first, so that few additions round the running sum
       auto weights = [&](int kb, int r0, int n) {
 #pragma unroll

@@ -220,17 +220,17 @@ struct Operand<float> {
 };
 
 // ---- tiles in LDS -----------------------------------------------------------------------------------------------
-// R rows of DH elements, in 16-byte chunks that are permuted within their row (an exclusive or with a number that goes by the row) so
-// that neither the rows of an operand at one chunk nor 4 rows x 2 neighbouring chunks (transposed) meet in a bank.
+// R rows of DH elements, in 16-byte chunks that are permuted within their row (an exclusive or with a number that goes by the row) so that
+// what one cycle of LDS serves (256 bytes) does not meet in a bank: an operand's 16 rows at one chunk, and transposed 4 rows x 64 bytes
+// (two bits of the row choose among four times 64 bytes, the next two within them; at 64 elements two rows share 256 bytes).
 template <typename T, int DH>
 struct Tile {
   static constexpr int kRow = DH * int(sizeof(T));
   static constexpr int kChunks = kRow / 16;
-  static constexpr int kPeriod = sizeof(T) == 2 && DH == 128 ? 16 : 8;
+  static constexpr int kPeriod = sizeof(T) == 2 ? 16 : 8;
   __device__ static __forceinline__ int turn(int r) {
     if constexpr (sizeof(T) == 4) return r & 7;
-    const int x = (r & 3) << 1 | ((r >> 2) & 1);
-    return DH == 128 ? x | (r & 8) : x;
+    return DH == 128 ? (r & 3) << 2 | ((r >> 2) & 3) : (r & 2) << 1 | ((r >> 2) & 3);
   }
   __device__ static __forceinline__ int chunk_at(int r, int ch) { return r * kRow + ((ch ^ turn(r)) << 4); }
 };
@@ -247,13 +247,13 @@ __device__ __forceinline__ V lds_read(uint32_t at) {
 //   by_row(add, r0, t)          row r0 + c, elements 16 t + 8 h .. + 7
 //   transposed(add, r0, t, db)  column 32 db + c, rows r0 + 16 t + 8 (e / 4) + 4 h + e % 4, e = 0 .. 7
 // of the tile `add` bytes behind the place the reader is at; r0: a multiple of 32.
-// FEW: one register for the rows instead of one per step, at an exclusive or a read (tiles then start at multiples of a row).
+// FEW: a third of the registers, at an exclusive or a read (tiles then start at multiples of 256 bytes).
 template <typename T, int DH, bool FEW = false>
 struct Reader {
   typedef Tile<T, DH> L;
   typedef typename Operand<T>::type Frag;
   static constexpr bool F32 = sizeof(T) == 4;
-  static constexpr int NR = F32 ? 4 : FEW ? 1 : DH / 16, NC = F32 ? 4 : DH / 32;
+  static constexpr int NR = F32 ? 4 : FEW ? 1 : DH / 16, NC = F32 ? 4 : DH / 32 * (FEW ? 1 : 2);
   uint32_t row[NR], col[NC];
   __device__ __forceinline__ void move(uint32_t by) {
 #pragma unroll
@@ -275,7 +275,7 @@ struct Reader {
       // 16 lanes read 4 rows x 16 columns, and each gets 4 rows of its column
       const int grp = lane >> 4, r = 4 * (grp >> 1) + ((lane & 15) >> 2), x = (grp & 1) * 16 + (lane & 3) * 4;
 #pragma unroll
-      for (int i = 0; i < NC; ++i) col[i] = uint32_t(L::chunk_at(r, (32 * i + x) >> 3) + (x & 4) * 2);
+      for (int i = 0; i < NC; ++i) col[i] = uint32_t(L::chunk_at(r + i / (DH / 32) * 8, (32 * (i % (DH / 32)) + x) >> 3) + (x & 4) * 2);
     }
     move(place);
   }
@@ -301,8 +301,9 @@ struct Reader {
         bf16x8 v;
       } u;
 #pragma unroll
-      for (int e4 = 0; e4 < 2; ++e4) {       // rows 8 further on: the other half of the permutation at 128 elements
-        const uint32_t at = col[DH == 128 ? db ^ (2 * e4) : db] + (ahead + uint32_t((r0 + 16 * t + 8 * e4) * L::kRow));
+      for (int e4 = 0; e4 < 2; ++e4) {       // (rows 8 further on: another bit of the permutation)
+        const uint32_t at = FEW ? (col[db] ^ uint32_t(e4 << 5)) + (ahead + uint32_t((r0 + 16 * t + 8 * e4) * L::kRow))
+                                : col[FEW ? 0 : e4 * (DH / 32) + db] + (ahead + uint32_t((r0 + 16 * t) * L::kRow));
         u.q[e4] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)(LdsPtr)uintptr_t(at));
       }
       return u.v;
