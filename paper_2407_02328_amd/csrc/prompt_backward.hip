@@ -3,7 +3,7 @@
 //   p_ij = exp(w_ij - lse_i),  g_ij = p_ij (do_i . v_j - delta_i),  delta_i = do_i . out_i
 //   dq_i = scale sum_j g_ij k_j;   dk_j = scale sum_i g_ij q_i,   dv_j = sum_i p_ij do_i   (i over the queries of all heads of j's group)
 //
-// Three launches without atomics, so that a gradient's bits do not hang on the order of workgroups: delta; dq, whose workgroups own
+// Two launches without atomics, so that a gradient's bits do not hang on the order of workgroups: delta and dq, whose workgroups own
 // queries and go over the keys; dk and dv, whose workgroups own keys and go over the queries of the group.  The weights are made anew
 // in both (seven products instead of the five that one pass would need, which would have to add dq up in memory).
 // delta wants out as it was before P and it were rounded: from the rounded one a short row's gradients are up to 2.2 times as far off as
@@ -26,27 +26,39 @@ struct BackwardArgs {
   bool by_work;
 };
 
-// ---- delta: DH / EPL lanes a row, 16 bytes each ----
-template <typename T, int DH>
-__global__ __launch_bounds__(256) void prompt_delta_kernel(const BackwardArgs<T> a, int rows) {
-  constexpr int EPL = Vec16<T>::EPL, LPR = DH / EPL;
-  const int64_t i = (int64_t(blockIdx.x) * 256 + threadIdx.x) / LPR;      // token x head, heads fastest
-  if (i >= int64_t(rows) * a.s.heads) return;                             // (whole rows leave together)
-  const int head = int(i % a.s.heads), row = int(i / a.s.heads), sub = threadIdx.x % LPR;
-  const bool packed = a.s.q_start != nullptr;
-  const int b = packed ? 0 : row / a.s.q_tokens, t = packed ? row : row - b * a.s.q_tokens;
-  float x[EPL], y[EPL], z[EPL], sum = 0.f;
-  Vec16<T>::load(a.d_out.p + b * a.d_out.seq + t * a.d_out.token + head * a.d_out.head + sub * EPL, x);
-  Vec16<T>::load(a.out.p + b * a.out.seq + t * a.out.token + head * a.out.head + sub * EPL, y);
+// The products of 32 rows of dO with those of out (and what its rounding left), as dO goes by on its way to LDS (carry_rows): delta of row
+// DH / EPL lanes share comes out in all of them, for rows lane / (DH / EPL) + i * (64 / (DH / EPL)).
+template <typename T, int DH, int N>
+__device__ __forceinline__ void carry_dots(float (&dot)[N], const char *d_out, int64_t d_stride, const char *out, int64_t o_stride, const char *rest,
+                                           int64_t r_stride, int rows, unsigned char *own, int lane) {
+  typedef Tile<T, DH> L;
+  constexpr int EPL = Vec16<T>::EPL;
+  static_assert(N == 32 * L::kChunks / 64, "rows of a lane");
+  const int row = lane / L::kChunks, ch = lane % L::kChunks;
+  typename Vec16<T>::Raw d[N], o[N], z[N];
 #pragma unroll
-  for (int e = 0; e < EPL; ++e) sum = fmaf(x[e], y[e], sum);
-  if (a.rest.p) {
-    Vec16<T>::load(a.rest.p + b * a.rest.seq + t * a.rest.token + head * a.rest.head + sub * EPL, z);
-#pragma unroll
-    for (int e = 0; e < EPL; ++e) sum = fmaf(x[e], z[e], sum);
+  for (int i = 0; i < N; ++i) {
+    const int64_t there = min(row + i * (64 / L::kChunks), rows - 1);
+    d[i] = Vec16<T>::load_raw(reinterpret_cast<const T *>(d_out + there * d_stride + ch * 16));
+    o[i] = Vec16<T>::load_raw(reinterpret_cast<const T *>(out + there * o_stride + ch * 16));
+    if (rest) z[i] = Vec16<T>::load_raw(reinterpret_cast<const T *>(rest + there * r_stride + ch * 16));
   }
-  sum = group_sum<LPR>(sum);
-  if (sub == 0) a.delta[row_value(packed, b, 0, a.s.q_tokens, a.s.heads, head) + t] = sum;
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    const int mine = row + i * (64 / L::kChunks);
+    float x[EPL], y[EPL], sum = 0.f;
+    Vec16<T>::values(d[i], x);
+    Vec16<T>::values(o[i], y);
+#pragma unroll
+    for (int e = 0; e < EPL; ++e) sum = fmaf(x[e], y[e], sum);
+    if (rest) {
+      Vec16<T>::values(z[i], y);
+#pragma unroll
+      for (int e = 0; e < EPL; ++e) sum = fmaf(x[e], y[e], sum);
+    }
+    dot[i] = group_sum<L::kChunks>(sum);
+    Vec16<T>::store_raw(reinterpret_cast<T *>(own + L::chunk_at(mine, ch)), mine < rows ? d[i] : typename Vec16<T>::Raw{});
+  }
 }
 
 // ---- dq: 128 queries a workgroup, 32 a wave ----
@@ -88,13 +100,37 @@ __global__ __launch_bounds__(256) ADORE_WAVES(sizeof(T) == 4 ? 1 : DH == 128 ? 2
   unsigned char *own = smem + 2 * kTile + wave * (32 * L::kRow);    // the wave's share of the second stage
   Frag qf[ST], df[ST];
   operand_rows<T, DH, false>(qf, read, reinterpret_cast<const char *>(a.q.p + sq.b * a.q.seq + row * a.q.token + head * a.q.head), a.q.token * es, rows, own, 2 * kTile + wave * (32 * L::kRow), lane);
-  operand_rows<T, DH, false>(df, read, reinterpret_cast<const char *>(a.d_out.p + sq.b * a.d_out.seq + row * a.d_out.token + head * a.d_out.head),
-                      a.d_out.token * es, rows, own, 2 * kTile + wave * (32 * L::kRow), lane);
-  float lse = INFINITY, delta = 0.f;            // of the lane's query; weights of a query that is not there are 0
-  if (c < rows) {
-    const size_t at = row_value(a.s.q_start != nullptr, sq.b, sq.q_first, a.s.q_tokens, a.s.heads, head) + q0 + c;
-    lse = subtrahend(a.lse[at]);
-    delta = a.delta[at];
+  // of the lane's query; weights of a query that is not there are 0
+  float lse = INFINITY, delta = 0.f;
+  {
+    constexpr int N = 32 * L::kChunks / 64;
+    const size_t at = row_value(a.s.q_start != nullptr, sq.b, sq.q_first, a.s.q_tokens, a.s.heads, head) + q0;
+    float dot[N];
+    wave_lds_fence();
+    if (rows > 0) {
+      if (c < rows) lse = subtrahend(a.lse[at + c]);
+      carry_dots<T, DH>(dot, reinterpret_cast<const char *>(a.d_out.p + sq.b * a.d_out.seq + row * a.d_out.token + head * a.d_out.head),
+                        a.d_out.token * es, reinterpret_cast<const char *>(a.out.p + sq.b * a.out.seq + row * a.out.token + head * a.out.head),
+                        a.out.token * es,
+                        a.rest.p ? reinterpret_cast<const char *>(a.rest.p + sq.b * a.rest.seq + row * a.rest.token + head * a.rest.head) : nullptr,
+                        a.rest.token * es, rows, own, lane);
+    }
+    wave_lds_fence();
+#pragma unroll
+    for (int t = 0; t < ST; ++t) df[t] = read.by_row(2 * kTile + wave * (32 * L::kRow), 0, t);
+    wave_lds_fence();
+    if (rows > 0) {
+      float *const s_delta = reinterpret_cast<float *>(own);
+      if (lane % L::kChunks == 0) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) s_delta[lane / L::kChunks + i * (64 / L::kChunks)] = dot[i];
+      }
+      wave_lds_fence();
+      if (c < rows) {
+        delta = s_delta[c];
+        if (h == 0) a.delta[at + c] = delta;    // for dk and dv
+      }
+    }
   }
   f32x16 dq[DB];
 #pragma unroll
@@ -350,10 +386,6 @@ hipError_t launch_backward(BackwardArgs<T> a, hipStream_t st) {
   if (e == hipSuccess) e = allow_lds(&prompt_dkv_kernel<T, DH>, dkv_lds);
   if (e != hipSuccess) return e;
   if (a.s.q_tokens > 0) {
-    const int rows = a.s.q_start ? a.s.q_tokens : a.s.batch * a.s.q_tokens, per = 256 / (DH / Vec16<T>::EPL);
-    const long long blocks = ((long long)rows * a.s.heads + per - 1) / per;
-    hipLaunchKernelGGL((prompt_delta_kernel<T, DH>), dim3(unsigned(blocks)), dim3(256), 0, st, a, rows);
-    if ((e = hipGetLastError()) != hipSuccess) return e;
     const long long query_blocks = blocks_at_most(a.s.q_start, a.s.batch, a.s.q_tokens, 128) * a.s.heads;
     a.by_work = query_blocks < 1024;
     hipLaunchKernelGGL((prompt_dq_kernel<T, DH>), dim3(unsigned(query_blocks)), dim3(256), dq_lds, st, a);
