@@ -347,7 +347,8 @@ int adore_topk_attention_static(const void *q, const void *k, const void *v, voi
  * lse: fp32 [heads][q_tokens] packed, [batch][heads][q_tokens] without starts; scores alike with kv_heads and k_tokens,
  * which for a dense batch is the layout that adore_init_cache takes as score_override in H2O mode.
  * Products are accumulated in fp32, softmax statistics are fp32, weights and their gradients are rounded to the storage
- * type where they enter a product; outputs are rounded once.  No atomics: equal inputs give equal bits.
+ * type where they enter a product; outputs are rounded once.  A row reaches what sees it and nothing else, infinities and NaN too
+ * (later keys and values no earlier query, earlier queries no later key's gradients or scores).  No atomics: equal inputs give equal bits.
  * Calls only enqueue work on hip_stream (a hipStream_t, NULL = the default stream).
  * Errors of all: E_INVALID (null, sizes, kv_heads that do not divide heads, a scale that is negative or not finite, one of
  * the two starts alone, rows not on 16-byte boundaries, a negative stride or a token stride beyond 2^22 elements),

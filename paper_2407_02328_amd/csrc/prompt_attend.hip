@@ -84,10 +84,16 @@ __global__ __launch_bounds__(256) ADORE_WAVES(sizeof(T) == 4 ? 1 : DH == 128 ? 2
   for (int db = 0; db < DB; ++db) o[db] = f32x16{0.f};
   float top = -INFINITY, sum = 0.f;             // of the lane's query: running maximum of the products, sum of its share of the keys
   const float slack = 8.f / scale;
+  const int hidden = max(block * BQ + off + 1, 0) / KT;               // the first tile that not all of the workgroup's queries see all of
+  bool found = false;                           // ... where a value is not finite
   for (int it = 0; it < tiles; ++it) {
     const int k0 = it * KT;
     arrived();
     __syncthreads();
+    if (it >= hidden) {
+      found |= make_finite<T, DH, KT, NT>(smem + (it & 1) * 2 * kTile + kTile);
+      __syncthreads();
+    }
     if (it + 1 < tiles) {
       const uint32_t next = share + uint32_t(~it & 1) * uint32_t(2 * kTile);
       kp += ks;
@@ -171,7 +177,11 @@ __global__ __launch_bounds__(256) ADORE_WAVES(sizeof(T) == 4 ? 1 : DH == 128 ? 2
     read.move(it & 1 ? uint32_t(-2 * kTile) : uint32_t(2 * kTile));
   }
   __syncthreads();
+  found = any_of_four(found, reinterpret_cast<int *>(smem + 4 * 32 * L::kRow));
   if (rows <= 0) return;
+  if (found)
+    add_not_finite<T, DH>(o, reinterpret_cast<const char *>(a.v.p + sq.b * a.v.seq + sq.k_first * a.v.token + hk * a.v.head),
+                          a.v.token * int64_t(sizeof(T)), hidden * KT, mine + 1, seen, lane);
   sum = add_lane_xor<32>(sum);
   const bool some = sum > 0.f || sum != sum;    // (a query without keys: zeros, and -inf)
   if (a.lse && lane < rows) {
@@ -271,10 +281,28 @@ __global__ __launch_bounds__(256) void prompt_scores_kernel(const ScoreArgs<T> a
     __syncthreads();
     if (it + 1 < tiles) load(~it & 1);
     Frag x[ST];
+    float part[4] = {0.f};
+    // A hidden query whose log-sum-exp is NaN: its weights are none at all, where the sums below would make them NaN.
+    if (q0 + off < k0 + 31 && __builtin_amdgcn_ballot_w64(s_lse[it & 1][lane % QT] != s_lse[it & 1][lane % QT])) {
+#pragma unroll 1
+      for (int qb = 0; qb < QB; ++qb) {
+        f32x16 s = {0.f};
+#pragma unroll
+        for (int t = 0; t < ST; ++t) s = Operand<T>::mma(read.by_row(uint32_t(qb * 32 * L::kRow), 0, t), kf[t], s);
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          const int i = qb * 32 + 8 * (r >> 2) + 4 * h + (r & 3);
+          if (k0 + c <= q0 + i + off) part[r & 3] += __builtin_amdgcn_exp2f(fmaf(s[r], scale, -s_lse[it & 1][i]));
+        }
+      }
+      sum += (part[0] + part[1]) + (part[2] + part[3]);
+      if (it + 1 < tiles && tid < QT) s_lse[~it & 1][tid] = row_lse;
+      read.move(it & 1 ? uint32_t(-kTile) : uint32_t(kTile));
+      continue;
+    }
 #pragma unroll
     for (int t = 0; t < ST; ++t) x[t] = read.by_row(0, 0, t);
     f32x16 s[QB];
-    float part[4] = {0.f};
     auto weights = [&](int qb, int r4) {
       const f32x4 lse = *reinterpret_cast<const f32x4 *>(&s_lse[it & 1][qb * 32 + 8 * r4 + 4 * h]);
 #pragma unroll

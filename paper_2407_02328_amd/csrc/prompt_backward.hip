@@ -135,10 +135,16 @@ __global__ __launch_bounds__(256) ADORE_WAVES(sizeof(T) == 4 ? 1 : DH == 128 ? 2
   f32x16 dq[DB];
 #pragma unroll
   for (int db = 0; db < DB; ++db) dq[db] = f32x16{0.f};
+  const int hidden = max(block * BQ + off + 1, 0) / KT;    // the first tile that not all of the workgroup's queries see all of
+  bool found = false;                                      // ... where an element of K is not finite
   for (int it = 0; it < tiles; ++it) {
     const int k0 = it * KT;
     arrived();
     __syncthreads();
+    if (it >= hidden) {
+      found |= make_finite<T, DH, KT, NT>(smem + (it & 1) * 2 * kTile);
+      __syncthreads();
+    }
     if (it + 1 < tiles) {
       const uint32_t next = share + uint32_t(~it & 1) * uint32_t(2 * kTile);
       kp += KT * a.k.token * es;
@@ -178,6 +184,11 @@ __global__ __launch_bounds__(256) ADORE_WAVES(sizeof(T) == 4 ? 1 : DH == 128 ? 2
         for (int r = t * (16 / ST); r < (t + 1) * (16 / ST); ++r) s[r] = __builtin_amdgcn_exp2f(fmaf(s[r], scale, -lse));
       }
       pin();
+      if (k0 + kb * 32 + 31 > q0 + off) {         // (a hidden row of V may be anything)
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+          if (k0 + kb * 32 + 8 * (r >> 2) + 4 * h + (r & 3) > seen) g[r] = delta;
+      }
 #pragma unroll
       for (int r = 0; r < 8; ++r) g[r] = s[r] * (g[r] - delta);
       Frag gf = Operand<T>::of(g, 0);
@@ -204,7 +215,11 @@ __global__ __launch_bounds__(256) ADORE_WAVES(sizeof(T) == 4 ? 1 : DH == 128 ? 2
     read.move(it & 1 ? uint32_t(-2 * kTile) : uint32_t(2 * kTile));
   }
   __syncthreads();
+  found = any_of_four(found, reinterpret_cast<int *>(smem));
   if (rows <= 0) return;
+  if (found)
+    add_not_finite<T, DH>(dq, reinterpret_cast<const char *>(a.k.p + sq.b * a.k.seq + sq.k_first * a.k.token + hk * a.k.head), a.k.token * es, hidden * KT,
+                          mine + 1, seen, lane);
   store_rows<T, DH>(dq, a.s.scale, own, reinterpret_cast<char *>(a.dq.p + sq.b * a.dq.seq + row * a.dq.token + head * a.dq.head),
                     a.dq.token * es, rows, nullptr, 0, lane);
 }
@@ -237,7 +252,16 @@ __global__ __launch_bounds__(256) ADORE_WAVES(sizeof(T) == 2 ? 2 : 1) void promp
   const int k0 = block * BK + wave * 32, off = sq.nk - sq.nq;
   const int rows = min(32, sq.nk - k0);
   const int64_t row = int64_t(sq.k_first) + k0, es = int64_t(sizeof(T));
-  const int first = max(block * BK - off, 0) / QT * QT;
+  // Queries that some of the block's keys are hidden from, if one of them is not finite, or has no keys (log-sum-exp or delta tells), are
+  // added one by one when the tiles are done.
+  const int diagonal = max(block * BK - off, 0) / QT * QT, behind = min((block * BK + BK - 1 - off + QT - 1) / QT * QT, sq.nq);
+  bool odd = false;
+  for (int j = 0; j < a.s.group; ++j) {
+    const size_t row0 = row_value(a.s.q_start != nullptr, sq.b, sq.q_first, a.s.q_tokens, a.s.heads, hk * a.s.group + j);
+    for (int i = diagonal + tid; i < behind; i += NT) odd |= !(subtrahend(a.lse[row0 + i]) < INFINITY && fabsf(a.delta[row0 + i]) < INFINITY);
+  }
+  odd = any_of_four(__builtin_amdgcn_ballot_w64(odd) != 0, reinterpret_cast<int *>(s_delta + 2 * QT));
+  const int first = odd ? behind : diagonal;
   const int per = first < sq.nq ? (sq.nq - first + QT - 1) / QT : 0, tiles = per * a.s.group;
   const float scale = a.s.scale_log2;
   const bool packed = a.s.q_start != nullptr;
@@ -371,6 +395,43 @@ __global__ __launch_bounds__(256) ADORE_WAVES(sizeof(T) == 2 ? 2 : 1) void promp
   }
   __syncthreads();
   if (rows <= 0) return;
+  if (odd) {
+    // a lane: its key, half of the elements
+    const int64_t key = row + min(c, rows - 1);
+    const T *kr = a.k.p + sq.b * a.k.seq + key * a.k.token + hk * a.k.head + 4 * h, *vr = a.v.p + sq.b * a.v.seq + key * a.v.token + hk * a.v.head + 4 * h;
+    for (int j = 0; j < a.s.group; ++j) {
+      const int head = hk * a.s.group + j;
+      const size_t row0 = row_value(packed, sq.b, sq.q_first, a.s.q_tokens, a.s.heads, head);
+      for (int i = diagonal; i < behind; ++i) {
+        const int64_t query = int64_t(sq.q_first) + i;
+        const T *qr = a.q.p + sq.b * a.q.seq + query * a.q.token + head * a.q.head + 4 * h;
+        const T *dr = a.d_out.p + sq.b * a.d_out.seq + query * a.d_out.token + head * a.d_out.head + 4 * h;
+        float w = 0.f, x = 0.f;
+#pragma unroll 1
+        for (int e = 0; e < DH; e += 8)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            w = fmaf(to_float(qr[e + r]), to_float(kr[e + r]), w);
+            x = fmaf(to_float(dr[e + r]), to_float(vr[e + r]), x);
+          }
+        w = add_lane_xor<32>(w);
+        x = add_lane_xor<32>(x);
+        w = __builtin_amdgcn_exp2f(fmaf(w, scale, -subtrahend(a.lse[row0 + i])));
+        x = w * (x - a.delta[row0 + i]);
+        if (k0 + c <= i + off) {
+#pragma unroll
+          for (int db = 0; db < DB; ++db)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+              const int e = 32 * db + 8 * (r >> 2) + (r & 3);
+              dv[db][r] = fmaf(w, to_float(dr[e]), dv[db][r]);
+              dk[db][r] = fmaf(x, to_float(qr[e]), dk[db][r]);
+              if (r % 4 == 3) pin();
+            }
+        }
+      }
+    }
+  }
   store_rows<T, DH>(dk, a.s.scale, own, reinterpret_cast<char *>(a.dk.p + sq.b * a.dk.seq + row * a.dk.token + hk * a.dk.head), a.dk.token * es, rows,
                     nullptr, 0, lane);
   store_rows<T, DH>(dv, 1.f, own, reinterpret_cast<char *>(a.dv.p + sq.b * a.dv.seq + row * a.dv.token + hk * a.dv.head), a.dv.token * es, rows,
@@ -381,7 +442,7 @@ template <typename T, int DH>
 hipError_t launch_backward(BackwardArgs<T> a, hipStream_t st) {
   // a stage, and behind it another one or every wave's own 32 rows, for the operands at the beginning and the results at the end
   constexpr int row = Tile<T, DH>::kRow, waves = 4 * 32 * row, dq_stage = 2 * kDqKeys<T> * row;
-  constexpr int dq_lds = dq_stage + (dq_stage > waves ? dq_stage : waves), dkv_lds = 4 * kDkvQueries<T> * row + waves + 4 * kDkvQueries<T> * 4;
+  constexpr int dq_lds = dq_stage + (dq_stage > waves ? dq_stage : waves), dkv_lds = 4 * kDkvQueries<T> * row + waves + 4 * kDkvQueries<T> * 4 + 16;
   hipError_t e = allow_lds(&prompt_dq_kernel<T, DH>, dq_lds);
   if (e == hipSuccess) e = allow_lds(&prompt_dkv_kernel<T, DH>, dkv_lds);
   if (e != hipSuccess) return e;

@@ -24,6 +24,7 @@ typedef float f32x8 __attribute__((ext_vector_type(8)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
 
 // Rows of a tensor: token t of sequence b, head h starts at p + b seq + (first + t) token + h head (elements); first = start[b], or
 // 0 without starts.
@@ -310,6 +311,74 @@ struct Reader {
     }
   }
 };
+
+// ---- hidden rows that are not finite ----
+// A weight of 0 hides a row from a matrix product only where the row is finite.  Rows that some of a workgroup's columns see and others do
+// not are all in its few tiles on the diagonal: there infinities and NaN become 0, and when all tiles are done every column takes
+// those that it does see (add_not_finite), from memory.
+
+// The workgroup's tile of R rows; whether this wave found any.  Barriers before and behind are the caller's.
+template <typename T, int DH, int R, int NT>
+__device__ __forceinline__ bool make_finite(unsigned char *tile) {
+  constexpr int N = R * Tile<T, DH>::kChunks / NT;
+  constexpr uint32_t kSize = sizeof(T) == 2 ? 0x7fff7fffu : 0x7fffffffu;
+  static_assert(N * NT == R * Tile<T, DH>::kChunks, "as many chunks for every thread");
+  int tid = threadIdx.x;
+  asm("" : "+v"(tid));   // (worked out here, not kept in registers)
+  u32x4 *const chunk = reinterpret_cast<u32x4 *>(tile) + tid;
+  bool found = false;
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    u32x4 w = chunk[i * NT];
+    bool bad;
+    if constexpr (sizeof(T) == 2) {
+      u16x2 most = {0, 0};
+#pragma unroll
+      for (int j = 0; j < 4; ++j) most = __builtin_elementwise_max(most, __builtin_bit_cast(u16x2, w[j] & kSize));
+      bad = most[0] >= 0x7f80 || most[1] >= 0x7f80;
+    } else {
+      uint32_t most = 0;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) most = max(most, w[j] & kSize);
+      bad = most >= 0x7f800000u;
+    }
+    if (bad) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        if ((w[j] & 0x7f800000u) == 0x7f800000u) w[j] &= sizeof(T) == 2 ? 0xffffu : 0u;
+        if (sizeof(T) == 2 && (w[j] & 0x7f80u) == 0x7f80u) w[j] &= 0xffff0000u;
+      }
+      chunk[i * NT] = w;
+      found = true;
+    }
+  }
+  return __builtin_amdgcn_ballot_w64(found) != 0;
+}
+
+// Whether it holds in any of the workgroup's four waves; s: four words that nothing else uses from here on.
+__device__ __forceinline__ bool any_of_four(bool mine, int *s) {
+  if ((threadIdx.x & 63) == 0) s[threadIdx.x >> 6] = mine;
+  __syncthreads();
+  return (s[0] | s[1] | s[2] | s[3]) != 0;
+}
+
+// acc (element 32 db + .., column c) += what is not finite of rows from .. to - 1 at `rows`, up to the last that the lane's column sees.
+template <typename T, int DH>
+__device__ __forceinline__ void add_not_finite(f32x16 (&acc)[DH / 32], const char *rows, int64_t stride, int from, int to, int seen, int lane) {
+#pragma unroll 1
+  for (int i = from; i < to; ++i) {
+    if (i > seen) continue;
+    const T *row = reinterpret_cast<const T *>(rows + i * stride) + 4 * (lane >> 5);
+#pragma unroll
+    for (int db = 0; db < DH / 32; ++db)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        const float x = to_float(row[32 * db + 8 * (r >> 2) + (r & 3)]);
+        acc[db][r] += fabsf(x) < INFINITY ? 0.f : x;
+        if (r % 4 == 3) pin();
+      }
+  }
+}
 
 // 32 rows' way from memory to the wave's own LDS, 16 bytes at a time; rows from `rows` on are zeros.
 template <typename T, int DH>
