@@ -36,9 +36,10 @@ constexpr int kKeys = sizeof(T) == 2 ? 64 : 32;
 
 // REST: P goes in as two bf16 terms (within 2^-16) and what rounding out leaves is handed out, for a backward pass whose delta is as good
 // as its other terms.
-template <typename T, int DH, bool REST>
-__global__ __launch_bounds__(256) ADORE_WAVES(sizeof(T) == 4 ? 1 : DH == 128 ? 2 : REST ? 3 : 4) void prompt_attend_kernel(const AttendArgs<T> a) {
-  constexpr int NT = 256, BQ = 128, KT = kKeys<T>, KB = KT / 32, DB = DH / 32, ST = DH / 16;
+template <typename T, int DH, bool REST, int SW>
+__global__ __launch_bounds__(256) ADORE_WAVES(sizeof(T) == 4 || SW > 1 ? 1 : DH == 128 ? 2 : REST ? 3 : 4)
+void prompt_attend_kernel(const AttendArgs<T> a) {
+  constexpr int NT = 256, BQ = Shared<SW>::kRows, KT = SW > 1 ? 32 * SW : kKeys<T>, KB = SW > 1 ? 1 : KT / 32, DB = DH / 32, ST = DH / 16;
   typedef Tile<T, DH> L;
   typedef typename Operand<T>::type Frag;
   constexpr int kTile = KT * L::kRow;
@@ -56,7 +57,8 @@ __global__ __launch_bounds__(256) ADORE_WAVES(sizeof(T) == 4 ? 1 : DH == 128 ? 2
     if (a.lse && tid < n) a.lse[size_t(head) * a.s.q_tokens + first + tid] = -INFINITY;
     return;
   }
-  const int q0 = block * BQ + wave * 32, off = sq.nk - sq.nq;
+  const Shared<SW> mate(wave);
+  const int q0 = block * BQ + mate.rows * 32, off = sq.nk - sq.nq;
   const int rows = min(32, sq.nq - q0);        // may be <= 0
   const char *kp = reinterpret_cast<const char *>(a.k.p + sq.b * a.k.seq + sq.k_first * a.k.token + hk * a.k.head);
   const char *vp = reinterpret_cast<const char *>(a.v.p + sq.b * a.v.seq + sq.k_first * a.v.token + hk * a.v.head);
@@ -73,11 +75,12 @@ __global__ __launch_bounds__(256) ADORE_WAVES(sizeof(T) == 4 ? 1 : DH == 128 ? 2
     lk(kp, sq.nk, share);
     lv(vp, sq.nk, share + kTile);
   }
-  Reader<T, DH> read(base0, lane);
+  Reader<T, DH> read(base0 + uint32_t(mate.part * 32 * L::kRow), lane);
   // the query operand, through the wave's share of the second stage
   Frag qf[ST];
   operand_rows<T, DH, false>(qf, read, reinterpret_cast<const char *>(a.q.p + sq.b * a.q.seq + (int64_t(sq.q_first) + q0) * a.q.token + head * a.q.head),
-                      a.q.token * int64_t(sizeof(T)), rows, smem + 2 * kTile + wave * (32 * L::kRow), 2 * kTile + wave * (32 * L::kRow), lane);
+                      a.q.token * int64_t(sizeof(T)), rows, smem + 2 * kTile + wave * (32 * L::kRow),
+                      uint32_t(2 * kTile + (wave - mate.part) * (32 * L::kRow)), lane);
 
   f32x16 o[DB];
 #pragma unroll
@@ -87,7 +90,7 @@ __global__ __launch_bounds__(256) ADORE_WAVES(sizeof(T) == 4 ? 1 : DH == 128 ? 2
   const int hidden = max(block * BQ + off + 1, 0) / KT;               // the first tile that not all of the workgroup's queries see all of
   bool found = false;                           // ... where a value is not finite
   for (int it = 0; it < tiles; ++it) {
-    const int k0 = it * KT;
+    const int k0 = it * KT + mate.part * 32;    // the wave's first key of the tile
     arrived();
     __syncthreads();
     if (it >= hidden) {
@@ -98,8 +101,8 @@ __global__ __launch_bounds__(256) ADORE_WAVES(sizeof(T) == 4 ? 1 : DH == 128 ? 2
       const uint32_t next = share + uint32_t(~it & 1) * uint32_t(2 * kTile);
       kp += ks;
       vp += vs;
-      lk(kp, sq.nk - k0 - KT, next);
-      lv(vp, sq.nk - k0 - KT, next + kTile);
+      lk(kp, sq.nk - (it + 1) * KT, next);
+      lv(vp, sq.nk - (it + 1) * KT, next + kTile);
     }
     if (k0 <= mine) {
       // Operands are on their way from LDS ahead of the products that take them, and arithmetic stands between products: a wave issues in
@@ -121,7 +124,7 @@ __global__ __launch_bounds__(256) ADORE_WAVES(sizeof(T) == 4 ? 1 : DH == 128 ? 2
         }
       }
       pin();
-      if (k0 + KT - 1 > q0 + off) {             // some of the wave's queries do not see all of the tile
+      if (k0 + 32 * KB - 1 > q0 + off) {        // some of the wave's queries do not see all of these keys
 #pragma unroll
         for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
@@ -178,6 +181,34 @@ __global__ __launch_bounds__(256) ADORE_WAVES(sizeof(T) == 4 ? 1 : DH == 128 ? 2
   }
   __syncthreads();
   found = any_of_four(found, reinterpret_cast<int *>(smem + 4 * 32 * L::kRow));
+  if constexpr (SW > 1) {
+    constexpr int kFloats = 64 * (16 * DB + 2);
+    float *const parts = reinterpret_cast<float *>(smem + 4 * 32 * L::kRow + 256) + mate.rows * kFloats;   // behind any_of_four's words
+    constexpr int kPart = Shared<SW>::kRowWaves * kFloats;
+    if (mate.part > 0) {
+      float *const to = parts + (mate.part - 1) * kPart;
+      put_sums(o, to, lane);
+      to[16 * DB * 64 + lane] = top;
+      to[(16 * DB + 1) * 64 + lane] = sum;
+    }
+    __syncthreads();
+    if (mate.part > 0) return;
+    float m = top;
+#pragma unroll
+    for (int i = 0; i < SW - 1; ++i) m = fmaxf(m, parts[i * kPart + 16 * DB * 64 + lane]);
+    auto fade = [&](float t) { return t == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((t - m) * scale); };
+    const float mine_fades = fade(top);
+    sum *= mine_fades;
+#pragma unroll
+    for (int db = 0; db < DB; ++db) o[db] *= mine_fades;
+#pragma unroll
+    for (int i = 0; i < SW - 1; ++i) {
+      const float f = fade(parts[i * kPart + 16 * DB * 64 + lane]);
+      sum = fmaf(parts[i * kPart + (16 * DB + 1) * 64 + lane], f, sum);
+      add_sums(o, parts + i * kPart, f, lane);
+    }
+    top = m;
+  }
   if (rows <= 0) return;
   if (found)
     add_not_finite<T, DH>(o, reinterpret_cast<const char *>(a.v.p + sq.b * a.v.seq + sq.k_first * a.v.token + hk * a.v.head),
@@ -196,16 +227,24 @@ __global__ __launch_bounds__(256) ADORE_WAVES(sizeof(T) == 4 ? 1 : DH == 128 ? 2
                     a.rest.token * int64_t(sizeof(T)), lane);
 }
 
-template <typename T, int DH, bool REST>
-hipError_t launch_attend_prompt(AttendArgs<T> a, hipStream_t st) {
+template <typename T, int DH, bool REST, int SW>
+hipError_t launch_attend_shared(AttendArgs<T> a, hipStream_t st) {
   // a stage, and behind it another one or the waves' 32 queries each
-  constexpr int stage = 2 * kKeys<T> * Tile<T, DH>::kRow, waves = 4 * 32 * Tile<T, DH>::kRow, lds = stage + (stage > waves ? stage : waves);
-  const hipError_t e = allow_lds(&prompt_attend_kernel<T, DH, REST>, lds);
+  constexpr int row = Tile<T, DH>::kRow, stage = 2 * (SW > 1 ? 32 * SW : kKeys<T>) * row, waves = 4 * 32 * row, lds = stage + (stage > waves ? stage : waves);
+  static_assert(SW == 1 || waves + 256 + 4 * (SW - 1) / SW * 256 * (DH / 2 + 2) <= lds, "the parts' sums");
+  const hipError_t e = allow_lds(&prompt_attend_kernel<T, DH, REST, SW>, lds);
   if (e != hipSuccess) return e;
-  const long long blocks = blocks_at_most(a.s.q_start, a.s.batch, a.s.q_tokens, 128) * a.s.heads;
+  const long long blocks = blocks_at_most(a.s.q_start, a.s.batch, a.s.q_tokens, Shared<SW>::kRows) * a.s.heads;
   a.by_work = blocks < 1024;      // two for each place: beyond, what a sequence's blocks share counts for more (4096: 198 / 229 us)
-  hipLaunchKernelGGL((prompt_attend_kernel<T, DH, REST>), dim3(unsigned(blocks)), dim3(256), lds, st, a);
+  hipLaunchKernelGGL((prompt_attend_kernel<T, DH, REST, SW>), dim3(unsigned(blocks)), dim3(256), lds, st, a);
   return hipGetLastError();
+}
+
+template <typename T, int DH, bool REST>
+hipError_t launch_attend_prompt(const AttendArgs<T> &a, hipStream_t st) {
+  if (share_queries<T>(a.s))
+    return launch_attend_shared<T, DH, REST, DH * sizeof(T) == 512 ? 2 : 4>(a, st);      // (as many as two stages leave LDS for)
+  return launch_attend_shared<T, DH, REST, 1>(a, st);
 }
 
 // ---- the attention every key received -----------------------------------------------------------------------------
@@ -223,9 +262,9 @@ struct ScoreArgs {
 template <typename T>
 constexpr int kQueries = sizeof(T) == 2 ? 64 : 32;
 
-template <typename T, int DH>
+template <typename T, int DH, int SW>
 __global__ __launch_bounds__(256) void prompt_scores_kernel(const ScoreArgs<T> a) {
-  constexpr int NT = 256, BK = 128, QT = kQueries<T>, QB = QT / 32, ST = DH / 16;
+  constexpr int NT = 256, BK = Shared<SW>::kRows, QT = SW > 1 ? 32 * SW : kQueries<T>, WQ = SW > 1 ? 32 : QT, QB = WQ / 32, ST = DH / 16;
   typedef Tile<T, DH> L;
   typedef typename Operand<T>::type Frag;
   constexpr int kTile = QT * L::kRow;
@@ -241,7 +280,8 @@ __global__ __launch_bounds__(256) void prompt_scores_kernel(const ScoreArgs<T> a
     if (tid < n) a.scores[size_t(hk) * a.s.k_tokens + first + tid] = 0.f;
     return;
   }
-  const int k0 = block * BK + wave * 32, off = sq.nk - sq.nq;
+  const Shared<SW> mate(wave);
+  const int k0 = block * BK + mate.rows * 32, off = sq.nk - sq.nq;
   const int rows = min(32, sq.nk - k0);
   const int first = max(block * BK - off, 0) / QT * QT;    // the first tile with a query that sees a key of the workgroup
   const int per = first < sq.nq ? (sq.nq - first + QT - 1) / QT : 0, tiles = per * a.s.group;
@@ -265,25 +305,28 @@ __global__ __launch_bounds__(256) void prompt_scores_kernel(const ScoreArgs<T> a
       lp += a.s.q_tokens;
     }
   };
-  Reader<T, DH> read(base0, lane);
+  Reader<T, DH> read(base0 + uint32_t(mate.part * 32 * L::kRow), lane);
   Frag kf[ST];                                              // through the wave's quarter of LDS
   operand_rows<T, DH, false>(kf, read, reinterpret_cast<const char *>(a.k.p + sq.b * a.k.seq + (int64_t(sq.k_first) + k0) * a.k.token + hk * a.k.head),
-                      a.k.token * int64_t(sizeof(T)), rows, smem + wave * (32 * L::kRow), wave * (32 * L::kRow), lane);
+                      a.k.token * int64_t(sizeof(T)), rows, smem + wave * (32 * L::kRow),
+                      uint32_t((wave - mate.part) * (32 * L::kRow)), lane);
   __syncthreads();
   if (tiles > 0) load(0);
   if (tid < QT) s_lse[0][tid] = row_lse;
   float sum = 0.f;
-  int q0 = first - QT;
+  const int mine = mate.part * 32;                          // the wave's first query of a tile's
+  int tile = first - QT;
   for (int it = 0; it < tiles; ++it) {
-    q0 += QT;
-    if (q0 >= sq.nq) q0 = first;
+    tile += QT;
+    if (tile >= sq.nq) tile = first;
+    const int q0 = tile + mine;
     arrived();
     __syncthreads();
     if (it + 1 < tiles) load(~it & 1);
     Frag x[ST];
     float part[4] = {0.f};
     // A hidden query whose log-sum-exp is NaN: its weights are none at all, where the sums below would make them NaN.
-    if (q0 + off < k0 + 31 && __builtin_amdgcn_ballot_w64(s_lse[it & 1][lane % QT] != s_lse[it & 1][lane % QT])) {
+    if (q0 + off < k0 + 31 && __builtin_amdgcn_ballot_w64(s_lse[it & 1][mine + lane % WQ] != s_lse[it & 1][mine + lane % WQ])) {
 #pragma unroll 1
       for (int qb = 0; qb < QB; ++qb) {
         f32x16 s = {0.f};
@@ -292,7 +335,7 @@ __global__ __launch_bounds__(256) void prompt_scores_kernel(const ScoreArgs<T> a
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
           const int i = qb * 32 + 8 * (r >> 2) + 4 * h + (r & 3);
-          if (k0 + c <= q0 + i + off) part[r & 3] += __builtin_amdgcn_exp2f(fmaf(s[r], scale, -s_lse[it & 1][i]));
+          if (k0 + c <= q0 + i + off) part[r & 3] += __builtin_amdgcn_exp2f(fmaf(s[r], scale, -s_lse[it & 1][mine + i]));
         }
       }
       sum += (part[0] + part[1]) + (part[2] + part[3]);
@@ -304,7 +347,7 @@ __global__ __launch_bounds__(256) void prompt_scores_kernel(const ScoreArgs<T> a
     for (int t = 0; t < ST; ++t) x[t] = read.by_row(0, 0, t);
     f32x16 s[QB];
     auto weights = [&](int qb, int r4) {
-      const f32x4 lse = *reinterpret_cast<const f32x4 *>(&s_lse[it & 1][qb * 32 + 8 * r4 + 4 * h]);
+      const f32x4 lse = *reinterpret_cast<const f32x4 *>(&s_lse[it & 1][mine + qb * 32 + 8 * r4 + 4 * h]);
 #pragma unroll
       for (int i = 0; i < 4; ++i) part[i] += __builtin_amdgcn_exp2f(fmaf(s[qb][4 * r4 + i], scale, -lse[i]));
     };
@@ -336,18 +379,33 @@ __global__ __launch_bounds__(256) void prompt_scores_kernel(const ScoreArgs<T> a
     read.move(it & 1 ? uint32_t(-kTile) : uint32_t(kTile));
   }
   sum = add_lane_xor<32>(sum);
+  if constexpr (SW > 1) {
+    float *const sums = reinterpret_cast<float *>(smem);    // [part][rows of the workgroup]
+    __syncthreads();
+    if (lane < 32) sums[mate.part * BK + mate.rows * 32 + lane] = sum;
+    __syncthreads();
+    if (mate.part > 0) return;
+#pragma unroll
+    for (int i = 1; i < SW; ++i) sum += sums[i * BK + mate.rows * 32 + c];
+  }
   if (lane < rows) a.scores[row_value(packed, sq.b, sq.k_first, a.s.k_tokens, a.s.kv_heads, hk) + k0 + lane] = sum;
 }
 
-template <typename T, int DH>
-hipError_t launch_scores(ScoreArgs<T> a, hipStream_t st) {
-  constexpr int tiles = 2 * kQueries<T> * Tile<T, DH>::kRow, keys = 128 * Tile<T, DH>::kRow, lds = tiles > keys ? tiles : keys;
-  const hipError_t e = allow_lds(&prompt_scores_kernel<T, DH>, lds);
+template <typename T, int DH, int SW>
+hipError_t launch_scores_shared(ScoreArgs<T> a, hipStream_t st) {
+  constexpr int tiles = 2 * (SW > 1 ? 32 * SW : kQueries<T>) * Tile<T, DH>::kRow, keys = 128 * Tile<T, DH>::kRow, lds = tiles > keys ? tiles : keys;
+  const hipError_t e = allow_lds(&prompt_scores_kernel<T, DH, SW>, lds);
   if (e != hipSuccess) return e;
-  const long long blocks = blocks_at_most(a.s.k_start, a.s.batch, a.s.k_tokens, 128) * a.s.kv_heads;
+  const long long blocks = blocks_at_most(a.s.k_start, a.s.batch, a.s.k_tokens, Shared<SW>::kRows) * a.s.kv_heads;
   a.by_work = blocks < 1024;      // (as above; 1512: 177 / 197 us)
-  hipLaunchKernelGGL((prompt_scores_kernel<T, DH>), dim3(unsigned(blocks)), dim3(256), lds, st, a);
+  hipLaunchKernelGGL((prompt_scores_kernel<T, DH, SW>), dim3(unsigned(blocks)), dim3(256), lds, st, a);
   return hipGetLastError();
+}
+
+template <typename T, int DH>
+hipError_t launch_scores(const ScoreArgs<T> &a, hipStream_t st) {
+  if (share_scored_keys(a.s)) return launch_scores_shared<T, DH, 4>(a, st);
+  return launch_scores_shared<T, DH, 1>(a, st);
 }
 
 template <typename T>

@@ -65,9 +65,9 @@ __device__ __forceinline__ void carry_dots(float (&dot)[N], const char *d_out, i
 template <typename T>
 constexpr int kDqKeys = sizeof(T) == 2 ? 64 : 32;
 
-template <typename T, int DH>
-__global__ __launch_bounds__(256) ADORE_WAVES(sizeof(T) == 4 ? 1 : DH == 128 ? 2 : 3) void prompt_dq_kernel(const BackwardArgs<T> a) {
-  constexpr int NT = 256, BQ = 128, KT = kDqKeys<T>, KB = KT / 32, DB = DH / 32, ST = DH / 16;
+template <typename T, int DH, int SW>
+__global__ __launch_bounds__(256) ADORE_WAVES(sizeof(T) == 4 || SW > 1 ? 1 : DH == 128 ? 2 : 3) void prompt_dq_kernel(const BackwardArgs<T> a) {
+  constexpr int NT = 256, BQ = Shared<SW>::kRows, KT = SW > 1 ? 32 * SW : kDqKeys<T>, KB = SW > 1 ? 1 : KT / 32, DB = DH / 32, ST = DH / 16;
   typedef Tile<T, DH> L;
   typedef typename Operand<T>::type Frag;
   constexpr int kTile = KT * L::kRow;
@@ -82,7 +82,8 @@ __global__ __launch_bounds__(256) ADORE_WAVES(sizeof(T) == 4 ? 1 : DH == 128 ? 2
     zero_rows<T, DH>(a.dq, head, first, n, tid, NT);
     return;
   }
-  const int q0 = block * BQ + wave * 32, off = sq.nk - sq.nq;
+  const Shared<SW> mate(wave);
+  const int q0 = block * BQ + mate.rows * 32, off = sq.nk - sq.nq;
   const int rows = min(32, sq.nq - q0);
   const int64_t row = int64_t(sq.q_first) + q0, es = int64_t(sizeof(T));
   const char *kp = reinterpret_cast<const char *>(a.k.p + sq.b * a.k.seq + sq.k_first * a.k.token + hk * a.k.head);
@@ -91,15 +92,17 @@ __global__ __launch_bounds__(256) ADORE_WAVES(sizeof(T) == 4 ? 1 : DH == 128 ? 2
   const int mine = rows > 0 ? q0 + rows - 1 + off : -1, seen = q0 + c + off;
   const float scale = a.s.scale_log2;
   const uint32_t base0 = __builtin_amdgcn_readfirstlane(lds_offset(smem)), share = base0 + uint32_t(wave) * 1024u;
-  Reader<T, DH> read(base0, lane);
+  Reader<T, DH> read(base0 + uint32_t(mate.part * 32 * L::kRow), lane);
   const TileLoad<T, DH, KT, NT> lk(a.k.token * es, tid), lv(a.v.token * es, tid);
   if (tiles > 0) {
     lk(kp, sq.nk, share);
     lv(vp, sq.nk, share + kTile);
   }
   unsigned char *own = smem + 2 * kTile + wave * (32 * L::kRow);    // the wave's share of the second stage
+  const uint32_t own_ahead = uint32_t(2 * kTile + (wave - mate.part) * (32 * L::kRow));
   Frag qf[ST], df[ST];
-  operand_rows<T, DH, false>(qf, read, reinterpret_cast<const char *>(a.q.p + sq.b * a.q.seq + row * a.q.token + head * a.q.head), a.q.token * es, rows, own, 2 * kTile + wave * (32 * L::kRow), lane);
+  operand_rows<T, DH, false>(qf, read, reinterpret_cast<const char *>(a.q.p + sq.b * a.q.seq + row * a.q.token + head * a.q.head), a.q.token * es,
+                             rows, own, own_ahead, lane);
   // of the lane's query; weights of a query that is not there are 0
   float lse = INFINITY, delta = 0.f;
   {
@@ -117,7 +120,7 @@ __global__ __launch_bounds__(256) ADORE_WAVES(sizeof(T) == 4 ? 1 : DH == 128 ? 2
     }
     wave_lds_fence();
 #pragma unroll
-    for (int t = 0; t < ST; ++t) df[t] = read.by_row(2 * kTile + wave * (32 * L::kRow), 0, t);
+    for (int t = 0; t < ST; ++t) df[t] = read.by_row(own_ahead, 0, t);
     wave_lds_fence();
     if (rows > 0) {
       float *const s_delta = reinterpret_cast<float *>(own);
@@ -128,7 +131,7 @@ __global__ __launch_bounds__(256) ADORE_WAVES(sizeof(T) == 4 ? 1 : DH == 128 ? 2
       wave_lds_fence();
       if (c < rows) {
         delta = s_delta[c];
-        if (h == 0) a.delta[at + c] = delta;    // for dk and dv
+        if (h == 0 && mate.part == 0) a.delta[at + c] = delta;    // for dk and dv
       }
     }
   }
@@ -138,7 +141,7 @@ __global__ __launch_bounds__(256) ADORE_WAVES(sizeof(T) == 4 ? 1 : DH == 128 ? 2
   const int hidden = max(block * BQ + off + 1, 0) / KT;    // the first tile that not all of the workgroup's queries see all of
   bool found = false;                                      // ... where an element of K is not finite
   for (int it = 0; it < tiles; ++it) {
-    const int k0 = it * KT;
+    const int k0 = it * KT + mate.part * 32;
     arrived();
     __syncthreads();
     if (it >= hidden) {
@@ -149,8 +152,8 @@ __global__ __launch_bounds__(256) ADORE_WAVES(sizeof(T) == 4 ? 1 : DH == 128 ? 2
       const uint32_t next = share + uint32_t(~it & 1) * uint32_t(2 * kTile);
       kp += KT * a.k.token * es;
       vp += KT * a.v.token * es;
-      lk(kp, sq.nk - k0 - KT, next);
-      lv(vp, sq.nk - k0 - KT, next + kTile);
+      lk(kp, sq.nk - (it + 1) * KT, next);
+      lv(vp, sq.nk - (it + 1) * KT, next + kTile);
     }
     if (k0 > mine) {
       read.move(it & 1 ? uint32_t(-2 * kTile) : uint32_t(2 * kTile));
@@ -216,6 +219,15 @@ __global__ __launch_bounds__(256) ADORE_WAVES(sizeof(T) == 4 ? 1 : DH == 128 ? 2
   }
   __syncthreads();
   found = any_of_four(found, reinterpret_cast<int *>(smem));
+  if constexpr (SW > 1) {
+    constexpr int kFloats = 64 * 16 * DB, kPart = Shared<SW>::kRowWaves * kFloats;
+    float *const parts = reinterpret_cast<float *>(smem + 256) + mate.rows * kFloats;
+    if (mate.part > 0) put_sums(dq, parts + (mate.part - 1) * kPart, lane);
+    __syncthreads();
+    if (mate.part > 0) return;
+#pragma unroll
+    for (int i = 0; i < SW - 1; ++i) add_sums(dq, parts + i * kPart, 1.f, lane);
+  }
   if (rows <= 0) return;
   if (found)
     add_not_finite<T, DH>(dq, reinterpret_cast<const char *>(a.k.p + sq.b * a.k.seq + sq.k_first * a.k.token + hk * a.k.head), a.k.token * es, hidden * KT,
@@ -227,17 +239,14 @@ __global__ __launch_bounds__(256) ADORE_WAVES(sizeof(T) == 4 ? 1 : DH == 128 ? 2
 // ---- dk and dv: 128 keys a workgroup, 32 a wave ----
 // At 128 elements a wave's K, V and their gradients would be 192 registers, and with the rest more than two waves a SIMD leave room for:
 // V stays in LDS (a spilled register in the loop costs a wait for the next tile: loads return in order).
-template <typename T>
-constexpr int kDkvQueries = 32;
-
-template <typename T, int DH>
-__global__ __launch_bounds__(256) ADORE_WAVES(sizeof(T) == 2 ? 2 : 1) void prompt_dkv_kernel(const BackwardArgs<T> a) {
-  constexpr int NT = 256, BK = 128, QT = kDkvQueries<T>, DB = DH / 32, ST = DH / 16;
+template <typename T, int DH, int SW>
+__global__ __launch_bounds__(256) ADORE_WAVES(sizeof(T) == 2 && SW == 1 ? 2 : 1) void prompt_dkv_kernel(const BackwardArgs<T> a) {
+  constexpr int NT = 256, BK = Shared<SW>::kRows, QT = 32 * SW, DB = DH / 32, ST = DH / 16;
   typedef Tile<T, DH> L;
   typedef typename Operand<T>::type Frag;
   constexpr int kTile = QT * L::kRow, kWave = 32 * L::kRow;
   extern __shared__ __align__(16) unsigned char smem[];   // two stages of Q and dO (32 rows a wave besides), the workgroup's V
-  float *const s_lse = reinterpret_cast<float *>(smem + 8 * kTile), *const s_delta = s_lse + 2 * QT;   // [stage][QT] each, behind V
+  float *const s_lse = reinterpret_cast<float *>(smem + 4 * kTile + Shared<SW>::kRowWaves * kWave), *const s_delta = s_lse + 2 * QT;   // [stage][QT] each, behind V
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), c = lane & 31, h = lane >> 5;
   const int hk = blockIdx.x % a.s.kv_heads;
   Sequence sq;
@@ -249,7 +258,8 @@ __global__ __launch_bounds__(256) ADORE_WAVES(sizeof(T) == 2 ? 2 : 1) void promp
     zero_rows<T, DH>(a.dv, hk, first, n, tid, NT);
     return;
   }
-  const int k0 = block * BK + wave * 32, off = sq.nk - sq.nq;
+  const Shared<SW> mate(wave);
+  const int k0 = block * BK + mate.rows * 32, off = sq.nk - sq.nq;
   const int rows = min(32, sq.nk - k0);
   const int64_t row = int64_t(sq.k_first) + k0, es = int64_t(sizeof(T));
   // Queries that some of the block's keys are hidden from, if one of them is not finite, or has no keys (log-sum-exp or delta tells), are
@@ -266,7 +276,7 @@ __global__ __launch_bounds__(256) ADORE_WAVES(sizeof(T) == 2 ? 2 : 1) void promp
   const float scale = a.s.scale_log2;
   const bool packed = a.s.q_start != nullptr;
   const uint32_t base0 = __builtin_amdgcn_readfirstlane(lds_offset(smem)), share = base0 + uint32_t(wave) * 1024u;
-  Reader<T, DH, sizeof(T) == 2> read(base0, lane);
+  Reader<T, DH, sizeof(T) == 2> read(base0 + uint32_t(mate.part * kWave), lane);
   const TileLoad<T, DH, QT, NT> lq(a.q.token * es, tid), ld(a.d_out.token * es, tid);
   // The tile after the last one loaded: its head's rows, its first query.  From the last query back to the diagonal: the workgroups of
   // a head start with the same tiles, one reads what the others find in the L2.
@@ -299,32 +309,33 @@ __global__ __launch_bounds__(256) ADORE_WAVES(sizeof(T) == 2 ? 2 : 1) void promp
     }
   };
   unsigned char *own = smem + wave * kWave;
-  constexpr int kVAt = 4 * kTile;                          // = four waves' 32 rows: a stage is 64 of them
-  static_assert(4 * kTile == 4 * kWave, "the waves' own rows end where V begins");
+  constexpr int kVAt = 4 * kTile;
+  static_assert(4 * kTile >= 4 * kWave, "the waves' own rows end where V begins, or before");
   Frag kf[ST];
   operand_rows<T, DH, sizeof(T) == 2>(kf, read, reinterpret_cast<const char *>(a.k.p + sq.b * a.k.seq + row * a.k.token + hk * a.k.head), a.k.token * es, rows, own,
-                      wave * kWave, lane);
-  if (rows > 0)
+                      uint32_t((wave - mate.part) * kWave), lane);
+  if (rows > 0 && mate.part == 0)
     carry_rows<T, DH>(reinterpret_cast<const char *>(a.v.p + sq.b * a.v.seq + row * a.v.token + hk * a.v.head), a.v.token * es, rows,
-                      own + kVAt, lane);
+                      smem + kVAt + mate.rows * kWave, lane);
   __syncthreads();
   if (tiles > 0) load(0);
   hand_over(0);
-  const uint32_t v_ahead = kVAt + uint32_t(wave) * kWave;  // of the reader at stage 0
+  const uint32_t v_ahead = uint32_t(kVAt + (mate.rows - mate.part) * kWave);   // of the reader at stage 0
   f32x16 dk[DB], dv[DB];
 #pragma unroll
   for (int db = 0; db < DB; ++db) dk[db] = dv[db] = f32x16{0.f};
-  int q0 = final + QT;
+  int tile = final + QT;
   for (int it = 0; it < tiles; ++it) {
-    q0 -= QT;
-    if (q0 < first) q0 = final;
+    tile -= QT;
+    if (tile < first) tile = final;
+    const int q0 = tile + mate.part * 32;                   // the wave's first query of the tile
     arrived();
     __syncthreads();
     if (it + 1 < tiles) load(~it & 1);
     // Operands on their way ahead of their products, arithmetic between products (a wave issues in order).  A tile that none of the wave's
     // keys is seen from is worked on like any other: its weights are zeros.
     const uint32_t va = v_ahead - uint32_t((it & 1) * 2 * kTile);
-    const float *const rows_lse = s_lse + (it & 1) * QT + 4 * h, *const rows_delta = s_delta + (it & 1) * QT + 4 * h;
+    const float *const rows_lse = s_lse + (it & 1) * QT + mate.part * 32 + 4 * h, *const rows_delta = rows_lse + 2 * QT;
     Frag x[4], y[4];                                        // rings, four products deep
     f32x16 s = {0.f}, g = {0.f};
 #pragma unroll
@@ -394,6 +405,22 @@ __global__ __launch_bounds__(256) ADORE_WAVES(sizeof(T) == 2 ? 2 : 1) void promp
     read.move(it & 1 ? uint32_t(-2 * kTile) : uint32_t(2 * kTile));
   }
   __syncthreads();
+  if constexpr (SW > 1) {
+    constexpr int kFloats = 64 * 16 * DB * 2, kPart = Shared<SW>::kRowWaves * kFloats;
+    static_assert(4 * kWave + (SW - 1) * kPart * 4 <= 4 * kTile, "the parts' sums lie in the stages, behind the waves' own rows");
+    float *const parts = reinterpret_cast<float *>(smem + 4 * kWave) + mate.rows * kFloats;
+    if (mate.part > 0) {
+      put_sums(dk, parts + (mate.part - 1) * kPart, lane);
+      put_sums(dv, parts + (mate.part - 1) * kPart + kFloats / 2, lane);
+    }
+    __syncthreads();
+    if (mate.part > 0) return;
+#pragma unroll
+    for (int i = 0; i < SW - 1; ++i) {
+      add_sums(dk, parts + i * kPart, 1.f, lane);
+      add_sums(dv, parts + i * kPart + kFloats / 2, 1.f, lane);
+    }
+  }
   if (rows <= 0) return;
   if (odd) {
     // a lane: its key, half of the elements
@@ -438,26 +465,43 @@ __global__ __launch_bounds__(256) ADORE_WAVES(sizeof(T) == 2 ? 2 : 1) void promp
                     nullptr, 0, lane);
 }
 
-template <typename T, int DH>
-hipError_t launch_backward(BackwardArgs<T> a, hipStream_t st) {
+template <typename T, int DH, int SW>
+hipError_t launch_dq(BackwardArgs<T> a, hipStream_t st) {
   // a stage, and behind it another one or every wave's own 32 rows, for the operands at the beginning and the results at the end
-  constexpr int row = Tile<T, DH>::kRow, waves = 4 * 32 * row, dq_stage = 2 * kDqKeys<T> * row;
-  constexpr int dq_lds = dq_stage + (dq_stage > waves ? dq_stage : waves), dkv_lds = 4 * kDkvQueries<T> * row + waves + 4 * kDkvQueries<T> * 4 + 16;
-  hipError_t e = allow_lds(&prompt_dq_kernel<T, DH>, dq_lds);
-  if (e == hipSuccess) e = allow_lds(&prompt_dkv_kernel<T, DH>, dkv_lds);
+  constexpr int row = Tile<T, DH>::kRow, stage = 2 * (SW > 1 ? 32 * SW : kDqKeys<T>) * row, waves = 4 * 32 * row, lds = stage + (stage > waves ? stage : waves);
+  static_assert(SW == 1 || 256 + 4 * (SW - 1) / SW * 256 * (DH / 2) <= stage, "the parts' sums lie in the first stage");
+  const hipError_t e = allow_lds(&prompt_dq_kernel<T, DH, SW>, lds);
   if (e != hipSuccess) return e;
-  if (a.s.q_tokens > 0) {
-    const long long query_blocks = blocks_at_most(a.s.q_start, a.s.batch, a.s.q_tokens, 128) * a.s.heads;
-    a.by_work = query_blocks < 1024;
-    hipLaunchKernelGGL((prompt_dq_kernel<T, DH>), dim3(unsigned(query_blocks)), dim3(256), dq_lds, st, a);
-    if ((e = hipGetLastError()) != hipSuccess) return e;
-  }
-  if (a.s.k_tokens > 0) {
-    const long long key_blocks = blocks_at_most(a.s.k_start, a.s.batch, a.s.k_tokens, 128) * a.s.kv_heads;
-    a.by_work = key_blocks < 2048;   // 1024, with 4 to 64 tiles of 4 heads each: 796 -> 610 us
-    hipLaunchKernelGGL((prompt_dkv_kernel<T, DH>), dim3(unsigned(key_blocks)), dim3(256), dkv_lds, st, a);
-  }
+  const long long blocks = blocks_at_most(a.s.q_start, a.s.batch, a.s.q_tokens, Shared<SW>::kRows) * a.s.heads;
+  a.by_work = blocks < 1024;
+  hipLaunchKernelGGL((prompt_dq_kernel<T, DH, SW>), dim3(unsigned(blocks)), dim3(256), lds, st, a);
   return hipGetLastError();
+}
+
+template <typename T, int DH, int SW>
+hipError_t launch_dkv(BackwardArgs<T> a, hipStream_t st) {
+  // two stages of Q and dO, V, a stage's log-sum-exps and deltas twice, four words
+  constexpr int lds = (4 * 32 * SW + Shared<SW>::kRows) * Tile<T, DH>::kRow + 4 * 32 * SW * 4 + 16;
+  const hipError_t e = allow_lds(&prompt_dkv_kernel<T, DH, SW>, lds);
+  if (e != hipSuccess) return e;
+  const long long blocks = blocks_at_most(a.s.k_start, a.s.batch, a.s.k_tokens, Shared<SW>::kRows) * a.s.kv_heads;
+  a.by_work = blocks < 2048;   // 1024, with 4 to 64 tiles of 4 heads each: 796 -> 610 us
+  hipLaunchKernelGGL((prompt_dkv_kernel<T, DH, SW>), dim3(unsigned(blocks)), dim3(256), lds, st, a);
+  return hipGetLastError();
+}
+
+template <typename T, int DH>
+hipError_t launch_backward(const BackwardArgs<T> &a, hipStream_t st) {
+  constexpr bool wide = DH * sizeof(T) == 512;       // rows that LDS has no room for twice 128 of (dq), twice 64 and V (dk and dv)
+  hipError_t e = hipSuccess;
+  if (a.s.q_tokens > 0) e = share_queries<T>(a.s) ? launch_dq<T, DH, wide ? 2 : 4>(a, st) : launch_dq<T, DH, 1>(a, st);
+  if (e == hipSuccess && a.s.k_tokens > 0) {
+    if constexpr (!wide) {
+      if (share_keys<T>(a.s)) return launch_dkv<T, DH, 4>(a, st);
+    }
+    e = launch_dkv<T, DH, 1>(a, st);
+  }
+  return e;
 }
 
 size_t delta_bytes(const adore_prompt_config &c, bool packed) {

@@ -355,6 +355,55 @@ __device__ __forceinline__ bool make_finite(unsigned char *tile) {
   return __builtin_amdgcn_ballot_w64(found) != 0;
 }
 
+// ---- waves that share rows ----
+// Where blocks of 128 rows are too few to fill the chip, a workgroup takes fewer rows and SW of its four waves the same 32: each a part of
+// what those rows go over, 32 of a tile's 32 SW.  At the end the first of them adds up the others' sums.  Four times the workgroups, of which
+// a unit has room for one (two stages of wide tiles), and none waits four times as long as it must for the longest row.  Both sides
+// (128-row blocks / shared rows, us; heads x tokens, bf16 at 128 elements unless said):
+//   forward  16 x 300 11.0 / 10.9, 32 x 512 15.6 / 20.0, 8 x 2048 40.7 / 32.5, 12 x 2048 41.4 / 50.3, 2 x 8000 135 / 89, 3 x 8000 140 / 137,
+//            4 x 8000 140 / 167, one query of 32 heads behind 4096 keys 72 / 45; fp32 64 elements: 4 x 128 15.0 / 9.0, 64 x 512 45.6 / 46.8,
+//            16 x 2048 159 / 111; fp32: 64 x 512 79 / 58
+//   dq       as the forward: 16 x 300 13.7 / 13.1, 32 x 512 19.0 / 24.3, 8 x 2048 50.4 / 39.4, 12 x 2048 52.6 / 62.1
+//   dk, dv   16 x 300 18.9 / 16.9, 32 x 512 28.9 / 32.8, 8 x 2048 90 / 55, 16 x 2048 108 / 110, 8 of 2 kv heads x 8000 1341 / 548, 4 x 8000
+//            381 / 301, 8 kv heads x 2560 behind 512 queries 94 / 120; fp32 64 elements: 4 x 128 23.8 / 12.0, 64 x 512 85 / 79
+//   scores   16 x 300 8.5 / 6.0, 64 x 512 12.3 / 12.0, 16 x 2048 36 / 24, 8 of 2 kv heads x 8000 490 / 216; 264 blocks behind 64 queries 9.2 / 17.6
+// (fp32 tiles are a quarter as fast and one workgroup of theirs fills a unit either way.)
+inline long long length_of(const int32_t *start, int batch, int tokens) { return start ? tokens / batch : tokens; }   // on average
+template <typename T>
+inline bool share_queries(const PromptShape &s) {
+  const int most = sizeof(T) == 4 ? 256 : length_of(s.q_start, s.batch, s.q_tokens) >= 2048 ? 128 : 64;
+  return blocks_at_most(s.q_start, s.batch, s.q_tokens, 128) * s.heads <= most;
+}
+inline long long key_blocks(const PromptShape &s) { return blocks_at_most(s.k_start, s.batch, s.k_tokens, 128) * s.kv_heads; }
+template <typename T>
+inline bool share_keys(const PromptShape &s) {          // of dk and dv
+  const long long queries = length_of(s.q_start, s.batch, s.q_tokens) * s.group;
+  return key_blocks(s) <= (sizeof(T) == 4 || queries >= 4096 ? 256 : queries >= 2048 ? 128 : 64);
+}
+inline bool share_scored_keys(const PromptShape &s) { return key_blocks(s) <= 256; }
+
+template <int SW>
+struct Shared {
+  static constexpr int kRowWaves = 4 / SW, kRows = 32 * kRowWaves;
+  int rows, part;                             // the wave's rows of the workgroup's, its part
+  __device__ __forceinline__ explicit Shared(int wave) : rows(wave % kRowWaves), part(wave / kRowWaves) {}
+};
+// A part's sums, as registers of 64 lanes, to and from LDS.
+template <int DB>
+__device__ __forceinline__ void put_sums(const f32x16 (&o)[DB], float *to, int lane) {
+#pragma unroll
+  for (int db = 0; db < DB; ++db)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) to[(16 * db + r) * 64 + lane] = o[db][r];
+}
+template <int DB>
+__device__ __forceinline__ void add_sums(f32x16 (&o)[DB], const float *from, float factor, int lane) {
+#pragma unroll
+  for (int db = 0; db < DB; ++db)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) o[db][r] = fmaf(from[(16 * db + r) * 64 + lane], factor, o[db][r]);
+}
+
 // Whether it holds in any of the workgroup's four waves; s: four words that nothing else uses from here on.
 __device__ __forceinline__ bool any_of_four(bool mine, int *s) {
   if ((threadIdx.x & 63) == 0) s[threadIdx.x >> 6] = mine;
