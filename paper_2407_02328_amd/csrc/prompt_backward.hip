@@ -239,14 +239,19 @@ __global__ __launch_bounds__(256) ADORE_WAVES(sizeof(T) == 4 || SW > 1 ? 1 : DH 
 // ---- dk and dv: 128 keys a workgroup, 32 a wave ----
 // At 128 elements a wave's K, V and their gradients would be 192 registers, and with the rest more than two waves a SIMD leave room for:
 // V stays in LDS (a spilled register in the loop costs a wait for the next tile: loads return in order).
+// (fp32 at 128 elements, waves that share keys: LDS has no room for V, one wave a SIMD leaves registers for it)
+template <typename T, int DH, int SW>
+constexpr bool kValuesInRegisters = SW > 1 && DH * sizeof(T) == 512;
+
 template <typename T, int DH, int SW>
 __global__ __launch_bounds__(256) ADORE_WAVES(sizeof(T) == 2 && SW == 1 ? 2 : 1) void prompt_dkv_kernel(const BackwardArgs<T> a) {
   constexpr int NT = 256, BK = Shared<SW>::kRows, QT = 32 * SW, DB = DH / 32, ST = DH / 16;
   typedef Tile<T, DH> L;
   typedef typename Operand<T>::type Frag;
   constexpr int kTile = QT * L::kRow, kWave = 32 * L::kRow;
+  constexpr bool VR = kValuesInRegisters<T, DH, SW>;
   extern __shared__ __align__(16) unsigned char smem[];   // two stages of Q and dO (32 rows a wave besides), the workgroup's V
-  float *const s_lse = reinterpret_cast<float *>(smem + 4 * kTile + Shared<SW>::kRowWaves * kWave), *const s_delta = s_lse + 2 * QT;   // [stage][QT] each, behind V
+  float *const s_lse = reinterpret_cast<float *>(smem + 4 * kTile + (VR ? 0 : Shared<SW>::kRowWaves * kWave)), *const s_delta = s_lse + 2 * QT;   // [stage][QT] each, behind V
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), c = lane & 31, h = lane >> 5;
   const int hk = blockIdx.x % a.s.kv_heads;
   Sequence sq;
@@ -314,7 +319,11 @@ __global__ __launch_bounds__(256) ADORE_WAVES(sizeof(T) == 2 && SW == 1 ? 2 : 1)
   Frag kf[ST];
   operand_rows<T, DH, sizeof(T) == 2>(kf, read, reinterpret_cast<const char *>(a.k.p + sq.b * a.k.seq + row * a.k.token + hk * a.k.head), a.k.token * es, rows, own,
                       uint32_t((wave - mate.part) * kWave), lane);
-  if (rows > 0 && mate.part == 0)
+  Frag vf[VR ? ST : 1];
+  if constexpr (VR)
+    operand_rows<T, DH, sizeof(T) == 2>(vf, read, reinterpret_cast<const char *>(a.v.p + sq.b * a.v.seq + row * a.v.token + hk * a.v.head), a.v.token * es,
+                                        rows, own, uint32_t((wave - mate.part) * kWave), lane);
+  else if (rows > 0 && mate.part == 0)
     carry_rows<T, DH>(reinterpret_cast<const char *>(a.v.p + sq.b * a.v.seq + row * a.v.token + hk * a.v.head), a.v.token * es, rows,
                       smem + kVAt + mate.rows * kWave, lane);
   __syncthreads();
@@ -345,7 +354,7 @@ __global__ __launch_bounds__(256) ADORE_WAVES(sizeof(T) == 2 && SW == 1 ? 2 : 1)
       pin();
       s = Operand<T>::mma(x[t & 3], kf[t], s);
       x[t & 3] = t + 4 < ST ? read.by_row(0, 0, t + 4) : read.by_row(kTile, 0, t + 4 - ST);
-      if (t >= ST - 4) y[t - ST + 4] = read.by_row(va, 0, t - ST + 4);
+      if (!VR && t >= ST - 4) y[t - ST + 4] = read.by_row(va, 0, t - ST + 4);
     }
     pin();
     if (q0 + off < k0 + 31) {                               // some of the queries do not see some of the wave's keys
@@ -360,9 +369,9 @@ __global__ __launch_bounds__(256) ADORE_WAVES(sizeof(T) == 2 && SW == 1 ? 2 : 1)
 #pragma unroll
     for (int t = 0; t < ST; ++t) {
       pin();
-      g = Operand<T>::mma(x[t & 3], y[t & 3], g);
+      g = Operand<T>::mma(x[t & 3], VR ? vf[VR ? t : 0] : y[t & 3], g);
       x[t & 3] = t + 4 < ST ? read.by_row(kTile, 0, t + 4) : next_of(t + 4 - ST);
-      if (t + 4 < ST) y[t & 3] = read.by_row(va, 0, t + 4);
+      if (!VR && t + 4 < ST) y[t & 3] = read.by_row(va, 0, t + 4);
       if (t % (ST / 4) == 0) {
         const int r4 = t / (ST / 4);
         const f32x4 lse = *reinterpret_cast<const f32x4 *>(rows_lse + 8 * r4);
@@ -481,7 +490,7 @@ hipError_t launch_dq(BackwardArgs<T> a, hipStream_t st) {
 template <typename T, int DH, int SW>
 hipError_t launch_dkv(BackwardArgs<T> a, hipStream_t st) {
   // two stages of Q and dO, V, a stage's log-sum-exps and deltas twice, four words
-  constexpr int lds = (4 * 32 * SW + Shared<SW>::kRows) * Tile<T, DH>::kRow + 4 * 32 * SW * 4 + 16;
+  constexpr int rows = 4 * 32 * SW + (kValuesInRegisters<T, DH, SW> ? 0 : Shared<SW>::kRows), lds = rows * Tile<T, DH>::kRow + 4 * 32 * SW * 4 + 16;
   const hipError_t e = allow_lds(&prompt_dkv_kernel<T, DH, SW>, lds);
   if (e != hipSuccess) return e;
   const long long blocks = blocks_at_most(a.s.k_start, a.s.batch, a.s.k_tokens, Shared<SW>::kRows) * a.s.kv_heads;
@@ -492,15 +501,10 @@ hipError_t launch_dkv(BackwardArgs<T> a, hipStream_t st) {
 
 template <typename T, int DH>
 hipError_t launch_backward(const BackwardArgs<T> &a, hipStream_t st) {
-  constexpr bool wide = DH * sizeof(T) == 512;       // rows that LDS has no room for twice 128 of (dq), twice 64 and V (dk and dv)
+  constexpr int SW = DH * sizeof(T) == 512 ? 2 : 4;  // (as many as two stages leave LDS for)
   hipError_t e = hipSuccess;
-  if (a.s.q_tokens > 0) e = share_queries<T>(a.s) ? launch_dq<T, DH, wide ? 2 : 4>(a, st) : launch_dq<T, DH, 1>(a, st);
-  if (e == hipSuccess && a.s.k_tokens > 0) {
-    if constexpr (!wide) {
-      if (share_keys<T>(a.s)) return launch_dkv<T, DH, 4>(a, st);
-    }
-    e = launch_dkv<T, DH, 1>(a, st);
-  }
+  if (a.s.q_tokens > 0) e = share_queries<T>(a.s) ? launch_dq<T, DH, SW>(a, st) : launch_dq<T, DH, 1>(a, st);
+  if (e == hipSuccess && a.s.k_tokens > 0) e = share_keys<T>(a.s) ? launch_dkv<T, DH, SW>(a, st) : launch_dkv<T, DH, 1>(a, st);
   return e;
 }
 
