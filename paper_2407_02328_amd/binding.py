@@ -201,6 +201,10 @@ def topk_attention_static(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, top
 _CODES = {torch.float32: ADORE_F32, torch.bfloat16: ADORE_BF16}
 
 
+# torch's current stream of a device as a number (torch.cuda.current_stream makes an object of it, 2 us)
+_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda index: torch.cuda.current_stream(index).cuda_stream)
+
+
 class _Prompts:
     """The sequences and heads of a call on prompts, read off q and k, and its tensors' descriptions.
 
@@ -217,6 +221,7 @@ class _Prompts:
             raise ValueError(f"q: expected a bf16 or fp32 GPU tensor, got {q.device} {q.dtype}")
         self.device, self.index, self.dtype = q.device, index, q.dtype
         self.q_shape, self.k_shape = qs, ks = q.shape, k.shape
+        self.q_odd, self.k_odd = 1 in qs or 0 in qs, 1 in ks or 0 in ks
         self.packed = packed = q_start is not None
         if len(qs) != (3 if packed else 4) or len(ks) != len(qs):
             raise ValueError("q, k: expected [tokens, heads, head_dim] with starts, [batch, heads, tokens, head_dim] without")
@@ -240,10 +245,12 @@ class _Prompts:
             self.q_rows, self.k_rows = qs[:3], ks[:3]
 
     def rows(self, t: torch.Tensor, shape, name: str, written: bool = False):
+        # (sizes of 1 and 0, whose strides mean nothing, are looked for once a shape)
         if not isinstance(t, torch.Tensor) or t.shape != shape or t.dtype is not self.dtype or t.get_device() != self.index:
             raise ValueError(f"{name}: expected a {self.dtype} tensor of shape {tuple(shape)} on {self.device}")
         stride = t.stride()
-        if stride[-1] != 1 or 0 in stride or 1 in shape or 0 in shape:
+        odd = self.q_odd if shape is self.q_shape else self.k_odd
+        if odd or stride[-1] != 1 or 0 in stride:
             if shape[-1] > 1 and stride[-1] != 1:
                 raise ValueError(f"{name}: its last dimension has to be dense")
             stride = tuple(0 if n <= 1 else s for n, s in zip(shape, stride))      # of one row: any
@@ -254,6 +261,14 @@ class _Prompts:
             return ctypes.byref(AdoreRows(ptr, 0, stride[0], stride[1]))
         return ctypes.byref(AdoreRows(ptr, stride[0], stride[2], stride[1]))
 
+    def fresh(self, t: torch.Tensor):
+        """Rows of a tensor that has just been made for a call: dense, and as it should be."""
+        shape = t.shape
+        if self.packed:
+            return ctypes.byref(AdoreRows(t.data_ptr() or 16, 0, shape[1] * shape[2], shape[2]))
+        head = shape[2] * shape[3]
+        return ctypes.byref(AdoreRows(t.data_ptr() or 16, shape[1] * head, shape[3], head))
+
     def values(self, t: torch.Tensor, shape, name: str):
         if not isinstance(t, torch.Tensor) or t.shape != shape or t.dtype is not torch.float32 or t.get_device() != self.index or \
                 not t.is_contiguous():
@@ -262,7 +277,7 @@ class _Prompts:
 
     @property
     def stream(self):
-        return torch.cuda.current_stream(self.index).cuda_stream
+        return _stream(self.index)
 
 
 def prompt_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, *, q_start: torch.Tensor = None,
@@ -275,13 +290,15 @@ def prompt_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, *, q_sta
     dense last dimension (q, k and v may be views of one projection).  out is allocated here unless given."""
     lib = load_library()
     p = _Prompts(q, k, q_start, k_start, scale)
+    rows = None
     if out is None:
-        out = torch.empty(p.q_shape, dtype=q.dtype, device=q.device)
-    lse = torch.empty(p.q_rows, dtype=torch.float32, device=q.device)
-    left = torch.empty(p.q_shape, dtype=q.dtype, device=q.device) if rest and q.dtype == torch.bfloat16 else None
+        out = torch.empty(p.q_shape, dtype=q.dtype, device=p.device)
+        rows = p.fresh(out)
+    lse = torch.empty(p.q_rows, dtype=torch.float32, device=p.device)
+    left = torch.empty(p.q_shape, dtype=q.dtype, device=p.device) if rest and q.dtype == torch.bfloat16 else None
     _check(lib, lib.adore_prompt_attention(ctypes.byref(p.cfg), *p.starts, p.rows(q, p.q_shape, "q"), p.rows(k, p.k_shape, "k"),
-                                           p.rows(v, p.k_shape, "v"), p.rows(out, p.q_shape, "out", True), p.values(lse, p.q_rows, "lse"),
-                                           None if left is None else p.rows(left, p.q_shape, "rest", True), p.stream))
+                                           p.rows(v, p.k_shape, "v"), rows or p.rows(out, p.q_shape, "out", True), lse.data_ptr() or 16,
+                                           None if left is None else p.fresh(left), p.stream))
     return (out, lse, left) if rest else (out, lse)
 
 
@@ -294,15 +311,19 @@ def prompt_attention_backward(d_out: torch.Tensor, q: torch.Tensor, k: torch.Ten
     q, k and v in the gradient of one projection, say)."""
     lib = load_library()
     p = _Prompts(q, k, q_start, k_start, scale)
-    dq, dk, dv = (torch.empty(s, dtype=q.dtype, device=q.device) if t is None else t
-                  for t, s in ((dq, p.q_shape), (dk, p.k_shape), (dv, p.k_shape)))
+    def gradient(t, shape, name):
+        if t is not None:
+            return t, p.rows(t, shape, name, True)
+        t = torch.empty(shape, dtype=q.dtype, device=p.device)
+        return t, p.fresh(t)
+
+    (dq, dq_rows), (dk, dk_rows), (dv, dv_rows) = gradient(dq, p.q_shape, "dq"), gradient(dk, p.k_shape, "dk"), gradient(dv, p.k_shape, "dv")
     need = lib.adore_prompt_backward_workspace_bytes(ctypes.byref(p.cfg), int(p.packed))
     workspace = torch.empty(max(need, 1), dtype=torch.uint8, device=q.device)
     _check(lib, lib.adore_prompt_attention_backward(
         ctypes.byref(p.cfg), *p.starts, p.rows(d_out, p.q_shape, "d_out"), p.rows(q, p.q_shape, "q"), p.rows(k, p.k_shape, "k"),
         p.rows(v, p.k_shape, "v"), p.rows(out, p.q_shape, "out"), None if rest is None else p.rows(rest, p.q_shape, "rest"),
-        p.values(lse, p.q_rows, "lse"), p.rows(dq, p.q_shape, "dq", True), p.rows(dk, p.k_shape, "dk", True),
-        p.rows(dv, p.k_shape, "dv", True), workspace.data_ptr(), need, p.stream))
+        p.values(lse, p.q_rows, "lse"), dq_rows, dk_rows, dv_rows, workspace.data_ptr(), need, p.stream))
     return dq, dk, dv
 
 
@@ -383,7 +404,7 @@ class Q4Cache:
             out = torch.empty_like(q)
         mine, rows = self._mine, self._rows
         ptr = (self._ptr(q, mine, "q"), self._ptr(k, rows, "k"), self._ptr(v, rows, "v"), *self._state, self._ptr(out, mine, "out"))
-        stream = torch.cuda.current_stream(self._index).cuda_stream
+        stream = _stream(self._index)
         if held:
             k_held, v_held = torch.empty_like(k), torch.empty_like(v)
             _check(self.lib, self.lib.adore_q4_step(self._cfg, *ptr, k_held.data_ptr(), v_held.data_ptr(), *self._space, stream))
@@ -404,7 +425,7 @@ class Q4Cache:
         k, v = (torch.empty(shape, dtype=self.dtype, device=self.device) if t is None else self._tensor(t, shape, self.dtype, n)
                 for t, n in ((k, "k"), (v, "v")))
         _check(self.lib, self.lib.adore_q4_read(self._cfg, self._state[0], self._state[1], k.data_ptr(), v.data_ptr(),
-                                                torch.cuda.current_stream(self.device).cuda_stream))
+                                                _stream(self._index)))
         return k, v
 
 

@@ -8,6 +8,9 @@
 // the running maximum and sum of the softmax (fp32).  S^T = K Q^T leaves a query's weights in two lanes, so the maximum is a tree
 // over a lane's registers and one exchange, and P^T is already the right operand of O^T += V^T P^T; V comes out of LDS
 // transposed.  P is rounded to the storage type, like every tensor the matrix cores take; its sum is not.
+// Bound by the matrix unit and the softmax's vector work, which share a SIMD (a tile of 64 keys and 32 queries: 1024 and some 960 cycles at 128
+// elements, 512 and 960 at 64): 2 x 8192 tokens of 32 heads over 4 1010 us (1.09 PFLOP/s; a library product of 8192^3 reaches 1.34),
+// 16 x 1024 of 32 heads 202 us (0.68), 24 packed sequences of 1 to 2777 tokens at 64 elements 243 us (0.72).
 #include <hip/hip_runtime.h>
 
 #include <cmath>
@@ -250,6 +253,8 @@ hipError_t launch_attend_prompt(const AttendArgs<T> &a, hipStream_t st) {
 // ---- the attention every key received -----------------------------------------------------------------------------
 // A workgroup takes 128 keys of a kv head, a wave 32 of them, and goes over the queries that see them, of all heads of the group:
 // S = Q K^T leaves a key's weights in two lanes, which add them up.  No atomics: the order of the sum is fixed.
+// Bound by exponentials and adds (768 cycles of a tile's, next to 512 of the matrix unit): 16 x 1024 tokens of 32 heads 117 us,
+// 3 x 1000 behind 7192, 32 heads over 8, 170 us.
 template <typename T>
 struct ScoreArgs {
   PromptShape s;
