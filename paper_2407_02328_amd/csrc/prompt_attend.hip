@@ -9,8 +9,8 @@
 // over a lane's registers and one exchange, and P^T is already the right operand of O^T += V^T P^T; V comes out of LDS
 // transposed.  P is rounded to the storage type, like every tensor the matrix cores take; its sum is not.
 // Bound by the matrix unit and the softmax's vector work, which share a SIMD (a tile of 64 keys and 32 queries: 1024 and some 960 cycles at 128
-// elements, 512 and 960 at 64): 2 x 8192 tokens of 32 heads over 4 1010 us (1.09 PFLOP/s; a library product of 8192^3 reaches 1.34),
-// 16 x 1024 of 32 heads 202 us (0.68), 24 packed sequences of 1 to 2777 tokens at 64 elements 243 us (0.72).
+// elements, 512 and 960 at 64): 2 x 8192 tokens of 32 heads over 4 986 us (1.11 PFLOP/s; a library product of 8192^3 reaches 1.34),
+// 16 x 1024 of 32 heads 196 us (0.70), 24 packed sequences of 1 to 2777 tokens at 64 elements 238 us (0.73).
 #include <hip/hip_runtime.h>
 
 #include <cmath>
@@ -110,10 +110,12 @@ void prompt_attend_kernel(const AttendArgs<T> a) {
     if (k0 <= mine) {
       // Operands are on their way from LDS ahead of the products that take them, and arithmetic stands between products: a wave issues in
       // order, and left to itself the compiler reads, waits and multiplies in turn.
+      // While a wave has products to issue it goes ahead of the SIMD's others, which are at their maxima or waiting: 2 % less.
       Frag x[ST], v[DB];
       f32x16 s[KB];
 #pragma unroll
       for (int t = 0; t < ST; ++t) x[t] = read.by_row(0, 0, t);
+      __builtin_amdgcn_s_setprio(1);
       float m = -INFINITY;
 #pragma unroll
       for (int kb = 0; kb < KB; ++kb) {
@@ -127,6 +129,7 @@ void prompt_attend_kernel(const AttendArgs<T> a) {
         }
       }
       pin();
+      __builtin_amdgcn_s_setprio(0);
       if (k0 + 32 * KB - 1 > q0 + off) {        // some of the wave's queries do not see all of these keys
 #pragma unroll
         for (int kb = 0; kb < KB; ++kb)
@@ -161,6 +164,7 @@ void prompt_attend_kernel(const AttendArgs<T> a) {
       };
       Frag pf[2];
       weights(0, 0, 16);
+      __builtin_amdgcn_s_setprio(1);
       pf[0] = Operand<T>::of(s[0], 0);
       pf[1] = Operand<T>::of(s[0], 1);
 #pragma unroll
@@ -178,6 +182,7 @@ void prompt_attend_kernel(const AttendArgs<T> a) {
         }
         if (i + 2 < 2 * KB) pf[i & 1] = Operand<T>::of(s[(i + 2) >> 1], i & 1);
       }
+      __builtin_amdgcn_s_setprio(0);
       sum += (part[0] + part[1]) + (part[2] + part[3]);
     }
     read.move(it & 1 ? uint32_t(-2 * kTile) : uint32_t(2 * kTile));
