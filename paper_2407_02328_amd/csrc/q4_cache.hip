@@ -352,7 +352,7 @@ struct StepArgs {
 };
 
 constexpr int kPassHeads = 16;     // heads of a pass
-constexpr int kFinishThreads = 1024, kFinishSlots = 4 * kFinishThreads;   // of a finishing workgroup
+constexpr int kFinishThreads = 1024;   // of a finishing workgroup, each with 1, 2 or 4 slots
 
 // The token's place and position.  Whatever the cursor holds, the slot is one of the row's.
 __device__ __forceinline__ void cursor_of(const int32_t *cursor, int row, int slots, int &slot, int &n) {
@@ -682,9 +682,9 @@ __global__ __launch_bounds__(512) void q4_step_kernel(const StepArgs<T> a) {
   }
 }
 
-// Several workgroups a row: their sums together, and the slots' share of the attention, kFinishSlots to a workgroup.  The last one to
+// Several workgroups a row: their sums together, and the slots' share of the attention, OWN to a thread.  The last one to
 // arrive looks for the smallest key; keys and the counter go past the L2 (agent scope), nothing else is handed over.
-template <typename T, int DH>
+template <typename T, int DH, int OWN>
 __global__ __launch_bounds__(kFinishThreads) void q4_finish_kernel(const StepArgs<T> a, int parts) {
   extern __shared__ __align__(16) float s_dyn[];    // [group][2] maximum and 1 / sum, [group][splits] factor of each workgroup's sums
   __shared__ uint64_t s_key[kFinishThreads / 64];
@@ -695,8 +695,8 @@ __global__ __launch_bounds__(kFinishThreads) void q4_finish_kernel(const StepArg
   int slot, n;
   cursor_of(a.cursor, row, K, slot, n);
   // the slots' part is on its way while the heads' sums are put together
-  constexpr int kOwn = kFinishSlots / kFinishThreads, kEarly = 4;
-  const int first = part * kFinishSlots + tid;
+  constexpr int kOwn = OWN, kEarly = 4;
+  const int first = part * (OWN * kFinishThreads) + tid;
   auto exponent = [&](int i, int j) { return i == slot ? a.part_new[size_t(row) * group + j] : a.logit[(size_t(row) * group + j) * KP + i]; };
   float score[kOwn], early[kOwn][kEarly];
   int at[kOwn];
@@ -801,7 +801,8 @@ int q4_shape(const adore_q4_config *c, Q4Shape *s) {
 // How a step's work is cut.
 struct StepPlan {
   bool wide;
-  int passes, splits, waves, extra, parts;
+  int passes, splits, waves, extra;
+  int own, parts;      // slots of a finishing thread, finishing workgroups of a row
 };
 constexpr int kMaxLds = 128 * 1024;
 int step_lds(const Q4Shape &s, int head_dim, const StepPlan &p) {
@@ -835,7 +836,12 @@ StepPlan plan_step(const Q4Shape &s, int head_dim) {
     p.waves = 4;
     p.splits = 2;
   }
-  p.parts = (s.slots + kFinishSlots - 1) / kFinishSlots;
+  // Finishing workgroups: as many as have a place each, and one a row where that is enough (slots of a thread 1 / 2 / 4: 4 rows of 8000, 16 heads
+  // 23.3 / 26.0 / 31.2 us a step, 16 rows of 4556, 7 heads 18.9 / 20.9 / 24.2; 32 rows of 16384, 4 heads 33.0 / 28.3 / 29.2; 30 of 1335 12.8 / 11.5 / 11.9).
+  p.own = s.slots > 2 * kFinishThreads ? 1 : 2;
+  auto parts_of = [&](int own) { return (s.slots + own * kFinishThreads - 1) / (own * kFinishThreads); };
+  while (p.own < 4 && rows * parts_of(p.own) > 256) p.own *= 2;
+  p.parts = parts_of(p.own);
   return p;
 }
 bool alone(const StepPlan &p) { return p.splits == 1 && p.passes == 1; }
@@ -874,7 +880,14 @@ hipError_t launch_step(const StepArgs<T> &a, const StepPlan &p, hipStream_t st) 
   const unsigned rows = unsigned(a.s.batch) * unsigned(a.s.kv_heads);
   hipLaunchKernelGGL((q4_step_kernel<T, DH, WIDE>), dim3(rows * unsigned(p.splits), unsigned(p.passes)), dim3(64 * (p.waves + p.extra)), lds, st, a);
   if ((e = hipGetLastError()) != hipSuccess || alone(p)) return e;
-  hipLaunchKernelGGL((q4_finish_kernel<T, DH>), dim3(rows * unsigned(p.parts)), dim3(kFinishThreads), a.s.group * (2 + p.splits) * 4, st, a, p.parts);
+  const dim3 grid(rows * unsigned(p.parts)), block(kFinishThreads);
+  const int factors = a.s.group * (2 + p.splits) * 4;
+  if (p.own == 1)
+    hipLaunchKernelGGL((q4_finish_kernel<T, DH, 1>), grid, block, factors, st, a, p.parts);
+  else if (p.own == 2)
+    hipLaunchKernelGGL((q4_finish_kernel<T, DH, 2>), grid, block, factors, st, a, p.parts);
+  else
+    hipLaunchKernelGGL((q4_finish_kernel<T, DH, 4>), grid, block, factors, st, a, p.parts);
   return hipGetLastError();
 }
 
