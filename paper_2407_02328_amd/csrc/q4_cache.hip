@@ -390,8 +390,8 @@ __device__ __forceinline__ void terms_of(float (&x)[8], bf16x8 (&t)[N]) {
   }
 }
 
-// Reads every code once: 16 sequences, 32 heads, 512 slots 13.5 us (one launch, 2.8 TB/s), 4 sequences, 32 heads over 8, 16384 slots 20 us (3.9 TB/s)
-// and 9 for the second launch, one row of 64 slots 5.4 us, which is latency.
+// Reads every code once: 16 sequences, 32 heads, 512 slots 13.5 us (one launch, 2.8 TB/s), 4 sequences, 32 heads over 8, 16384 slots 19 us (4.0 TB/s)
+// and 8 for the second launch, one row of 64 slots 5.4 us, which is latency.
 // Columns of the matrix instructions.  The second product's left operand (V) has no scales in it: they belong to a slot and a group of 32
 // elements, so the weights take them, and every group of elements needs weights of its own.  With few heads (WIDE false: up to
 // 16 / groups) a column is a (head, group): a lane scales its weights once, and of the products with all elements keeps its group's.
