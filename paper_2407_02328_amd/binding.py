@@ -225,6 +225,9 @@ class _Prompts:
         self.packed = packed = q_start is not None
         if len(qs) != (3 if packed else 4) or len(ks) != len(qs):
             raise ValueError("q, k: expected [tokens, heads, head_dim] with starts, [batch, heads, tokens, head_dim] without")
+        # (the kernels go by q's sequences and elements; rows() holds v and the gradients to k's shape)
+        if ks[-1] != qs[-1] or (not packed and ks[0] != qs[0]):
+            raise ValueError(f"k: expected q's {'' if packed else f'{qs[0]} sequences and '}{qs[-1]} elements, got shape {tuple(ks)}")
         if scale is None:
             scale = 0.0
         elif not scale > 0.0:
