@@ -485,10 +485,15 @@ struct TileLoad {
       for (int i = 0; i < N; ++i) to_lds(p, uint32_t(min(row + i * kPer, left - 1)) * pitch + col_of(tid), lds + uint32_t(i * NT * 16));
     }
   }
-  // (m0: nothing else in these kernels uses it.  As a builtin, the compiler would wait for the load ahead of every LDS read.)
+  // (As a builtin, the compiler would wait for the load ahead of every LDS read.  It does not look into the block for what the
+  // hardware wants between a scalar write of m0 and a load that goes by it: one wait state.  m0 is a register that the compiler
+  // never gives out, which it warns of where it is named as overwritten.)
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
   __device__ static __forceinline__ void to_lds(const char *base, uint32_t off, uint32_t lds) {
-    asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(off), "s"(base) : "memory");
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(off), "s"(base) : "memory", "m0");
   }
+#pragma clang diagnostic pop
 };
 __device__ __forceinline__ void arrived() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
 // The wave's transposed result o[db] (row = element 32 db + .., column = row c of 32) to the rows of `to`, through LDS of the wave's
