@@ -11,6 +11,8 @@
 // Bound by the matrix unit: 8 x 2048 tokens of 32 heads over 8, 128 elements: dq 435 us (0.95 PFLOP/s), dk and dv 625 us (0.88).
 #include <hip/hip_runtime.h>
 
+#include <climits>
+
 #include "prompt_device.h"
 
 namespace adore {
@@ -65,6 +67,12 @@ __device__ __forceinline__ void carry_dots(float (&dot)[N], const char *d_out, i
 // ---- dq: 128 queries a workgroup, 32 a wave ----
 template <typename T>
 constexpr int kDqKeys = sizeof(T) == 2 ? 64 : 32;
+// Its LDS: a stage of K and V, and behind it another one or every wave's own 32 rows, for the operands at the beginning and the results at
+// the end; four words.
+template <typename T, int DH, int SW>
+constexpr int kDqStage = 2 * (SW > 1 ? 32 * SW : kDqKeys<T>) * Tile<T, DH>::kRow;
+template <typename T, int DH, int SW>
+constexpr int kDqWords = kDqStage<T, DH, SW> + (kDqStage<T, DH, SW> > 128 * Tile<T, DH>::kRow ? kDqStage<T, DH, SW> : 128 * Tile<T, DH>::kRow);
 
 template <typename T, int DH, int SW>
 __global__ __launch_bounds__(256) ADORE_WAVES(sizeof(T) == 4 || SW > 1 ? 1 : DH == 128 ? 2 : 3) void prompt_dq_kernel(const BackwardArgs<T> a) {
@@ -140,14 +148,14 @@ __global__ __launch_bounds__(256) ADORE_WAVES(sizeof(T) == 4 || SW > 1 ? 1 : DH 
 #pragma unroll
   for (int db = 0; db < DB; ++db) dq[db] = f32x16{0.f};
   const int hidden = max(block * BQ + off + 1, 0) / KT;    // the first tile that not all of the workgroup's queries see all of
-  bool found = false;                                      // ... where an element of K is not finite
+  int from = INT_MAX;                                      // first key of the first such tile where an element of K is not finite
   for (int it = 0; it < tiles; ++it) {
     const int k0 = it * KT + mate.part * 32;
     arrived();
     __syncthreads();
     if (it >= hidden) {
-      found |= make_finite<T, DH, KT, NT>(smem + (it & 1) * 2 * kTile);
-      __syncthreads();
+      const bool found = any_of_four(find_not_finite<T, DH, KT, NT>(smem + (it & 1) * 2 * kTile), reinterpret_cast<int *>(smem + kDqWords<T, DH, SW>));
+      if (__builtin_amdgcn_readfirstlane(found)) from = min(from, it * KT);
     }
     if (it + 1 < tiles) {
       const uint32_t next = share + uint32_t(~it & 1) * uint32_t(2 * kTile);
@@ -156,7 +164,7 @@ __global__ __launch_bounds__(256) ADORE_WAVES(sizeof(T) == 4 || SW > 1 ? 1 : DH 
       lk(kp, sq.nk - (it + 1) * KT, next);
       lv(vp, sq.nk - (it + 1) * KT, next + kTile);
     }
-    if (k0 > mine) {
+    if (k0 > mine || it * KT >= from) {
       read.move(it & 1 ? uint32_t(-2 * kTile) : uint32_t(2 * kTile));
       continue;
     }
@@ -219,10 +227,9 @@ __global__ __launch_bounds__(256) ADORE_WAVES(sizeof(T) == 4 || SW > 1 ? 1 : DH 
     read.move(it & 1 ? uint32_t(-2 * kTile) : uint32_t(2 * kTile));
   }
   __syncthreads();
-  found = any_of_four(found, reinterpret_cast<int *>(smem));
   if constexpr (SW > 1) {
     constexpr int kFloats = 64 * 16 * DB, kPart = Shared<SW>::kRowWaves * kFloats;
-    float *const parts = reinterpret_cast<float *>(smem + 256) + mate.rows * kFloats;
+    float *const parts = reinterpret_cast<float *>(smem) + mate.rows * kFloats;
     if (mate.part > 0) put_sums(dq, parts + (mate.part - 1) * kPart, lane);
     __syncthreads();
     if (mate.part > 0) return;
@@ -230,9 +237,36 @@ __global__ __launch_bounds__(256) ADORE_WAVES(sizeof(T) == 4 || SW > 1 ? 1 : DH 
     for (int i = 0; i < SW - 1; ++i) add_sums(dq, parts + i * kPart, 1.f, lane);
   }
   if (rows <= 0) return;
-  if (found)
-    add_not_finite<T, DH>(dq, reinterpret_cast<const char *>(a.k.p + sq.b * a.k.seq + sq.k_first * a.k.token + hk * a.k.head), a.k.token * es, hidden * KT,
-                          mine + 1, seen, lane);
+  // a lane: its query, half of the elements
+  const int64_t query = row + min(c, rows - 1);
+  const T *const qr = a.q.p + sq.b * a.q.seq + query * a.q.token + head * a.q.head + 4 * h;
+  const T *const dr = a.d_out.p + sq.b * a.d_out.seq + query * a.d_out.token + head * a.d_out.head + 4 * h;
+#pragma unroll 1
+  for (int i = from; i <= mine; ++i) {
+    const int64_t key = int64_t(sq.k_first) + i;
+    const T *const kr = a.k.p + sq.b * a.k.seq + key * a.k.token + hk * a.k.head + 4 * h;
+    const T *const vr = a.v.p + sq.b * a.v.seq + key * a.v.token + hk * a.v.head + 4 * h;
+    float w = 0.f, x = 0.f;
+#pragma unroll 1
+    for (int e = 0; e < DH; e += 8)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        w = fmaf(to_float(qr[e + r]), to_float(kr[e + r]), w);
+        x = fmaf(to_float(dr[e + r]), to_float(vr[e + r]), x);
+      }
+    w = add_lane_xor<32>(w);
+    x = add_lane_xor<32>(x);
+    x = __builtin_amdgcn_exp2f(fmaf(w, scale, -lse)) * (x - delta);
+    if (i <= seen) {
+#pragma unroll
+      for (int db = 0; db < DB; ++db)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          dq[db][r] = fmaf(x, to_float(kr[32 * db + 8 * (r >> 2) + (r & 3)]), dq[db][r]);
+          if (r % 4 == 3) pin();
+        }
+    }
+  }
   store_rows<T, DH>(dq, a.s.scale, own, reinterpret_cast<char *>(a.dq.p + sq.b * a.dq.seq + row * a.dq.token + head * a.dq.head),
                     a.dq.token * es, rows, nullptr, 0, lane);
 }
@@ -477,9 +511,8 @@ __global__ __launch_bounds__(256) ADORE_WAVES(sizeof(T) == 2 && SW == 1 ? 2 : 1)
 
 template <typename T, int DH, int SW>
 hipError_t launch_dq(BackwardArgs<T> a, hipStream_t st) {
-  // a stage, and behind it another one or every wave's own 32 rows, for the operands at the beginning and the results at the end
-  constexpr int row = Tile<T, DH>::kRow, stage = 2 * (SW > 1 ? 32 * SW : kDqKeys<T>) * row, waves = 4 * 32 * row, lds = stage + (stage > waves ? stage : waves);
-  static_assert(SW == 1 || 256 + 4 * (SW - 1) / SW * 256 * (DH / 2) <= stage, "the parts' sums lie in the first stage");
+  constexpr int lds = kDqWords<T, DH, SW> + 16;
+  static_assert(SW == 1 || 4 * (SW - 1) / SW * 256 * (DH / 2) <= kDqStage<T, DH, SW>, "the parts' sums lie in the first stage");
   const hipError_t e = allow_lds(&prompt_dq_kernel<T, DH, SW>, lds);
   if (e != hipSuccess) return e;
   const long long blocks = blocks_at_most(a.s.q_start, a.s.batch, a.s.q_tokens, Shared<SW>::kRows) * a.s.heads;

@@ -314,14 +314,31 @@ struct Reader {
 
 // ---- hidden rows that are not finite ----
 // A weight of 0 hides a row from a matrix product only where the row is finite.  Rows that some of a workgroup's columns see and others do
-// not are all in its few tiles on the diagonal: there infinities and NaN become 0, and when all tiles are done every column takes
-// those that it does see (add_not_finite), from memory.
+// not are all in its few tiles on the diagonal.  Of V, infinities and NaN become 0 there, and when all tiles are done every column takes
+// those that it does see (add_not_finite), from memory.  K makes the weights too, so that a tile of it is left as it is: where any is found
+// (find_not_finite), the keys from there on are gone over one by one.
+
+// 16 bytes, one of whose elements is an infinity or NaN.
+template <typename T>
+__device__ __forceinline__ bool chunk_not_finite(const u32x4 &w) {
+  constexpr uint32_t kSize = sizeof(T) == 2 ? 0x7fff7fffu : 0x7fffffffu;
+  if constexpr (sizeof(T) == 2) {
+    u16x2 most = {0, 0};
+#pragma unroll
+    for (int j = 0; j < 4; ++j) most = __builtin_elementwise_max(most, __builtin_bit_cast(u16x2, w[j] & kSize));
+    return most[0] >= 0x7f80 || most[1] >= 0x7f80;
+  } else {
+    uint32_t most = 0;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) most = max(most, w[j] & kSize);
+    return most >= 0x7f800000u;
+  }
+}
 
 // The workgroup's tile of R rows; whether this wave found any.  Barriers before and behind are the caller's.
 template <typename T, int DH, int R, int NT>
 __device__ __forceinline__ bool make_finite(unsigned char *tile) {
   constexpr int N = R * Tile<T, DH>::kChunks / NT;
-  constexpr uint32_t kSize = sizeof(T) == 2 ? 0x7fff7fffu : 0x7fffffffu;
   static_assert(N * NT == R * Tile<T, DH>::kChunks, "as many chunks for every thread");
   int tid = threadIdx.x;
   asm("" : "+v"(tid));   // (worked out here, not kept in registers)
@@ -330,19 +347,7 @@ __device__ __forceinline__ bool make_finite(unsigned char *tile) {
 #pragma unroll
   for (int i = 0; i < N; ++i) {
     u32x4 w = chunk[i * NT];
-    bool bad;
-    if constexpr (sizeof(T) == 2) {
-      u16x2 most = {0, 0};
-#pragma unroll
-      for (int j = 0; j < 4; ++j) most = __builtin_elementwise_max(most, __builtin_bit_cast(u16x2, w[j] & kSize));
-      bad = most[0] >= 0x7f80 || most[1] >= 0x7f80;
-    } else {
-      uint32_t most = 0;
-#pragma unroll
-      for (int j = 0; j < 4; ++j) most = max(most, w[j] & kSize);
-      bad = most >= 0x7f800000u;
-    }
-    if (bad) {
+    if (chunk_not_finite<T>(w)) {
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         if ((w[j] & 0x7f800000u) == 0x7f800000u) w[j] &= sizeof(T) == 2 ? 0xffffu : 0u;
@@ -352,6 +357,20 @@ __device__ __forceinline__ bool make_finite(unsigned char *tile) {
       found = true;
     }
   }
+  return __builtin_amdgcn_ballot_w64(found) != 0;
+}
+
+// ... only looked at.
+template <typename T, int DH, int R, int NT>
+__device__ __forceinline__ bool find_not_finite(const unsigned char *tile) {
+  constexpr int N = R * Tile<T, DH>::kChunks / NT;
+  static_assert(N * NT == R * Tile<T, DH>::kChunks, "as many chunks for every thread");
+  int tid = threadIdx.x;
+  asm("" : "+v"(tid));
+  const u32x4 *const chunk = reinterpret_cast<const u32x4 *>(tile) + tid;
+  bool found = false;
+#pragma unroll
+  for (int i = 0; i < N; ++i) found |= chunk_not_finite<T>(chunk[i * NT]);
   return __builtin_amdgcn_ballot_w64(found) != 0;
 }
 
@@ -404,7 +423,7 @@ __device__ __forceinline__ void add_sums(f32x16 (&o)[DB], const float *from, flo
     for (int r = 0; r < 16; ++r) o[db][r] = fmaf(from[(16 * db + r) * 64 + lane], factor, o[db][r]);
 }
 
-// Whether it holds in any of the workgroup's four waves; s: four words that nothing else uses from here on.
+// Whether it holds in any of the workgroup's four waves; s: four words that nothing else uses until the next barrier behind this one.
 __device__ __forceinline__ bool any_of_four(bool mine, int *s) {
   if ((threadIdx.x & 63) == 0) s[threadIdx.x >> 6] = mine;
   __syncthreads();
