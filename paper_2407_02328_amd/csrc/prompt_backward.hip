@@ -303,16 +303,20 @@ __global__ __launch_bounds__(256) ADORE_WAVES(sizeof(T) == 2 && SW == 1 ? 2 : 1)
   const int rows = min(32, sq.nk - k0);
   const int64_t row = int64_t(sq.k_first) + k0, es = int64_t(sizeof(T));
   // Queries that some of the block's keys are hidden from, if one of them is not finite, or has no keys (log-sum-exp or delta tells), are
-  // added one by one when the tiles are done.
-  const int diagonal = max(block * BK - off, 0) / QT * QT, behind = min((block * BK + BK - 1 - off + QT - 1) / QT * QT, sq.nq);
+  // added one by one when the tiles are done.  So are those of a last tile that is not full: the rows it lacks repeat the last
+  // query's with weights of 0, which do not hide it where it is not finite.
+  const int diagonal = max(block * BK - off, 0) / QT * QT, behind = min((max(block * BK + BK - 1 - off, 0) + QT - 1) / QT * QT, sq.nq);
+  const int end = sq.nq > behind ? sq.nq / QT * QT : sq.nq;
   bool odd = false;
   for (int j = 0; j < a.s.group; ++j) {
     const size_t row0 = row_value(a.s.q_start != nullptr, sq.b, sq.q_first, a.s.q_tokens, a.s.heads, hk * a.s.group + j);
-    for (int i = diagonal + tid; i < behind; i += NT) odd |= !(subtrahend(a.lse[row0 + i]) < INFINITY && fabsf(a.delta[row0 + i]) < INFINITY);
+    auto look = [&](int i) { odd |= !(subtrahend(a.lse[row0 + i]) < INFINITY && fabsf(a.delta[row0 + i]) < INFINITY); };
+    for (int i = diagonal + tid; i < behind; i += NT) look(i);
+    if (end < sq.nq && tid == NT - 1) look(sq.nq - 1);
   }
   odd = any_of_four(__builtin_amdgcn_ballot_w64(odd) != 0, reinterpret_cast<int *>(s_delta + 2 * QT));
-  const int first = odd ? behind : diagonal;
-  const int per = first < sq.nq ? (sq.nq - first + QT - 1) / QT : 0, tiles = per * a.s.group;
+  const int first = odd ? behind : diagonal, stop = odd ? end : sq.nq;
+  const int per = first < stop ? (stop - first + QT - 1) / QT : 0, tiles = per * a.s.group;
   const float scale = a.s.scale_log2;
   const bool packed = a.s.q_start != nullptr;
   const uint32_t base0 = __builtin_amdgcn_readfirstlane(lds_offset(smem)), share = base0 + uint32_t(wave) * 1024u;
@@ -473,7 +477,7 @@ __global__ __launch_bounds__(256) ADORE_WAVES(sizeof(T) == 2 && SW == 1 ? 2 : 1)
     for (int j = 0; j < a.s.group; ++j) {
       const int head = hk * a.s.group + j;
       const size_t row0 = row_value(packed, sq.b, sq.q_first, a.s.q_tokens, a.s.heads, head);
-      for (int i = diagonal; i < behind; ++i) {
+      for (int i = diagonal < behind ? diagonal : end; i < sq.nq; i = i + 1 == behind ? end : i + 1) {
         const int64_t query = int64_t(sq.q_first) + i;
         const T *qr = a.q.p + sq.b * a.q.seq + query * a.q.token + head * a.q.head + 4 * h;
         const T *dr = a.d_out.p + sq.b * a.d_out.seq + query * a.d_out.token + head * a.d_out.head + 4 * h;
