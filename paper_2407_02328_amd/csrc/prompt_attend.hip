@@ -13,6 +13,7 @@
 // 16 x 1024 of 32 heads 196 us (0.70), 24 packed sequences of 1 to 2777 tokens at 64 elements 238 us (0.73).
 #include <hip/hip_runtime.h>
 
+#include <cfloat>
 #include <cmath>
 
 #include "prompt_device.h"
@@ -89,7 +90,7 @@ void prompt_attend_kernel(const AttendArgs<T> a) {
 #pragma unroll
   for (int db = 0; db < DB; ++db) o[db] = f32x16{0.f};
   float top = -INFINITY, sum = 0.f;             // of the lane's query: running maximum of the products, sum of its share of the keys
-  const float slack = 8.f / scale;
+  const float slack = fminf(8.f / scale, FLT_MAX);    // (finite: ahead of the first keys, top + slack has to be less than any product)
   const int hidden = max(block * BQ + off + 1, 0) / KT;               // the first tile that not all of the workgroup's queries see all of
   bool found = false;                           // ... where a value is not finite
   for (int it = 0; it < tiles; ++it) {
