@@ -352,8 +352,8 @@ int adore_topk_attention_static(const void *q, const void *k, const void *v, voi
  * Calls only enqueue work on hip_stream (a hipStream_t, NULL = the default stream).
  * Errors of all: E_INVALID (null, sizes, kv_heads that do not divide heads, a scale that is negative or not finite, one of
  * the two starts alone, rows not on 16-byte boundaries, a negative stride or a token stride beyond 2^22 elements),
- * E_UNSUPPORTED (head_dim not in {64,128}, more than 2^24 tokens, 4096 heads, 65536 sequences, or 2^24 blocks of 32
- * tokens x heads), E_HIP. */
+ * E_UNSUPPORTED (head_dim not in {64,128}, more than 2^24 tokens, 4096 heads or 65536 sequences, 2^24 blocks of 32
+ * tokens x heads or more), E_HIP. */
 typedef struct {
   int32_t batch, heads, kv_heads, head_dim;
   int32_t q_tokens, k_tokens; /* rows of the packed tensors, or tokens of every sequence */

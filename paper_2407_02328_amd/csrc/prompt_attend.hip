@@ -468,7 +468,8 @@ int prompt_shape(const adore_prompt_config *c, const int32_t *q_start, const int
   constexpr int kMostTokens = 1 << 24, kMostHeads = 1 << 12, kMostBatch = 1 << 16;
   if (c->q_tokens > kMostTokens || c->k_tokens > kMostTokens || c->heads > kMostHeads || c->batch > kMostBatch) return ADORE_E_UNSUPPORTED;
   const long long rows = c->q_tokens > c->k_tokens ? c->q_tokens : c->k_tokens;
-  if (blocks_at_most(q_start, c->batch, int(rows), 32) * c->heads > (1ll << 24)) return ADORE_E_UNSUPPORTED;
+  // fewer than 2^32 threads, 256 a workgroup (with 32 tokens or fewer per sequence there are as many workgroups of 128 as of 32)
+  if (blocks_at_most(q_start, c->batch, int(rows), 32) * c->heads >= (1ll << 24)) return ADORE_E_UNSUPPORTED;
   s->q_start = q_start;
   s->k_start = k_start;
   s->batch = c->batch;
