@@ -342,8 +342,9 @@ int adore_topk_attention_static(const void *q, const void *k, const void *v, voi
  *   received_j = the sum of exp(w_ij - lse_i) over the queries of all heads of j's group
  * Sequences: with q_start and k_start (both [batch + 1] i32, DEVICE) packed ones, of any lengths from 0 on: the tokens
  * of sequence b are rows q_start[b] .. q_start[b + 1] - 1 of the q_tokens rows of q, d_out, out, dq (k_start: of the k_tokens
- * rows of k, v, dk, dv); starts that do not rise or leave the tensor are cut off at its ends.  Outputs at rows
- * behind the last sequence are set to zero (lse to -inf), so that a buffer may be longer than its sequences together.  Without (both NULL): `batch` sequences of q_tokens queries and k_tokens keys each.
+ * rows of k, v, dk, dv); starts that do not rise or leave the tensor are cut off at its ends.  Outputs at rows in front of the first
+ * sequence and behind the last one are set to zero (lse to -inf), so that a buffer may be longer than its sequences together.  Without
+ * starts (both NULL): `batch` sequences of q_tokens queries and k_tokens keys each.
  * lse: fp32 [heads][q_tokens] packed, [batch][heads][q_tokens] without starts; scores alike with kv_heads and k_tokens,
  * which for a dense batch is the layout that adore_init_cache takes as score_override in H2O mode.
  * Products are accumulated in fp32, softmax statistics are fp32, weights and their gradients are rounded to the storage

@@ -54,11 +54,10 @@ void prompt_attend_kernel(const AttendArgs<T> a) {
   Sequence sq;
   int block;
   if (!find_block<BQ, true>(a.s, item / a.s.group, a.by_work, sq, block)) {
-    int first;
-    const int n = tail_rows<BQ>(a.s.q_start, a.s.batch, a.s.q_tokens, block, first);
-    zero_rows<T, DH>(a.out, head, first, n, tid, NT);
-    if (REST) zero_rows<T, DH>(a.rest, head, first, n, tid, NT);
-    if (a.lse && tid < n) a.lse[size_t(head) * a.s.q_tokens + first + tid] = -INFINITY;
+    const SpareRows spare = spare_rows<BQ>(a.s.q_start, a.s.batch, a.s.q_tokens, block);
+    zero_rows<T, DH>(a.out, head, spare, tid, NT);
+    if (REST) zero_rows<T, DH>(a.rest, head, spare, tid, NT);
+    if (a.lse && tid < spare.n) a.lse[size_t(head) * a.s.q_tokens + spare.at(tid)] = -INFINITY;
     return;
   }
   const Shared<SW> mate(wave);
@@ -286,9 +285,8 @@ __global__ __launch_bounds__(256) void prompt_scores_kernel(const ScoreArgs<T> a
   Sequence sq;
   int block;
   if (!find_block<BK, false>(a.s, blockIdx.x / a.s.kv_heads, a.by_work, sq, block)) {
-    int first;
-    const int n = tail_rows<BK>(a.s.k_start, a.s.batch, a.s.k_tokens, block, first);
-    if (tid < n) a.scores[size_t(hk) * a.s.k_tokens + first + tid] = 0.f;
+    const SpareRows spare = spare_rows<BK>(a.s.k_start, a.s.batch, a.s.k_tokens, block);
+    if (tid < spare.n) a.scores[size_t(hk) * a.s.k_tokens + spare.at(tid)] = 0.f;
     return;
   }
   const Shared<SW> mate(wave);

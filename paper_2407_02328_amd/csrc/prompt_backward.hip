@@ -86,9 +86,8 @@ __global__ __launch_bounds__(256) ADORE_WAVES(sizeof(T) == 4 || SW > 1 ? 1 : DH 
   Sequence sq;
   int block;
   if (!find_block<BQ, true>(a.s, item / a.s.group, a.by_work, sq, block)) {
-    int first;
-    const int n = tail_rows<BQ>(a.s.q_start, a.s.batch, a.s.q_tokens, block, first);
-    zero_rows<T, DH>(a.dq, head, first, n, tid, NT);
+    const SpareRows spare = spare_rows<BQ>(a.s.q_start, a.s.batch, a.s.q_tokens, block);
+    zero_rows<T, DH>(a.dq, head, spare, tid, NT);
     return;
   }
   const Shared<SW> mate(wave);
@@ -292,10 +291,9 @@ __global__ __launch_bounds__(256) ADORE_WAVES(sizeof(T) == 2 && SW == 1 ? 2 : 1)
   Sequence sq;
   int block;
   if (!find_block<BK, false>(a.s, blockIdx.x / a.s.kv_heads, a.by_work, sq, block)) {
-    int first;
-    const int n = tail_rows<BK>(a.s.k_start, a.s.batch, a.s.k_tokens, block, first);
-    zero_rows<T, DH>(a.dk, hk, first, n, tid, NT);
-    zero_rows<T, DH>(a.dv, hk, first, n, tid, NT);
+    const SpareRows spare = spare_rows<BK>(a.s.k_start, a.s.batch, a.s.k_tokens, block);
+    zero_rows<T, DH>(a.dk, hk, spare, tid, NT);
+    zero_rows<T, DH>(a.dv, hk, spare, tid, NT);
     return;
   }
   const Shared<SW> mate(wave);

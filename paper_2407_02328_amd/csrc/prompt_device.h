@@ -75,7 +75,7 @@ __device__ __forceinline__ Sequence sequence_at(const PromptShape &a, int b) {
   return s;
 }
 
-// Blocks of `rows` rows that sequences have together, at most (a grid does not know the starts), and the rows behind the last sequence.
+// Blocks of `rows` rows that sequences have together, at most (a grid does not know the starts), and the rows that belong to none.
 inline long long blocks_at_most(const int32_t *start, int batch, int tokens, int rows) {
   return start ? (long long)tokens / rows + batch + 1 : (long long)batch * ((tokens + rows - 1) / rows);
 }
@@ -83,7 +83,7 @@ inline long long blocks_at_most(const int32_t *start, int batch, int tokens, int
 // Block `item` of the sequences' blocks of ROWS rows of q (whose work grows with their index: they see all keys before them) or of k
 // (whose work falls).  The order: one sequence behind the other, each with its longest block first, so that what
 // one sequence's workgroups share stays in the L2; by_work: the longest of all sequences first, so that a launch of few workgroups
-// ends with short ones.  False: there is no such block, and `block` is how far behind the last one (tail_rows).  All 64 lanes of a wave
+// ends with short ones.  False: there is no such block, and `block` is how far behind the last one (spare_rows).  All 64 lanes of a wave
 // call it together.
 template <int ROWS, bool OF_Q>
 __device__ __forceinline__ bool find_block(const PromptShape &a, int item, bool by_work, Sequence &s, int &block) {
@@ -142,19 +142,31 @@ __device__ __forceinline__ bool find_block(const PromptShape &a, int item, bool 
   return false;
 }
 
-// Rows behind the last sequence that the workgroup of a block beyond the sequences' own sees to (it sets what is written there to zero).
+// Rows of packed tensors that belong to no sequence: those behind the last one, then those in front of the first.  The workgroup of a
+// block beyond the sequences' own sees to ROWS of them, at(0) .. at(n - 1) (it sets what is written there to zero).
+struct SpareRows {
+  int end, behind, first, n;
+  __device__ __forceinline__ int at(int i) const {
+    const int r = first + i;
+    return r < behind ? end + r : r - behind;
+  }
+};
 template <int ROWS>
-__device__ __forceinline__ int tail_rows(const int32_t *start, int batch, int tokens, int block, int &first) {
-  const int64_t at = min(max(start[batch], 0), tokens) + int64_t(block) * ROWS;
-  first = int(min(at, int64_t(tokens)));
-  return min(ROWS, tokens - first);
+__device__ __forceinline__ SpareRows spare_rows(const int32_t *start, int batch, int tokens, int block) {
+  SpareRows r;
+  r.end = min(max(start[batch], 0), tokens);
+  r.behind = tokens - r.end;
+  const int all = r.behind + min(max(start[0], 0), r.end);
+  r.first = int(min(int64_t(block) * ROWS, int64_t(all)));
+  r.n = min(ROWS, all - r.first);
+  return r;
 }
 
 template <typename T, int DH>
-__device__ __forceinline__ void zero_rows(const Rows<T> &to, int head, int first, int n, int tid, int threads) {
+__device__ __forceinline__ void zero_rows(const Rows<T> &to, int head, const SpareRows &spare, int tid, int threads) {
   constexpr int kChunks = DH * int(sizeof(T)) / 16;
-  for (int i = tid; i < n * kChunks; i += threads)
-    *reinterpret_cast<u32x4 *>(reinterpret_cast<char *>(to.p + int64_t(first + i / kChunks) * to.token + head * to.head) + i % kChunks * 16) =
+  for (int i = tid; i < spare.n * kChunks; i += threads)
+    *reinterpret_cast<u32x4 *>(reinterpret_cast<char *>(to.p + int64_t(spare.at(i / kChunks)) * to.token + head * to.head) + i % kChunks * 16) =
         u32x4{0, 0, 0, 0};
 }
 
