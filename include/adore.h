@@ -350,7 +350,8 @@ int adore_topk_attention_static(const void *q, const void *k, const void *v, voi
  * Products are accumulated in fp32, softmax statistics are fp32, weights and their gradients are rounded to the storage
  * type where they enter a product; outputs are rounded once.  A row reaches what sees it and nothing else, infinities and NaN too
  * (later keys and values no earlier query, earlier queries no later key's gradients or scores).  No atomics: equal inputs give equal bits.
- * Calls only enqueue work on hip_stream (a hipStream_t, NULL = the default stream).
+ * Calls only enqueue work on hip_stream (a hipStream_t, NULL = the default stream), on the current device, which has to be the
+ * buffers' (here and in the calls on a 4-bit cache).
  * Errors of all: E_INVALID (null, sizes, kv_heads that do not divide heads, a scale that is negative or not finite, one of
  * the two starts alone, rows not on 16-byte boundaries, a negative stride or a token stride beyond 2^22 elements),
  * E_UNSUPPORTED (head_dim not in {64,128}, more than 2^24 tokens, 4096 heads or 65536 sequences, 2^24 blocks of 32

@@ -203,6 +203,18 @@ _CODES = {torch.float32: ADORE_F32, torch.bfloat16: ADORE_BF16}
 
 # torch's current stream of a device as a number (torch.cuda.current_stream makes an object of it, 2 us)
 _stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda index: torch.cuda.current_stream(index).cuda_stream)
+# ... and the current device as one (torch.cuda.current_device looks first whether torch is initialised; who has a GPU tensor knows)
+_current = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+
+
+def _call(lib, index: int, function, *args):
+    """A call of the library whose kernels go to the current device, which has to be that of its tensors."""
+    if _current() == index:
+        rc = function(*args)
+    else:
+        with torch.cuda.device(index):
+            rc = function(*args)
+    _check(lib, rc)
 
 
 class _Prompts:
@@ -299,9 +311,9 @@ def prompt_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, *, q_sta
         rows = p.fresh(out)
     lse = torch.empty(p.q_rows, dtype=torch.float32, device=p.device)
     left = torch.empty(p.q_shape, dtype=q.dtype, device=p.device) if rest and q.dtype == torch.bfloat16 else None
-    _check(lib, lib.adore_prompt_attention(ctypes.byref(p.cfg), *p.starts, p.rows(q, p.q_shape, "q"), p.rows(k, p.k_shape, "k"),
-                                           p.rows(v, p.k_shape, "v"), rows or p.rows(out, p.q_shape, "out", True), lse.data_ptr() or 16,
-                                           None if left is None else p.fresh(left), p.stream))
+    _call(lib, p.index, lib.adore_prompt_attention, ctypes.byref(p.cfg), *p.starts, p.rows(q, p.q_shape, "q"), p.rows(k, p.k_shape, "k"),
+          p.rows(v, p.k_shape, "v"), rows or p.rows(out, p.q_shape, "out", True), lse.data_ptr() or 16, None if left is None else p.fresh(left),
+          p.stream)
     return (out, lse, left) if rest else (out, lse)
 
 
@@ -323,10 +335,10 @@ def prompt_attention_backward(d_out: torch.Tensor, q: torch.Tensor, k: torch.Ten
     (dq, dq_rows), (dk, dk_rows), (dv, dv_rows) = gradient(dq, p.q_shape, "dq"), gradient(dk, p.k_shape, "dk"), gradient(dv, p.k_shape, "dv")
     need = lib.adore_prompt_backward_workspace_bytes(ctypes.byref(p.cfg), int(p.packed))
     workspace = torch.empty(max(need, 1), dtype=torch.uint8, device=q.device)
-    _check(lib, lib.adore_prompt_attention_backward(
-        ctypes.byref(p.cfg), *p.starts, p.rows(d_out, p.q_shape, "d_out"), p.rows(q, p.q_shape, "q"), p.rows(k, p.k_shape, "k"),
-        p.rows(v, p.k_shape, "v"), p.rows(out, p.q_shape, "out"), None if rest is None else p.rows(rest, p.q_shape, "rest"),
-        p.values(lse, p.q_rows, "lse"), dq_rows, dk_rows, dv_rows, workspace.data_ptr(), need, p.stream))
+    _call(lib, p.index, lib.adore_prompt_attention_backward, ctypes.byref(p.cfg), *p.starts, p.rows(d_out, p.q_shape, "d_out"),
+          p.rows(q, p.q_shape, "q"), p.rows(k, p.k_shape, "k"), p.rows(v, p.k_shape, "v"), p.rows(out, p.q_shape, "out"),
+          None if rest is None else p.rows(rest, p.q_shape, "rest"), p.values(lse, p.q_rows, "lse"), dq_rows, dk_rows, dv_rows,
+          workspace.data_ptr(), need, p.stream)
     return dq, dk, dv
 
 
@@ -338,8 +350,8 @@ def prompt_scores(q: torch.Tensor, k: torch.Tensor, lse: torch.Tensor, *, q_star
     p = _Prompts(q, k, q_start, k_start, scale)
     if scores is None:
         scores = torch.empty(p.k_rows, dtype=torch.float32, device=q.device)
-    _check(lib, lib.adore_prompt_scores(ctypes.byref(p.cfg), *p.starts, p.rows(q, p.q_shape, "q"), p.rows(k, p.k_shape, "k"),
-                                        p.values(lse, p.q_rows, "lse"), p.values(scores, p.k_rows, "scores"), p.stream))
+    _call(lib, p.index, lib.adore_prompt_scores, ctypes.byref(p.cfg), *p.starts, p.rows(q, p.q_shape, "q"), p.rows(k, p.k_shape, "k"),
+          p.values(lse, p.q_rows, "lse"), p.values(scores, p.k_rows, "scores"), p.stream)
     return scores
 
 
@@ -397,8 +409,8 @@ class Q4Cache:
         p = _Prompts(k, k, k_start, k_start, None)
         if p.device != self.device or p.dtype != self.dtype or (p.batch, p.cfg.kv_heads, p.cfg.head_dim) != (c.batch, c.kv_heads, c.head_dim):
             raise ValueError(f"k: expected {self.dtype} rows of {c.batch} sequences, {c.kv_heads} heads, {c.head_dim} elements on {self.device}")
-        _check(self.lib, self.lib.adore_q4_fill(self._cfg, p.starts[1], p.cfg.k_tokens, p.rows(k, p.k_shape, "k"), p.rows(v, p.k_shape, "v"),
-                                                None if scores is None else p.values(scores, p.k_rows, "scores"), *self._state, p.stream))
+        _call(self.lib, self._index, self.lib.adore_q4_fill, self._cfg, p.starts[1], p.cfg.k_tokens, p.rows(k, p.k_shape, "k"),
+              p.rows(v, p.k_shape, "v"), None if scores is None else p.values(scores, p.k_rows, "scores"), *self._state, p.stream)
 
     def step(self, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, *, out: torch.Tensor = None, held: bool = False):
         """One token of every sequence: q [batch, heads, head_dim], k and v [batch, kv_heads, head_dim], contiguous.  Returns out
@@ -410,9 +422,9 @@ class Q4Cache:
         stream = _stream(self._index)
         if held:
             k_held, v_held = torch.empty_like(k), torch.empty_like(v)
-            _check(self.lib, self.lib.adore_q4_step(self._cfg, *ptr, k_held.data_ptr(), v_held.data_ptr(), *self._space, stream))
+            _call(self.lib, self._index, self.lib.adore_q4_step, self._cfg, *ptr, k_held.data_ptr(), v_held.data_ptr(), *self._space, stream)
             return out, k_held, v_held
-        _check(self.lib, self.lib.adore_q4_step(self._cfg, *ptr, None, None, *self._space, stream))
+        _call(self.lib, self._index, self.lib.adore_q4_step, self._cfg, *ptr, None, None, *self._space, stream)
         return out
 
     def _ptr(self, t, shape, name):
@@ -427,8 +439,8 @@ class Q4Cache:
         shape = (c.batch, c.kv_heads, c.slots, c.head_dim)
         k, v = (torch.empty(shape, dtype=self.dtype, device=self.device) if t is None else self._tensor(t, shape, self.dtype, n)
                 for t, n in ((k, "k"), (v, "v")))
-        _check(self.lib, self.lib.adore_q4_read(self._cfg, self._state[0], self._state[1], k.data_ptr(), v.data_ptr(),
-                                                _stream(self._index)))
+        _call(self.lib, self._index, self.lib.adore_q4_read, self._cfg, self._state[0], self._state[1], k.data_ptr(), v.data_ptr(),
+              _stream(self._index))
         return k, v
 
 
