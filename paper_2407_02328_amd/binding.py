@@ -380,6 +380,7 @@ class Q4Cache:
         self.device = torch.device(device) if cache is None else cache.device
         rows = (batch, kv_heads)
         self.cache = self._buffer(cache, rows + ((slots + 63) // 64, 68 * head_dim), torch.uint8, 0, "cache", 256)
+        self.device = self.cache.device        # (with its number)
         self.slot_pos = self._buffer(slot_pos, rows + (slots,), torch.int32, -1, "slot_pos", 16)
         self.score = self._buffer(score, rows + (slots,), torch.float32, 0, "score", 16)
         self.cursor = self._buffer(cursor, rows + (2,), torch.int32, 0, "cursor", 8)
