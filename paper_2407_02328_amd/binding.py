@@ -302,7 +302,20 @@ def prompt_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, *, q_sta
 
     Packed sequences: q [q tokens, heads, head_dim], k and v [k tokens, kv heads, head_dim], q_start and k_start int32
     [batch + 1] on the GPU.  A dense batch: [batch, heads, tokens, head_dim] without starts.  bf16 or fp32, any strides with a
-    dense last dimension (q, k and v may be views of one projection).  out is allocated here unless given."""
+    dense last dimension (q, k and v may be views of one projection).  out is allocated here unless given.
+
+    Where q, k or v require gradients, out has them: torch's backward pass is prompt_attention_backward (once; lse and rest have
+    none, and out cannot be given then).  A step that is captured into a graph calls the two itself, under torch.no_grad()."""
+    if torch.is_grad_enabled() and (q.requires_grad or k.requires_grad or (isinstance(v, torch.Tensor) and v.requires_grad)):
+        if out is not None:
+            raise ValueError("out: cannot be given where gradients are required (call under torch.no_grad())")
+        got = _PromptAttention.apply(q, k, v, q_start, k_start, scale, rest)
+    else:
+        got = _attend_prompts(q, k, v, q_start, k_start, scale, out, rest)
+    return got if rest else got[:2]
+
+
+def _attend_prompts(q, k, v, q_start, k_start, scale, out, rest):
     lib = load_library()
     p = _Prompts(q, k, q_start, k_start, scale)
     rows = None
@@ -314,7 +327,30 @@ def prompt_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, *, q_sta
     _call(lib, p.index, lib.adore_prompt_attention, ctypes.byref(p.cfg), *p.starts, p.rows(q, p.q_shape, "q"), p.rows(k, p.k_shape, "k"),
           p.rows(v, p.k_shape, "v"), rows or p.rows(out, p.q_shape, "out", True), lse.data_ptr() or 16, None if left is None else p.fresh(left),
           p.stream)
-    return (out, lse, left) if rest else (out, lse)
+    return out, lse, left
+
+
+class _PromptAttention(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, q, k, v, q_start, k_start, scale, rest):
+        out, lse, left = _attend_prompts(q, k, v, q_start, k_start, scale, None, rest)
+        ctx.save_for_backward(q, k, v, out, lse, left, q_start, k_start)
+        ctx.scale = scale
+        ctx.mark_non_differentiable(*(x for x in (lse, left) if x is not None))
+        ctx.set_materialize_grads(False)
+        return out, lse, left
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, d_out, *_):
+        if d_out is None:
+            return (None,) * 7
+        q, k, v, out, lse, left, q_start, k_start = ctx.saved_tensors
+        # (whatever made d_out chose its layout: of a sum, one element for all)
+        if d_out.stride(-1) != 1 or d_out.data_ptr() % 16 or any(s * d_out.element_size() % 16 for s in d_out.stride()[:-1]):
+            d_out = d_out.clone(memory_format=torch.contiguous_format)
+        grads = prompt_attention_backward(d_out, q, k, v, out, lse, rest=left, q_start=q_start, k_start=k_start, scale=ctx.scale)
+        return *(g if want else None for g, want in zip(grads, ctx.needs_input_grad)), None, None, None, None
 
 
 def prompt_attention_backward(d_out: torch.Tensor, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, out: torch.Tensor,
@@ -345,7 +381,8 @@ def prompt_attention_backward(d_out: torch.Tensor, q: torch.Tensor, k: torch.Ten
 def prompt_scores(q: torch.Tensor, k: torch.Tensor, lse: torch.Tensor, *, q_start: torch.Tensor = None, k_start: torch.Tensor = None,
                   scale: float = None, scores: torch.Tensor = None) -> torch.Tensor:
     """adore_prompt_scores on torch's current stream: the attention every key received from the queries of its group's heads, fp32
-    [kv heads, k tokens] (packed) or [batch, kv heads, tokens].  lse as prompt_attention returned it."""
+    [kv heads, k tokens] (packed) or [batch, kv heads, tokens].  lse as prompt_attention returned it.  They carry no gradients: what
+    goes by them is a choice."""
     lib = load_library()
     p = _Prompts(q, k, q_start, k_start, scale)
     if scores is None:
