@@ -300,11 +300,13 @@ __global__ __launch_bounds__(256) ADORE_WAVES(sizeof(T) == 2 && SW == 1 ? 2 : 1)
   const int k0 = block * BK + mate.rows * 32, off = sq.nk - sq.nq;
   const int rows = min(32, sq.nk - k0);
   const int64_t row = int64_t(sq.k_first) + k0, es = int64_t(sizeof(T));
-  // Queries that some of the block's keys are hidden from, if one of them is not finite, or has no keys (log-sum-exp or delta tells), are
-  // added one by one when the tiles are done.  So are those of a last tile that is not full: the rows it lacks repeat the last
-  // query's with weights of 0, which do not hide it where it is not finite.
-  const int diagonal = max(block * BK - off, 0) / QT * QT, behind = min((max(block * BK + BK - 1 - off, 0) + QT - 1) / QT * QT, sq.nq);
-  const int end = sq.nq > behind ? sq.nq / QT * QT : sq.nq;
+  // Tiles of queries begin with the first that sees a key: those before it have no gradient to give, and may hold anything.
+  // Queries that some of the block's keys are hidden from, if one of them is not finite, or its weights are not numbers (log-sum-exp or
+  // delta tells), are added one by one when the tiles are done.  So are those of a last tile that is not full: the rows it lacks repeat
+  // the last query's with weights of 0, which do not hide it where it is not finite.
+  const int base = max(-off, 0), unseen = block * BK - off - base;       // (of the block's first key, from base on)
+  const int diagonal = base + max(unseen, 0) / QT * QT, behind = min(base + (max(unseen + BK - 1, 0) + QT - 1) / QT * QT, sq.nq);
+  const int end = sq.nq > behind ? base + (sq.nq - base) / QT * QT : sq.nq;
   bool odd = false;
   for (int j = 0; j < a.s.group; ++j) {
     const size_t row0 = row_value(a.s.q_start != nullptr, sq.b, sq.q_first, a.s.q_tokens, a.s.heads, hk * a.s.group + j);
