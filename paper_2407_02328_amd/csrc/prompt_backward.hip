@@ -140,6 +140,7 @@ __global__ __launch_bounds__(256) ADORE_WAVES(sizeof(T) == 4 || SW > 1 ? 1 : DH 
       if (c < rows) {
         delta = s_delta[c];
         if (h == 0 && mate.part == 0) a.delta[at + c] = delta;    // for dk and dv
+        if (seen < 0) delta = 0.f;                                // (sees no key: weights of 0, whatever dO holds)
       }
     }
   }
