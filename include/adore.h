@@ -349,7 +349,9 @@ int adore_topk_attention_static(const void *q, const void *k, const void *v, voi
  * which for a dense batch is the layout that adore_init_cache takes as score_override in H2O mode.
  * Products are accumulated in fp32, softmax statistics are fp32, weights and their gradients are rounded to the storage
  * type where they enter a product; outputs are rounded once.  A row reaches what sees it and nothing else, infinities and NaN too
- * (later keys and values no earlier query, earlier queries no later key's gradients or scores).  No atomics: equal inputs give equal bits.
+ * (later keys and values no earlier query, earlier queries no later key's gradients or scores); what the definition makes infinite
+ * may come out as NaN.  A product of minus infinity has weight 0 (a row that has no other: out 0, lse -inf), one of plus infinity makes
+ * its row NaN, lse too.  No atomics: equal inputs give equal bits.
  * Calls only enqueue work on hip_stream (a hipStream_t, NULL = the default stream), on the current device, which has to be the
  * buffers' (here and in the calls on a 4-bit cache).
  * Errors of all: E_INVALID (null, sizes, kv_heads that do not divide heads, a scale that is negative or not finite, one of

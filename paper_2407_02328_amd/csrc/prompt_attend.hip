@@ -9,8 +9,9 @@
 // over a lane's registers and one exchange, and P^T is already the right operand of O^T += V^T P^T; V comes out of LDS
 // transposed.  P is rounded to the storage type, like every tensor the matrix cores take; its sum is not.
 // Bound by the matrix unit and the softmax's vector work, which share a SIMD (a tile of 64 keys and 32 queries: 1024 and some 960 cycles at 128
-// elements, 512 and 960 at 64): 2 x 8192 tokens of 32 heads over 4 986 us (1.11 PFLOP/s; a library product of 8192^3 reaches 1.34),
-// 16 x 1024 of 32 heads 196 us (0.70), 24 packed sequences of 1 to 2777 tokens at 64 elements 238 us (0.73).
+// elements, 512 and 960 at 64): 2 x 8192 tokens of 32 heads over 4 965 us (1.14 PFLOP/s; a library product of 8192^3 reaches 1.34),
+// 16 x 1024 of 32 heads 193 us (0.71), 24 packed sequences of 1 to 2777 tokens at 64 elements 237 us (0.74).  The matrix unit is busy
+// 61, 35 and 37 % of these kernels' cycles, vector instructions 57, 45 and 71 %.
 #include <hip/hip_runtime.h>
 
 #include <cfloat>
@@ -258,8 +259,10 @@ hipError_t launch_attend_prompt(const AttendArgs<T> &a, hipStream_t st) {
 // ---- the attention every key received -----------------------------------------------------------------------------
 // A workgroup takes 128 keys of a kv head, a wave 32 of them, and goes over the queries that see them, of all heads of the group:
 // S = Q K^T leaves a key's weights in two lanes, which add them up.  No atomics: the order of the sum is fixed.
-// Bound by exponentials and adds (768 cycles of a tile's, next to 512 of the matrix unit): 16 x 1024 tokens of 32 heads 117 us,
-// 3 x 1000 behind 7192, 32 heads over 8, 170 us.
+// 16 x 1024 tokens of 32 heads 118 us, 3 x 1000 behind 7192, 32 heads over 8, 169 us: vector instructions take 54 and 57 % of the cycles
+// and the matrix unit 29 and 36 %, mostly one after the other.  A tile's exponentials are written between the products of its next block,
+// but the branch of hide() lets the compiler move them behind the last product, and results lie in accumulation registers, out of
+// which they are moved first.
 template <typename T>
 struct ScoreArgs {
   PromptShape s;
@@ -376,7 +379,7 @@ __global__ __launch_bounds__(256) void prompt_scores_kernel(const ScoreArgs<T> a
         pin();
         s[qb] = Operand<T>::mma(x[t], kf[t], s[qb]);
         if (qb + 1 < QB) x[t] = read.by_row(0, qb * 32 + 32, t);
-        if (qb > 0 && t % (ST / 4) == ST / 4 - 1) weights(qb - 1, t / (ST / 4));   // the block before under this one's products
+        if (qb > 0 && t % (ST / 4) == ST / 4 - 1) weights(qb - 1, t / (ST / 4));   // the block before (see above for where it ends up)
       }
       pin();
       hide(qb);

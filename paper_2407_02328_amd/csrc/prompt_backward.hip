@@ -8,7 +8,9 @@
 // in both (seven products instead of the five that one pass would need, which would have to add dq up in memory).
 // delta wants out as it was before P and it were rounded: from the rounded one a short row's gradients are up to 2.2 times as far off as
 // their own rounding, so the forward can take P in two terms and hand out what rounding left (rest): 1.4 times.
-// Bound by the matrix unit: 8 x 2048 tokens of 32 heads over 8, 128 elements: dq 435 us (0.95 PFLOP/s), dk and dv 625 us (0.88).
+// 8 x 2048 tokens of 32 heads over 8, 128 elements: dq 441 us (0.94 PFLOP/s), dk and dv 606 us (0.91).  The matrix unit is busy 46 and
+// 43 % of the cycles, vector instructions take 42 and 28 %, LDS 26 and 33 %: nothing bounds alone.  A wave's operands, products and
+// arithmetic wait for one another, and the registers leave two waves a SIMD to fill in.
 #include <hip/hip_runtime.h>
 
 #include <climits>
