@@ -395,6 +395,71 @@ int adore_prompt_attention_backward(const adore_prompt_config *cfg, const int32_
 int adore_prompt_scores(const adore_prompt_config *cfg, const int32_t *q_start, const int32_t *k_start,
                         const adore_rows *q, const adore_rows *k, const float *lse, float *scores, void *hip_stream);
 
+/* ---- Attention with a window and first tokens that stay visible (Sec. 3.1, baselines 2 and 5) ----
+ * adore_prompt_attention and its gradients for queries that see less: the query at position p = i + nk - nq sees keys
+ *   j <= p with p - j < window or j < sinks
+ * (itself among them; a window that no sequence exceeds is plain causal attention).  Everything else as above, what hidden rows may hold
+ * too; tiles that no query of a block sees are not read.  adore_ring_step (below) is the same for single tokens.
+ * Errors also: E_INVALID (window null or < 1, sinks < 0). */
+typedef struct {
+  int32_t window; /* >= 1: keys up to the query's own */
+  int32_t sinks;  /* >= 0: first keys of the sequence */
+} adore_window;
+int adore_window_attention(const adore_prompt_config *cfg, const adore_window *window, const int32_t *q_start,
+                           const int32_t *k_start, const adore_rows *q, const adore_rows *k, const adore_rows *v,
+                           const adore_rows *out, float *lse, const adore_rows *rest, void *hip_stream);
+size_t adore_window_backward_workspace_bytes(const adore_prompt_config *cfg, const adore_window *window, int32_t packed);
+int adore_window_attention_backward(const adore_prompt_config *cfg, const adore_window *window, const int32_t *q_start,
+                                    const int32_t *k_start, const adore_rows *d_out, const adore_rows *q, const adore_rows *k,
+                                    const adore_rows *v, const adore_rows *out, const adore_rows *rest, const float *lse,
+                                    const adore_rows *dq, const adore_rows *dk, const adore_rows *dv, void *workspace,
+                                    size_t workspace_bytes, void *hip_stream);
+
+/* ---- Queries and keys on their way from a projection: norms per head and the rotation by their tokens' positions ----
+ * For rows that the caller projects itself (what rope_base does to the keys that the library makes).  Stateless; streams and devices as above.
+ *   y = x * w / sqrt(mean of x^2 over the head + eps)   where the tensor has weights w (fp32 [head_dim]); y = x where it has none
+ *   the first rotary_dim elements of a head are pairs, j < rotary_dim / 2: (j, j + rotary_dim / 2), interleaved != 0: (2 j, 2 j + 1);
+ *   with t = 2 pi position turns[j] / 2^64 a pair (a, b) becomes magnitude (a cos t - b sin t), magnitude (a sin t + b cos t);
+ *   the other elements stay y.
+ * bf16 or fp32 rows, all arithmetic in fp32 (angles in 64-bit fractions of a turn: any int32 position is as exact as a near one, within
+ * 2^-33 turns), rounded once.  The mean of squares has to be a finite fp32 number.
+ * turns: adore_rotary_turns makes them (HOST memory, the caller copies them to the device): frequencies f_j = base^(-2 j / rotary_dim) as
+ * fractions of a turn.  factor: 1 for frequencies as they are; with original = 0 all are divided by it; with original > 0 those that
+ * make at most `low` turns over `original` positions are, those that make at least `high` are not, in between the share that is not
+ * rises evenly.  Errors: E_INVALID (sizes, numbers that are not finite or not positive, low >= high, frequencies of 2^32 turns or more).
+ * positions: i32, of token t of sequence b at positions[b * pos_seq + t * pos_token].  Rows as in adore_prompt_attention: a packed
+ * tensor is one sequence (batch 1, tokens rows; one token of each of a batch too).  kv_heads may be 0: no k (k, k_out, ... NULL).
+ * q_out, k_out may be q, k themselves with the same strides, and dq, dk may be d_q_out, d_k_out or q, k; no other overlap.
+ * Errors of all: E_INVALID (null, sizes, magnitude or eps negative or not finite, a negative stride, rows not on 16-byte boundaries, weights
+ * not 16-byte aligned), E_UNSUPPORTED (head_dim not in {64,128}, a rotary_dim that is no multiple of 16, more than 2^24 tokens, 4096
+ * heads or 65536 sequences), E_HIP. */
+typedef struct {
+  int32_t batch, heads, kv_heads, head_dim;
+  int32_t tokens;           /* of every sequence */
+  int32_t dtype;            /* ADORE_F32 | ADORE_BF16: rows; weights and their gradients are fp32 */
+  int32_t rotary_dim;       /* 0: norms only (turns and positions may be NULL) */
+  int32_t interleaved;
+  float magnitude;          /* 0: 1 */
+  float eps;
+} adore_rotate_config;
+int adore_rotary_turns(int32_t rotary_dim, double base, double factor, double original, double low, double high,
+                       uint64_t *turns /* HOST [rotary_dim / 2] */);
+int adore_rotate_heads(const adore_rotate_config *cfg, const uint64_t *turns, const int32_t *positions, int64_t pos_seq,
+                       int64_t pos_token, const float *q_weight, const float *k_weight, const adore_rows *q,
+                       const adore_rows *k, const adore_rows *q_out, const adore_rows *k_out, void *hip_stream);
+
+/* Gradients of sum(d_q_out . q_out) + sum(d_k_out . k_out) by q, k and the weights.  q and k as they went in; a tensor without weights is not
+ * read and may be NULL.  dq_weight, dk_weight: fp32 [head_dim], given exactly where the weights are; sums over all rows in fixed order
+ * (every row counts, one whose gradients are zeros too where it is not finite).  workspace: DEVICE, 256-byte aligned, at least
+ * adore_rotate_backward_workspace_bytes(cfg) bytes (0 for a configuration that is not taken), free to reuse after the work enqueued here has
+ * run; may be NULL without weights.  Errors also: E_WORKSPACE. */
+size_t adore_rotate_backward_workspace_bytes(const adore_rotate_config *cfg);
+int adore_rotate_heads_backward(const adore_rotate_config *cfg, const uint64_t *turns, const int32_t *positions, int64_t pos_seq,
+                                int64_t pos_token, const float *q_weight, const float *k_weight, const adore_rows *d_q_out,
+                                const adore_rows *d_k_out, const adore_rows *q, const adore_rows *k, const adore_rows *dq,
+                                const adore_rows *dk, float *dq_weight, float *dk_weight, void *workspace,
+                                size_t workspace_bytes, void *hip_stream);
+
 /* ---- A cache held in 4 bits, evicted by the attention its rows received (Sec. 3.1, baseline 6: H2O) ----
  * For prompts and answers whose cache should be small: 17/32 of a byte per element instead of 2 or 4, and `slots` rows per
  * (sequence, kv head), of which each holds its own tokens.  Stateless calls over four buffers of the caller's (DEVICE):
@@ -442,6 +507,42 @@ int adore_q4_step(const adore_q4_config *cfg, const void *q, const void *k_new, 
 
 /* What the cache holds: k, v [batch][kv_heads][slots][head_dim] storage type, zeros in free slots. */
 int adore_q4_read(const adore_q4_config *cfg, const void *cache, const int32_t *slot_pos, void *k, void *v, void *hip_stream);
+
+/* ---- A cache for attention with a window and first tokens that stay (Sec. 3.1, baselines 2 and 5) ----
+ * What serves adore_window_attention token by token: sinks + window rows per (sequence, kv head), the token at position p in slot p if
+ * p < sinks, else in slot sinks + (p - sinks) % window, so that a token takes the row of the one that leaves its window.  Stateless
+ * calls over two buffers of the caller's (DEVICE), of which one stream at a time may work on the same:
+ *   cache    adore_ring_cache_bytes, 256-byte aligned: blocks of 32 slots, laid out as csrc/ring_cache.hip says
+ *   cursor   [batch][kv_heads] i32: the position of the next token, below 2^31 (0: an empty cache, whose rows are not read)
+ * Free slots are not read and may hold anything.
+ * Errors of all: E_INVALID (null, sizes, window < 1, sinks < 0, a negative or infinite scale, misaligned buffers), E_UNSUPPORTED (head_dim not
+ * in {64,128}, window + sinks > 2^20, batch > 2^16, heads > 2^12, batch * kv_heads * blocks > 2^23, batch * heads > 2^20), E_HIP. */
+typedef struct {
+  int32_t batch, heads, kv_heads, head_dim;
+  int32_t window, sinks;
+  int32_t dtype; /* ADORE_F32 | ADORE_BF16: rows, cache and outputs */
+  float scale;   /* 0: 1 / sqrt(head_dim) */
+} adore_ring_config;
+size_t adore_ring_cache_bytes(const adore_ring_config *cfg);     /* HOST calls; 0 for a configuration that is not taken */
+size_t adore_ring_workspace_bytes(const adore_ring_config *cfg); /* of adore_ring_step */
+
+/* Loads prompts: of a sequence's n rows the first `sinks` and the last `window` (all if n <= sinks + window).  k, v as in
+ * adore_prompt_attention: packed with k_start (k_tokens rows in all), or k_tokens per sequence.  seen (DEVICE [batch] i32, may be NULL): how
+ * many tokens the sequence has had where rows between the first and the last ones were left out; counts for a sequence of at least
+ * sinks + window rows, and not below their number.  The cursor becomes n (seen). */
+int adore_ring_fill(const adore_ring_config *cfg, const int32_t *k_start, int32_t k_tokens, const adore_rows *k,
+                    const adore_rows *v, const int32_t *seen, void *cache, int32_t *cursor, void *hip_stream);
+
+/* One token: k_new, v_new [batch][kv_heads][head_dim] take the cursor's slots, then
+ *   out[b][h][:] = sum_s softmax_s(scale q[b][h] . K[s]) V[s]   over the slots that are held, the new one among them,
+ * q, out [batch][heads][head_dim] storage type, and the cursor moves on.  fp32 sums and statistics; in bf16 a weight enters its product
+ * within 2^-16.  workspace: 256-byte aligned, at least adore_ring_workspace_bytes(cfg) bytes, free to reuse after the work enqueued here has
+ * run.  Errors also: E_WORKSPACE. */
+int adore_ring_step(const adore_ring_config *cfg, const void *q, const void *k_new, const void *v_new, void *cache,
+                    int32_t *cursor, void *out, void *workspace, size_t workspace_bytes, void *hip_stream);
+
+/* What the cache holds: k, v [batch][kv_heads][sinks + window][head_dim] storage type in the order of positions, zeros behind the last. */
+int adore_ring_read(const adore_ring_config *cfg, const void *cache, const int32_t *cursor, void *k, void *v, void *hip_stream);
 
 const char *adore_strerror(int code);
 /* Debug aid for callers and tests, not a step of the method (no passage of the paper): with ADORE_GUARD_WORDS=1

@@ -7,6 +7,7 @@ a call fails, an exception is raised.
 from __future__ import annotations
 
 import ctypes
+import math
 import os
 from typing import Dict, Optional
 
@@ -27,6 +28,9 @@ EXPORTS = [
     "adore_set_input_order", "adore_check_guards", "adore_set_timing", "adore_read_timing", "adore_kernel_name", "adore_strerror", "adore_abi_version",
     "adore_topk_attention_workspace_bytes", "adore_topk_attention", "adore_topk_attention_static",
     "adore_prompt_attention", "adore_prompt_backward_workspace_bytes", "adore_prompt_attention_backward", "adore_prompt_scores",
+    "adore_window_attention", "adore_window_backward_workspace_bytes", "adore_window_attention_backward", "adore_rotary_turns",
+    "adore_rotate_heads", "adore_rotate_backward_workspace_bytes", "adore_rotate_heads_backward",
+    "adore_ring_cache_bytes", "adore_ring_workspace_bytes", "adore_ring_fill", "adore_ring_step", "adore_ring_read",
 ]
 
 EXPORTS_Q4 = ["adore_q4_cache_bytes", "adore_q4_workspace_bytes", "adore_q4_fill", "adore_q4_step", "adore_q4_read"]
@@ -60,6 +64,21 @@ class AdorePromptConfig(ctypes.Structure):
 class AdoreQ4Config(ctypes.Structure):
     _fields_ = [(n, ctypes.c_int32) for n in
                 ("batch", "heads", "kv_heads", "head_dim", "slots", "recent", "dtype")] + [("scale", ctypes.c_float)]
+
+
+class AdoreWindow(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("window", "sinks")]
+
+
+class AdoreRotateConfig(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in
+                ("batch", "heads", "kv_heads", "head_dim", "tokens", "dtype", "rotary_dim", "interleaved")] + \
+               [("magnitude", ctypes.c_float), ("eps", ctypes.c_float)]
+
+
+class AdoreRingConfig(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in
+                ("batch", "heads", "kv_heads", "head_dim", "window", "sinks", "dtype")] + [("scale", ctypes.c_float)]
 
 
 class AdoreRows(ctypes.Structure):
@@ -138,6 +157,13 @@ def load_library() -> ctypes.CDLL:
     lib.adore_prompt_attention_backward.argtypes = [cfg, vp, vp] + [rows] * 6 + [vp] + [rows] * 3 + [vp, sz, vp]
     lib.adore_prompt_scores.restype = ctypes.c_int
     lib.adore_prompt_scores.argtypes = [cfg, vp, vp, rows, rows, vp, vp, vp]
+    win = ctypes.POINTER(AdoreWindow)
+    lib.adore_window_attention.restype = ctypes.c_int
+    lib.adore_window_attention.argtypes = [cfg, win, vp, vp, rows, rows, rows, rows, vp, rows, vp]
+    lib.adore_window_backward_workspace_bytes.restype = sz
+    lib.adore_window_backward_workspace_bytes.argtypes = [cfg, win, i32]
+    lib.adore_window_attention_backward.restype = ctypes.c_int
+    lib.adore_window_attention_backward.argtypes = [cfg, win, vp, vp] + [rows] * 6 + [vp] + [rows] * 3 + [vp, sz, vp]
     q4 = ctypes.POINTER(AdoreQ4Config)
     lib.adore_q4_cache_bytes.restype = lib.adore_q4_workspace_bytes.restype = sz
     lib.adore_q4_cache_bytes.argtypes = lib.adore_q4_workspace_bytes.argtypes = [q4]
@@ -145,6 +171,21 @@ def load_library() -> ctypes.CDLL:
     lib.adore_q4_fill.argtypes = [q4, vp, i32, rows, rows] + [vp] * 6
     lib.adore_q4_step.argtypes = [q4] + [vp] * 11 + [sz, vp]
     lib.adore_q4_read.argtypes = [q4] + [vp] * 5
+    rot, f64, i64 = ctypes.POINTER(AdoreRotateConfig), ctypes.c_double, ctypes.c_int64
+    lib.adore_rotary_turns.restype = ctypes.c_int
+    lib.adore_rotary_turns.argtypes = [i32] + [f64] * 5 + [vp]
+    lib.adore_rotate_backward_workspace_bytes.restype = sz
+    lib.adore_rotate_backward_workspace_bytes.argtypes = [rot]
+    lib.adore_rotate_heads.restype = lib.adore_rotate_heads_backward.restype = ctypes.c_int
+    lib.adore_rotate_heads.argtypes = [rot, vp, vp, i64, i64, vp, vp] + [rows] * 4 + [vp]
+    lib.adore_rotate_heads_backward.argtypes = [rot, vp, vp, i64, i64, vp, vp] + [rows] * 6 + [vp, vp, vp, sz, vp]
+    ring = ctypes.POINTER(AdoreRingConfig)
+    lib.adore_ring_cache_bytes.restype = lib.adore_ring_workspace_bytes.restype = sz
+    lib.adore_ring_cache_bytes.argtypes = lib.adore_ring_workspace_bytes.argtypes = [ring]
+    lib.adore_ring_fill.restype = lib.adore_ring_step.restype = lib.adore_ring_read.restype = ctypes.c_int
+    lib.adore_ring_fill.argtypes = [ring, vp, i32, rows, rows] + [vp] * 4
+    lib.adore_ring_step.argtypes = [ring] + [vp] * 7 + [sz, vp]
+    lib.adore_ring_read.argtypes = [ring] + [vp] * 5
     _lib = lib
     return lib
 
@@ -295,8 +336,21 @@ class _Prompts:
         return _stream(self.index)
 
 
+def _window(window, sinks):
+    """The window of a call, None for none."""
+    if window is None:
+        if sinks:
+            raise ValueError("sinks: without a window all keys are seen")
+        return None
+    if window < 1 or sinks < 0:
+        raise ValueError("window, sinks: expected at least 1 and at least 0")
+    most = 1 << 30                             # (more than any sequence has)
+    return ctypes.byref(AdoreWindow(min(int(window), most), min(int(sinks), most)))
+
+
 def prompt_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, *, q_start: torch.Tensor = None,
-                     k_start: torch.Tensor = None, scale: float = None, out: torch.Tensor = None, rest: bool = False):
+                     k_start: torch.Tensor = None, scale: float = None, out: torch.Tensor = None, rest: bool = False, window: int = None,
+                     sinks: int = 0):
     """adore_prompt_attention on torch's current stream: causal attention over whole prompts; returns (out, lse), and with rest=True
     (out, lse, rest) for the backward pass (rest is None where out is fp32 and nothing is lost).
 
@@ -304,19 +358,24 @@ def prompt_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, *, q_sta
     [batch + 1] on the GPU.  A dense batch: [batch, heads, tokens, head_dim] without starts.  bf16 or fp32, any strides with a
     dense last dimension (q, k and v may be views of one projection).  out is allocated here unless given.
 
+    window, sinks (adore_window_attention): a query sees the last `window` keys up to its own and the sequence's first `sinks` ones only;
+    the backward pass takes the same two.  prompt_scores knows no window.
+
     Where q, k or v require gradients, out has them: torch's backward pass is prompt_attention_backward (once; lse and rest have
     none, and out cannot be given then).  A step that is captured into a graph calls the two itself, under torch.no_grad()."""
     if torch.is_grad_enabled() and (q.requires_grad or k.requires_grad or (isinstance(v, torch.Tensor) and v.requires_grad)):
         if out is not None:
             raise ValueError("out: cannot be given where gradients are required (call under torch.no_grad())")
-        got = _PromptAttention.apply(q, k, v, q_start, k_start, scale, rest)
+        got = _PromptAttention.apply(q, k, v, q_start, k_start, scale, rest, window, sinks)
     else:
-        got = _attend_prompts(q, k, v, q_start, k_start, scale, out, rest)
+        got = _attend_prompts(q, k, v, q_start, k_start, scale, out, rest, window, sinks)
     return got if rest else got[:2]
 
 
-def _attend_prompts(q, k, v, q_start, k_start, scale, out, rest):
+def _attend_prompts(q, k, v, q_start, k_start, scale, out, rest, window=None, sinks=0):
     lib = load_library()
+    win = _window(window, sinks)
+    function, how = (lib.adore_prompt_attention, ()) if win is None else (lib.adore_window_attention, (win,))
     p = _Prompts(q, k, q_start, k_start, scale)
     rows = None
     if out is None:
@@ -324,7 +383,7 @@ def _attend_prompts(q, k, v, q_start, k_start, scale, out, rest):
         rows = p.fresh(out)
     lse = torch.empty(p.q_rows, dtype=torch.float32, device=p.device)
     left = torch.empty(p.q_shape, dtype=q.dtype, device=p.device) if rest and q.dtype == torch.bfloat16 else None
-    _call(lib, p.index, lib.adore_prompt_attention, ctypes.byref(p.cfg), *p.starts, p.rows(q, p.q_shape, "q"), p.rows(k, p.k_shape, "k"),
+    _call(lib, p.index, function, ctypes.byref(p.cfg), *how, *p.starts, p.rows(q, p.q_shape, "q"), p.rows(k, p.k_shape, "k"),
           p.rows(v, p.k_shape, "v"), rows or p.rows(out, p.q_shape, "out", True), lse.data_ptr() or 16, None if left is None else p.fresh(left),
           p.stream)
     return out, lse, left
@@ -332,10 +391,10 @@ def _attend_prompts(q, k, v, q_start, k_start, scale, out, rest):
 
 class _PromptAttention(torch.autograd.Function):
     @staticmethod
-    def forward(ctx, q, k, v, q_start, k_start, scale, rest):
-        out, lse, left = _attend_prompts(q, k, v, q_start, k_start, scale, None, rest)
+    def forward(ctx, q, k, v, q_start, k_start, scale, rest, window, sinks):
+        out, lse, left = _attend_prompts(q, k, v, q_start, k_start, scale, None, rest, window, sinks)
         ctx.save_for_backward(q, k, v, out, lse, left, q_start, k_start)
-        ctx.scale = scale
+        ctx.how = dict(scale=scale, window=window, sinks=sinks)
         ctx.mark_non_differentiable(*(x for x in (lse, left) if x is not None))
         ctx.set_materialize_grads(False)
         return out, lse, left
@@ -344,21 +403,21 @@ class _PromptAttention(torch.autograd.Function):
     @torch.autograd.function.once_differentiable
     def backward(ctx, d_out, *_):
         if d_out is None:
-            return (None,) * 7
+            return (None,) * 9
         q, k, v, out, lse, left, q_start, k_start = ctx.saved_tensors
         # (whatever made d_out chose its layout: of a sum, one element for all)
         if d_out.stride(-1) != 1 or d_out.data_ptr() % 16 or any(s * d_out.element_size() % 16 for s in d_out.stride()[:-1]):
             d_out = d_out.clone(memory_format=torch.contiguous_format)
-        grads = prompt_attention_backward(d_out, q, k, v, out, lse, rest=left, q_start=q_start, k_start=k_start, scale=ctx.scale)
-        return *(g if want else None for g, want in zip(grads, ctx.needs_input_grad)), None, None, None, None
+        grads = prompt_attention_backward(d_out, q, k, v, out, lse, rest=left, q_start=q_start, k_start=k_start, **ctx.how)
+        return *(g if want else None for g, want in zip(grads, ctx.needs_input_grad)), *(None,) * 6
 
 
 def prompt_attention_backward(d_out: torch.Tensor, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, out: torch.Tensor,
                               lse: torch.Tensor, *, rest: torch.Tensor = None, q_start: torch.Tensor = None,
                               k_start: torch.Tensor = None, scale: float = None, dq: torch.Tensor = None, dk: torch.Tensor = None,
-                              dv: torch.Tensor = None):
+                              dv: torch.Tensor = None, window: int = None, sinks: int = 0):
     """adore_prompt_attention_backward on torch's current stream: (dq, dk, dv) of sum(d_out * out).  out, lse and rest as
-    prompt_attention returned them for these q, k, v, starts and scale; dq, dk, dv are allocated here unless given (the places of
+    prompt_attention returned them for these q, k, v, starts, scale, window and sinks; dq, dk, dv are allocated here unless given (the places of
     q, k and v in the gradient of one projection, say)."""
     lib = load_library()
     p = _Prompts(q, k, q_start, k_start, scale)
@@ -369,9 +428,15 @@ def prompt_attention_backward(d_out: torch.Tensor, q: torch.Tensor, k: torch.Ten
         return t, p.fresh(t)
 
     (dq, dq_rows), (dk, dk_rows), (dv, dv_rows) = gradient(dq, p.q_shape, "dq"), gradient(dk, p.k_shape, "dk"), gradient(dv, p.k_shape, "dv")
-    need = lib.adore_prompt_backward_workspace_bytes(ctypes.byref(p.cfg), int(p.packed))
+    win = _window(window, sinks)
+    if win is None:
+        function, how = lib.adore_prompt_attention_backward, ()
+        need = lib.adore_prompt_backward_workspace_bytes(ctypes.byref(p.cfg), int(p.packed))
+    else:
+        function, how = lib.adore_window_attention_backward, (win,)
+        need = lib.adore_window_backward_workspace_bytes(ctypes.byref(p.cfg), win, int(p.packed))
     workspace = torch.empty(max(need, 1), dtype=torch.uint8, device=q.device)
-    _call(lib, p.index, lib.adore_prompt_attention_backward, ctypes.byref(p.cfg), *p.starts, p.rows(d_out, p.q_shape, "d_out"),
+    _call(lib, p.index, function, ctypes.byref(p.cfg), *how, *p.starts, p.rows(d_out, p.q_shape, "d_out"),
           p.rows(q, p.q_shape, "q"), p.rows(k, p.k_shape, "k"), p.rows(v, p.k_shape, "v"), p.rows(out, p.q_shape, "out"),
           None if rest is None else p.rows(rest, p.q_shape, "rest"), p.values(lse, p.q_rows, "lse"), dq_rows, dk_rows, dv_rows,
           workspace.data_ptr(), need, p.stream)
@@ -390,6 +455,190 @@ def prompt_scores(q: torch.Tensor, k: torch.Tensor, lse: torch.Tensor, *, q_star
     _call(lib, p.index, lib.adore_prompt_scores, ctypes.byref(p.cfg), *p.starts, p.rows(q, p.q_shape, "q"), p.rows(k, p.k_shape, "k"),
           p.values(lse, p.q_rows, "lse"), p.values(scores, p.k_rows, "scores"), p.stream)
     return scores
+
+
+class Rotary:
+    """How heads are rotated: pairs of the first `rotary_dim` elements, (j, j + rotary_dim / 2) or, interleaved, (2 j, 2 j + 1), by
+    position * base^(-2 j / rotary_dim), and stretched by `magnitude`.
+
+    For longer texts than a model knows: factor with original=None divides all frequencies by it; with `original` positions, those that
+    make at most `low` turns over them are divided, those that make at least `high` are not, in between the two are blended.
+    Made once; any int32 position, any device (a copy of `turns` for each: the first call there must not be one that is captured)."""
+
+    def __init__(self, rotary_dim: int, *, base: float = 10000.0, interleaved: bool = False, factor: float = 1.0, original: float = None,
+                 low: float = 1.0, high: float = 32.0, magnitude: float = 1.0):
+        if rotary_dim <= 0 or rotary_dim % 16:
+            raise ValueError("rotary_dim: expected a positive multiple of 16")
+        if not (magnitude > 0.0 and math.isfinite(magnitude)):
+            raise ValueError("magnitude: expected a positive number")
+        if original is not None and not original > 0.0:
+            raise ValueError("original: expected a positive number")
+        self.rotary_dim, self.interleaved, self.magnitude = int(rotary_dim), bool(interleaved), float(magnitude)
+        lib = load_library()
+        turns = (ctypes.c_uint64 * (rotary_dim // 2))()
+        _check(lib, lib.adore_rotary_turns(rotary_dim, base, factor, 0.0 if original is None else original, low, high, turns))
+        self.turns = torch.tensor([t - (1 << 64) if t >> 63 else t for t in turns], dtype=torch.int64)     # (torch has no operations on uint64)
+        self._there = {}
+
+    def on(self, device: torch.device) -> torch.Tensor:
+        """The table on a device."""
+        if device not in self._there:
+            self._there[device] = self.turns.to(device)
+        return self._there[device]
+
+
+class _Heads:
+    """The rows of a call on queries and keys, packed [tokens, heads, head_dim] or dense [batch, heads, tokens, head_dim]."""
+
+    def __init__(self, q, k, positions, rotary, q_weight, k_weight, eps):
+        code = _CODES.get(q.dtype)
+        index = q.get_device()
+        if code is None or index < 0:
+            raise ValueError(f"q: expected a bf16 or fp32 GPU tensor, got {q.device} {q.dtype}")
+        self.device, self.index, self.dtype = q.device, index, q.dtype
+        qs = self.q_shape = q.shape
+        if len(qs) not in (3, 4):
+            raise ValueError("q: expected [tokens, heads, head_dim] or [batch, heads, tokens, head_dim]")
+        self.packed = len(qs) == 3
+        batch, heads, tokens = (1, qs[1], qs[0]) if self.packed else (qs[0], qs[1], qs[2])
+        kv = 0
+        self.k_shape = None
+        if k is not None:
+            self.k_shape = k.shape
+            kv = k.shape[1] if k.dim() == len(qs) else 0
+            if kv == 0 or k.shape != (qs[:1] + k.shape[1:2] + qs[2:]):
+                raise ValueError(f"k: expected q's shape {tuple(qs)} but for the heads, got {tuple(k.shape)}")
+        if not eps >= 0.0:
+            raise ValueError("eps: expected a number that is not negative")
+        if rotary is None and q_weight is None and k_weight is None:
+            raise ValueError("rotary: expected one, or weights of norms")
+        self.positions = (None, 0, 0)
+        if rotary is not None:
+            if rotary.rotary_dim > qs[-1]:
+                raise ValueError(f"rotary: expected one of at most {qs[-1]} elements")
+            want = (tokens,) if self.packed else (batch, tokens)
+            if not isinstance(positions, torch.Tensor) or positions.dtype is not torch.int32 or positions.get_device() != index or \
+                    (positions.shape != want and positions.shape != want[-1:]):
+                raise ValueError(f"positions: expected int32 {list(want)}{'' if self.packed else f' or [{tokens}]'} on {self.device}")
+            stride = positions.stride()
+            self.positions = (positions.data_ptr() or 16, stride[0] if len(stride) == 2 and batch > 1 else 0, stride[-1] if tokens > 1 else 0)
+            self.turns = rotary.on(self.device).data_ptr()
+            self.cfg = AdoreRotateConfig(batch, heads, kv, qs[-1], tokens, code, rotary.rotary_dim, int(rotary.interleaved), rotary.magnitude, eps)
+        else:
+            self.turns = None
+            self.cfg = AdoreRotateConfig(batch, heads, kv, qs[-1], tokens, code, 0, 0, 1.0, eps)
+        self.weights = tuple(None if w is None else self.weight(w, n) for w, n in ((q_weight, "q_weight"), (k_weight, "k_weight")))
+        if k is None and k_weight is not None:
+            raise ValueError("k_weight: there is no k")
+
+    def weight(self, w, name):
+        d = self.q_shape[-1]
+        if not isinstance(w, torch.Tensor) or w.dtype is not torch.float32 or w.get_device() != self.index or w.shape != (d,) or not w.is_contiguous() or \
+                w.data_ptr() % 16:
+            raise ValueError(f"{name}: expected contiguous fp32 [{d}] on {self.device}, 16-byte aligned")
+        return w.data_ptr()
+
+    def rows(self, t, shape, name: str, written: bool = False):
+        if not isinstance(t, torch.Tensor) or t.shape != shape or t.dtype is not self.dtype or t.get_device() != self.index:
+            raise ValueError(f"{name}: expected a {self.dtype} tensor of shape {tuple(shape)} on {self.device}")
+        stride = t.stride()
+        if shape[-1] > 1 and stride[-1] != 1:
+            raise ValueError(f"{name}: its last dimension has to be dense")
+        stride = tuple(0 if n <= 1 else s for n, s in zip(shape, stride))
+        if written and any(n > 1 and s == 0 for n, s in zip(shape, stride)):
+            raise ValueError(f"{name}: its rows lie on one another")
+        ptr = t.data_ptr() or 16
+        if self.packed:
+            return ctypes.byref(AdoreRows(ptr, 0, stride[0], stride[1]))
+        return ctypes.byref(AdoreRows(ptr, stride[0], stride[2], stride[1]))
+
+    def result(self, t, shape, name: str):
+        """A tensor to write to, made here unless given, and its rows; two Nones where there is none."""
+        if shape is None:
+            if t is not None:
+                raise ValueError(f"{name}: there is no k")
+            return None, None
+        if t is None:
+            t = torch.empty(shape, dtype=self.dtype, device=self.device)
+        return t, self.rows(t, shape, name, True)
+
+
+def rotate_heads(q: torch.Tensor, k: Optional[torch.Tensor], positions: Optional[torch.Tensor], rotary: Optional[Rotary], *,
+                 q_weight: torch.Tensor = None, k_weight: torch.Tensor = None, eps: float = 1e-6, q_out: torch.Tensor = None,
+                 k_out: torch.Tensor = None):
+    """adore_rotate_heads on torch's current stream: queries and keys on their way from a projection to attention or into a cache, each
+    head normed where its tensor has weights (fp32 [head_dim]), then rotated by its token's position.  Returns (q, k) anew, or in q_out and
+    k_out (which may be q and k themselves).
+
+    Packed rows: q [tokens, heads, head_dim], k [tokens, kv heads, head_dim], positions int32 [tokens] (one token of each sequence of a
+    batch too).  Dense: [batch, heads, tokens, head_dim] and positions [batch, tokens] or [tokens].  bf16 or fp32, any strides with a
+    dense last dimension (views of one projection).  k may be None; so may rotary, for norms alone.
+
+    Where q, k or weights require gradients the results have them (torch's backward pass is rotate_heads_backward, once); q_out and
+    k_out cannot be given then."""
+    inputs = (q, k, q_weight, k_weight)
+    if torch.is_grad_enabled() and any(isinstance(t, torch.Tensor) and t.requires_grad for t in inputs):
+        if q_out is not None or k_out is not None:
+            raise ValueError("q_out, k_out: cannot be given where gradients are required (call under torch.no_grad())")
+        return _RotateHeads.apply(q, k, q_weight, k_weight, positions, rotary, eps)
+    return _rotate(q, k, positions, rotary, q_weight, k_weight, eps, q_out, k_out)
+
+
+def _rotate(q, k, positions, rotary, q_weight, k_weight, eps, q_out=None, k_out=None):
+    lib = load_library()
+    h = _Heads(q, k, positions, rotary, q_weight, k_weight, eps)
+    q_out, q_to = h.result(q_out, h.q_shape, "q_out")
+    k_out, k_to = h.result(k_out, h.k_shape, "k_out")
+    _call(lib, h.index, lib.adore_rotate_heads, ctypes.byref(h.cfg), h.turns, *h.positions, *h.weights, h.rows(q, h.q_shape, "q"),
+          None if k is None else h.rows(k, h.k_shape, "k"), q_to, k_to, _stream(h.index))
+    return q_out, k_out
+
+
+def _sixteen(t):
+    """Rows on 16-byte boundaries, the last dimension dense (whatever made a gradient chose its layout)."""
+    if t is None or (t.stride(-1) == 1 and t.data_ptr() % 16 == 0 and all(s * t.element_size() % 16 == 0 for s in t.stride()[:-1])):
+        return t
+    return t.clone(memory_format=torch.contiguous_format)
+
+
+class _RotateHeads(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, q, k, q_weight, k_weight, positions, rotary, eps):
+        ctx.save_for_backward(q, k, q_weight, k_weight, positions)
+        ctx.rest = rotary, eps
+        return _rotate(q, k, positions, rotary, q_weight, k_weight, eps)
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, d_q, d_k):
+        q, k, q_weight, k_weight, positions = ctx.saved_tensors
+        rotary, eps = ctx.rest
+        grads = rotate_heads_backward(_sixteen(d_q), _sixteen(d_k), q, k, positions, rotary, q_weight=q_weight, k_weight=k_weight, eps=eps)
+        return *(g if want else None for g, want in zip(grads, ctx.needs_input_grad)), None, None, None
+
+
+def rotate_heads_backward(d_q: torch.Tensor, d_k: Optional[torch.Tensor], q: torch.Tensor, k: Optional[torch.Tensor],
+                          positions: Optional[torch.Tensor], rotary: Optional[Rotary], *, q_weight: torch.Tensor = None,
+                          k_weight: torch.Tensor = None, eps: float = 1e-6, dq: torch.Tensor = None, dk: torch.Tensor = None):
+    """adore_rotate_heads_backward on torch's current stream: (dq, dk, dq_weight, dk_weight) of sum(d_q * q_out) + sum(d_k * k_out), None
+    for what is not there.  The other arguments as rotate_heads took them; dq and dk are allocated here unless given (the places of q
+    and k in the gradient of one projection, say, or d_q and d_k themselves)."""
+    lib = load_library()
+    h = _Heads(q, k, positions, rotary, q_weight, k_weight, eps)
+    if k is None and d_k is not None:
+        raise ValueError("d_k: there is no k")
+    dq, dq_to = h.result(dq, h.q_shape, "dq")
+    dk, dk_to = h.result(dk, h.k_shape, "dk")
+    dqw, dkw = (None if w is None else torch.empty(h.q_shape[-1], dtype=torch.float32, device=h.device) for w in h.weights)
+    need, space = 0, None
+    if dqw is not None or dkw is not None:
+        need = lib.adore_rotate_backward_workspace_bytes(ctypes.byref(h.cfg))
+        space = torch.empty(max(need, 1), dtype=torch.uint8, device=h.device)
+    _call(lib, h.index, lib.adore_rotate_heads_backward, ctypes.byref(h.cfg), h.turns, *h.positions, *h.weights,
+          h.rows(d_q, h.q_shape, "d_q"), None if k is None else h.rows(d_k, h.k_shape, "d_k"), h.rows(q, h.q_shape, "q"),
+          None if k is None else h.rows(k, h.k_shape, "k"), dq_to, dk_to, None if dqw is None else dqw.data_ptr(),
+          None if dkw is None else dkw.data_ptr(), None if space is None else space.data_ptr(), need, _stream(h.index))
+    return dq, dk, dqw, dkw
 
 
 class Q4Cache:
@@ -479,6 +728,94 @@ class Q4Cache:
                 for t, n in ((k, "k"), (v, "v")))
         _call(self.lib, self._index, self.lib.adore_q4_read, self._cfg, self._state[0], self._state[1], k.data_ptr(), v.data_ptr(),
               _stream(self._index))
+        return k, v
+
+
+class WindowCache:
+    """A K/V cache for attention with a window and first tokens that stay (adore_ring_* in include/adore.h): what prompt_attention with a
+    window is served with, a token at a time.  fill() loads prompts, step() takes one token of every sequence, read() gives the
+    contents in the order of their positions.  Buffers that are given are used as they are; others are made here, empty.
+
+      cache   [batch, kv_heads, ceil((window + sinks) / 32), 64 * head_dim]      cursor   int32 [batch, kv_heads]: the next token's position
+
+    One stream at a time: every call works on the same buffers."""
+
+    def __init__(self, *, batch: int, heads: int, kv_heads: int, head_dim: int, window: int, sinks: int = 0, dtype, scale: float = None,
+                 cache: torch.Tensor = None, cursor: torch.Tensor = None, device="cuda:0"):
+        self.lib = load_library()
+        code = {"f32": ADORE_F32, "bf16": ADORE_BF16}[dtype] if isinstance(dtype, str) else _CODES[dtype]
+        if scale is not None and not scale > 0.0:
+            raise ValueError("scale: expected a positive number")
+        self.cfg = AdoreRingConfig(batch, heads, kv_heads, head_dim, window, sinks, code, float(scale or 0.0))
+        self.dtype = torch.bfloat16 if code == ADORE_BF16 else torch.float32
+        if self.lib.adore_ring_cache_bytes(ctypes.byref(self.cfg)) == 0:
+            raise AdoreError(-1, "invalid or unsupported configuration")
+        self.device = torch.device(device) if cache is None else cache.device
+        rows = (batch, kv_heads)
+        self.cache = self._buffer(cache, rows + ((window + sinks + 31) // 32, 64 * head_dim), self.dtype, "cache", 256)
+        self.device = self.cache.device        # (with its number)
+        self.cursor = self._buffer(cursor, rows, torch.int32, "cursor", 4)
+        self.workspace = torch.empty(self.lib.adore_ring_workspace_bytes(ctypes.byref(self.cfg)), dtype=torch.uint8, device=self.device)
+        # what every call hands over, made once (a step of few rows takes the host longer than the GPU)
+        self._cfg = ctypes.byref(self.cfg)
+        self._state = [ctypes.c_void_p(self.cache.data_ptr()), ctypes.c_void_p(self.cursor.data_ptr())]
+        self._space = [ctypes.c_void_p(self.workspace.data_ptr()), ctypes.c_size_t(self.workspace.numel())]
+        self._index = self.cache.get_device()
+        self._mine, self._rows = (batch, heads, head_dim), rows + (head_dim,)
+
+    @property
+    def positions(self) -> torch.Tensor:
+        """The next token's position in every sequence, int32 [batch], as the cache counts it: what its query and key are rotated by
+        ahead of step()."""
+        return self.cursor[:, 0]
+
+    def _buffer(self, t, shape, dtype, name, align):
+        if t is None:
+            return torch.zeros(shape, dtype=dtype, device=self.device)
+        return self._tensor(t, shape, dtype, name, align)
+
+    def _tensor(self, t, shape, dtype, name, align=16):
+        if not isinstance(t, torch.Tensor) or t.device != self.device or not t.is_cuda or t.dtype != dtype or tuple(t.shape) != tuple(shape) or \
+                not t.is_contiguous() or t.data_ptr() % align:
+            raise ValueError(f"{name}: expected a contiguous {dtype} tensor of shape {tuple(shape)} on {self.device}, {align}-byte aligned")
+        return t
+
+    def fill(self, k: torch.Tensor, v: torch.Tensor, *, k_start: torch.Tensor = None, seen: torch.Tensor = None):
+        """The prompts' first tokens and those of their last window: k, v [tokens, kv_heads, head_dim] with k_start (int32 [batch + 1]), or
+        [batch, kv_heads, tokens, head_dim].  seen (int32 [batch]): how many tokens the sequences have had, where rows in between were left
+        out (what read() gave, with new rows behind it)."""
+        c = self.cfg
+        p = _Prompts(k, k, k_start, k_start, None)
+        if p.device != self.device or p.dtype != self.dtype or (p.batch, p.cfg.kv_heads, p.cfg.head_dim) != (c.batch, c.kv_heads, c.head_dim):
+            raise ValueError(f"k: expected {self.dtype} rows of {c.batch} sequences, {c.kv_heads} heads, {c.head_dim} elements on {self.device}")
+        if seen is not None:
+            seen = self._tensor(seen, (c.batch,), torch.int32, "seen", 4).data_ptr()
+        _call(self.lib, self._index, self.lib.adore_ring_fill, self._cfg, p.starts[1], p.cfg.k_tokens, p.rows(k, p.k_shape, "k"),
+              p.rows(v, p.k_shape, "v"), seen, *self._state, p.stream)
+
+    def step(self, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, *, out: torch.Tensor = None) -> torch.Tensor:
+        """One token of every sequence: q [batch, heads, head_dim], k and v [batch, kv_heads, head_dim], contiguous.  Returns out
+        [batch, heads, head_dim]."""
+        mine, rows = self._mine, self._rows
+        at = (self._ptr(q, mine, "q"), self._ptr(k, rows, "k"), self._ptr(v, rows, "v"))
+        if out is None:
+            out = torch.empty_like(q)
+        _call(self.lib, self._index, self.lib.adore_ring_step, self._cfg, *at, *self._state, self._ptr(out, mine, "out"), *self._space,
+              _stream(self._index))
+        return out
+
+    def _ptr(self, t, shape, name):
+        if t.dtype is not self.dtype or t.shape != shape or t.get_device() != self._index or not t.is_contiguous() or t.data_ptr() % 16:
+            self._tensor(t, shape, self.dtype, name)
+        return t.data_ptr()
+
+    def read(self, k: torch.Tensor = None, v: torch.Tensor = None):
+        """What the cache holds: K and V [batch, kv_heads, sinks + window, head_dim] in the order of positions, zeros behind the last."""
+        c = self.cfg
+        shape = (c.batch, c.kv_heads, c.sinks + c.window, c.head_dim)
+        k, v = (torch.empty(shape, dtype=self.dtype, device=self.device) if t is None else self._tensor(t, shape, self.dtype, n)
+                for t, n in ((k, "k"), (v, "v")))
+        _call(self.lib, self._index, self.lib.adore_ring_read, self._cfg, *self._state, k.data_ptr(), v.data_ptr(), _stream(self._index))
         return k, v
 
 

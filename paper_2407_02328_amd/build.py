@@ -8,7 +8,8 @@ ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libadore.so")
 SOURCES = ["adore_api.hip", "attend.hip", "controller.hip", "select.hip", "rebuild.hip", "forward_attend.hip", "rope.hip", "topk_attend.hip", "h2o.hip",
-           "prompt_attend.hip", "prompt_backward.hip", "q4_cache.hip"]
+           "prompt_attend.hip", "prompt_backward.hip", "q4_cache.hip", "rotate_heads.hip",
+           "ring_cache.hip"]
 HEADERS = ["adore_internal.h", "device_utils.h", "select_device.h", "ctrl_device.h", "prompt_device.h"]
 
 HIPCC_FLAGS = [

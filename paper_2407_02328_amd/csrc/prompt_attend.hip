@@ -41,7 +41,8 @@ constexpr int kKeys = sizeof(T) == 2 ? 64 : 32;
 
 // REST: P goes in as two bf16 terms (within 2^-16) and what rounding out leaves is handed out, for a backward pass whose delta is as good
 // as its other terms.
-template <typename T, int DH, bool REST, int SW>
+// WIN: with a window (s.window, s.sinks).
+template <typename T, int DH, bool REST, int SW, bool WIN>
 __global__ __launch_bounds__(256) ADORE_WAVES(sizeof(T) == 4 || SW > 1 ? 1 : DH == 128 ? 2 : REST ? 3 : 4)
 void prompt_attend_kernel(const AttendArgs<T> a) {
   constexpr int NT = 256, BQ = Shared<SW>::kRows, KT = SW > 1 ? 32 * SW : kKeys<T>, KB = SW > 1 ? 1 : KT / 32, DB = DH / 32, ST = DH / 16;
@@ -68,16 +69,23 @@ void prompt_attend_kernel(const AttendArgs<T> a) {
   const char *vp = reinterpret_cast<const char *>(a.v.p + sq.b * a.v.seq + sq.k_first * a.v.token + hk * a.v.head);
 
   const int last = min(block * BQ + BQ, sq.nq) - 1 + off;             // the last key that a query of the workgroup sees
-  const int tiles = last < 0 ? 0 : last / KT + 1;
+  const int upto = last < 0 ? 0 : last / KT + 1;
+  const WindowTiles<KT> win(a.s, block * BQ + off, last, upto);       // (WIN)
+  const int tiles = WIN ? win.total : upto;
   const int mine = rows > 0 ? q0 + rows - 1 + off : -1;               // ... of the wave
   const int seen = q0 + c + off;                                      // ... of the lane
   const float scale = a.s.scale_log2;
   const uint32_t base0 = __builtin_amdgcn_readfirstlane(lds_offset(smem)), share = base0 + uint32_t(wave) * 1024u;
   const int64_t ks = KT * a.k.token * int64_t(sizeof(T)), vs = KT * a.v.token * int64_t(sizeof(T));   // from tile to tile
   const TileLoad<T, DH, KT, NT> lk(a.k.token * int64_t(sizeof(T)), tid), lv(a.v.token * int64_t(sizeof(T)), tid);
+  if (WIN && win.sinks == 0) {
+    kp += win.skip * ks;
+    vp += win.skip * vs;
+  }
   if (tiles > 0) {
-    lk(kp, sq.nk, share);
-    lv(vp, sq.nk, share + kTile);
+    const int left = sq.nk - (WIN ? win.tile(0) * KT : 0);
+    lk(kp, left, share);
+    lv(vp, left, share + kTile);
   }
   Reader<T, DH> read(base0 + uint32_t(mate.part * 32 * L::kRow), lane);
   // the query operand, through the wave's share of the second stage
@@ -94,21 +102,23 @@ void prompt_attend_kernel(const AttendArgs<T> a) {
   const int hidden = max(block * BQ + off + 1, 0) / KT;               // the first tile that not all of the workgroup's queries see all of
   bool found = false;                           // ... where a value is not finite
   for (int it = 0; it < tiles; ++it) {
-    const int k0 = it * KT + mate.part * 32;    // the wave's first key of the tile
+    const int tile = WIN ? win.tile(it) : it;
+    const int k0 = tile * KT + mate.part * 32;  // the wave's first key of the tile
     arrived();
     __syncthreads();
-    if (it >= hidden) {
+    if (tile >= hidden || (WIN && tile * KT < win.partial && tile * KT + KT > a.s.sinks)) {
       found |= make_finite<T, DH, KT, NT>(smem + (it & 1) * 2 * kTile + kTile);
       __syncthreads();
     }
     if (it + 1 < tiles) {
       const uint32_t next = share + uint32_t(~it & 1) * uint32_t(2 * kTile);
-      kp += ks;
-      vp += vs;
-      lk(kp, sq.nk - (it + 1) * KT, next);
-      lv(vp, sq.nk - (it + 1) * KT, next + kTile);
+      const int following = WIN ? win.tile(it + 1) : it + 1;
+      kp += WIN ? (following - tile) * ks : ks;
+      vp += WIN ? (following - tile) * vs : vs;
+      lk(kp, sq.nk - following * KT, next);
+      lv(vp, sq.nk - following * KT, next + kTile);
     }
-    if (k0 <= mine) {
+    if (k0 <= mine && (!WIN || k0 + 32 * KB > q0 + off - a.s.window + 1 || k0 < a.s.sinks)) {
       // Operands are on their way from LDS ahead of the products that take them, and arithmetic stands between products: a wave issues in
       // order, and left to itself the compiler reads, waits and multiplies in turn.
       // While a wave has products to issue it goes ahead of the SIMD's others, which are at their maxima or waiting: 2 % less.
@@ -137,6 +147,15 @@ void prompt_attend_kernel(const AttendArgs<T> a) {
 #pragma unroll
           for (int r = 0; r < 16; ++r)
             if (k0 + kb * 32 + 8 * (r >> 2) + 4 * h + (r & 3) > seen) s[kb][r] = -INFINITY;
+      }
+      if (WIN && k0 <= q0 + 31 + off - a.s.window && k0 + 32 * KB > a.s.sinks) {      // ... because they are too far behind
+#pragma unroll
+        for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) {
+            const int key = k0 + kb * 32 + 8 * (r >> 2) + 4 * h + (r & 3);
+            if (key <= seen - a.s.window && key >= a.s.sinks) s[kb][r] = -INFINITY;
+          }
       }
 #pragma unroll
       for (int kb = 0; kb < KB; ++kb)
@@ -219,9 +238,16 @@ void prompt_attend_kernel(const AttendArgs<T> a) {
     top = m;
   }
   if (rows <= 0) return;
-  if (found)
-    add_not_finite<T, DH>(o, reinterpret_cast<const char *>(a.v.p + sq.b * a.v.seq + sq.k_first * a.v.token + hk * a.v.head),
-                          a.v.token * int64_t(sizeof(T)), hidden * KT, mine + 1, seen, lane);
+  if (found) {
+    const char *const v0 = reinterpret_cast<const char *>(a.v.p + sq.b * a.v.seq + sq.k_first * a.v.token + hk * a.v.head);
+    const int64_t pitch = a.v.token * int64_t(sizeof(T));
+    if constexpr (WIN) {          // (all that the lane's query sees: what is not finite stays so when it is added twice)
+      add_not_finite<T, DH>(o, v0, pitch, 0, min(a.s.sinks, mine + 1), 0, seen, lane);
+      add_not_finite<T, DH>(o, v0, pitch, win.low, mine + 1, seen - a.s.window + 1, seen, lane);
+    } else {
+      add_not_finite<T, DH>(o, v0, pitch, hidden * KT, mine + 1, 0, seen, lane);
+    }
+  }
   sum = add_lane_xor<32>(sum);
   const bool some = sum > 0.f || sum != sum;    // (a query without keys: zeros, and -inf)
   if (a.lse && lane < rows) {
@@ -236,24 +262,24 @@ void prompt_attend_kernel(const AttendArgs<T> a) {
                     a.rest.token * int64_t(sizeof(T)), lane);
 }
 
-template <typename T, int DH, bool REST, int SW>
+template <typename T, int DH, bool REST, int SW, bool WIN>
 hipError_t launch_attend_shared(AttendArgs<T> a, hipStream_t st) {
   // a stage, and behind it another one or the waves' 32 queries each
   constexpr int row = Tile<T, DH>::kRow, stage = 2 * (SW > 1 ? 32 * SW : kKeys<T>) * row, waves = 4 * 32 * row, lds = stage + (stage > waves ? stage : waves);
   static_assert(SW == 1 || waves + 256 + 4 * (SW - 1) / SW * 256 * (DH / 2 + 2) <= lds, "the parts' sums");
-  const hipError_t e = allow_lds(&prompt_attend_kernel<T, DH, REST, SW>, lds);
+  const hipError_t e = allow_lds(&prompt_attend_kernel<T, DH, REST, SW, WIN>, lds);
   if (e != hipSuccess) return e;
   const long long blocks = blocks_at_most(a.s.q_start, a.s.batch, a.s.q_tokens, Shared<SW>::kRows) * a.s.heads;
   a.by_work = blocks < 1024;      // two for each place: beyond, what a sequence's blocks share counts for more (4096: 198 / 229 us)
-  hipLaunchKernelGGL((prompt_attend_kernel<T, DH, REST, SW>), dim3(unsigned(blocks)), dim3(256), lds, st, a);
+  hipLaunchKernelGGL((prompt_attend_kernel<T, DH, REST, SW, WIN>), dim3(unsigned(blocks)), dim3(256), lds, st, a);
   return hipGetLastError();
 }
 
-template <typename T, int DH, bool REST>
+template <typename T, int DH, bool REST, bool WIN>
 hipError_t launch_attend_prompt(const AttendArgs<T> &a, hipStream_t st) {
   if (share_queries<T>(a.s))
-    return launch_attend_shared<T, DH, REST, DH * sizeof(T) == 512 ? 2 : 4>(a, st);      // (as many as two stages leave LDS for)
-  return launch_attend_shared<T, DH, REST, 1>(a, st);
+    return launch_attend_shared<T, DH, REST, DH * sizeof(T) == 512 ? 2 : 4, WIN>(a, st);      // (as many as two stages leave LDS for)
+  return launch_attend_shared<T, DH, REST, 1, WIN>(a, st);
 }
 
 // ---- the attention every key received -----------------------------------------------------------------------------
@@ -420,7 +446,7 @@ hipError_t launch_scores(const ScoreArgs<T> &a, hipStream_t st) {
   return launch_scores_shared<T, DH, 1>(a, st);
 }
 
-template <typename T>
+template <typename T, bool WIN>
 int attend_typed(const adore_prompt_config &c, const PromptShape &s, const adore_rows *q, const adore_rows *k, const adore_rows *v,
                  const adore_rows *out, float *lse, const adore_rows *rest, hipStream_t st) {
   AttendArgs<T> a;
@@ -434,11 +460,11 @@ int attend_typed(const adore_prompt_config &c, const PromptShape &s, const adore
   hipError_t e;
   if constexpr (sizeof(T) == 2) {
     if (rest)
-      e = c.head_dim == 128 ? launch_attend_prompt<T, 128, true>(a, st) : launch_attend_prompt<T, 64, true>(a, st);
+      e = c.head_dim == 128 ? launch_attend_prompt<T, 128, true, WIN>(a, st) : launch_attend_prompt<T, 64, true, WIN>(a, st);
     else
-      e = c.head_dim == 128 ? launch_attend_prompt<T, 128, false>(a, st) : launch_attend_prompt<T, 64, false>(a, st);
+      e = c.head_dim == 128 ? launch_attend_prompt<T, 128, false, WIN>(a, st) : launch_attend_prompt<T, 64, false, WIN>(a, st);
   } else {
-    e = c.head_dim == 128 ? launch_attend_prompt<T, 128, false>(a, st) : launch_attend_prompt<T, 64, false>(a, st);
+    e = c.head_dim == 128 ? launch_attend_prompt<T, 128, false, WIN>(a, st) : launch_attend_prompt<T, 64, false, WIN>(a, st);
   }
   return e == hipSuccess ? ADORE_OK : ADORE_E_HIP;
 }
@@ -454,6 +480,18 @@ int scores_typed(const adore_prompt_config &c, const PromptShape &s, const adore
   a.scores = scores;
   const hipError_t e = c.head_dim == 128 ? launch_scores<T, 128>(a, st) : launch_scores<T, 64>(a, st);
   return e == hipSuccess ? ADORE_OK : ADORE_E_HIP;
+}
+
+template <bool WIN>
+int attend_prompts(const adore_prompt_config *cfg, const PromptShape &s, const adore_rows *q, const adore_rows *k, const adore_rows *v,
+                   const adore_rows *out, float *lse, const adore_rows *rest, void *hip_stream) {
+  if (!prompt_rows_ok(q, cfg->dtype) || !prompt_rows_ok(k, cfg->dtype) || !prompt_rows_ok(v, cfg->dtype) ||
+      !prompt_rows_ok(out, cfg->dtype) || (rest && (cfg->dtype != ADORE_BF16 || !prompt_rows_ok(rest, cfg->dtype))))
+    return ADORE_E_INVALID;
+  if (s.q_tokens == 0) return ADORE_OK;
+  const hipStream_t st = static_cast<hipStream_t>(hip_stream);
+  return cfg->dtype == ADORE_BF16 ? attend_typed<bf16_t, WIN>(*cfg, s, q, k, v, out, lse, rest, st)
+                                  : attend_typed<float, WIN>(*cfg, s, q, k, v, out, lse, rest, st);
 }
 
 }  // namespace
@@ -481,6 +519,16 @@ int prompt_shape(const adore_prompt_config *c, const int32_t *q_start, const int
   s->k_tokens = c->k_tokens;
   s->scale = c->scale > 0.f ? c->scale : 1.f / sqrtf(float(c->head_dim));
   s->scale_log2 = s->scale * kLog2e;
+  s->window = s->sinks = 0;
+  return ADORE_OK;
+}
+
+// A window, for a shape that prompt_shape filled in.  No sequence has more than 2^24 tokens: beyond, sums of positions would pass 32 bits.
+int window_shape(const adore_window *w, PromptShape *s) {
+  constexpr int kMost = 1 << 25;
+  if (!w || w->window < 1 || w->sinks < 0) return ADORE_E_INVALID;
+  s->window = w->window < kMost ? w->window : kMost;
+  s->sinks = w->sinks < kMost ? w->sinks : kMost;
   return ADORE_OK;
 }
 
@@ -498,17 +546,18 @@ extern "C" {
 int adore_prompt_attention(const adore_prompt_config *cfg, const int32_t *q_start, const int32_t *k_start, const adore_rows *q,
                            const adore_rows *k, const adore_rows *v, const adore_rows *out, float *lse, const adore_rows *rest,
                            void *hip_stream) {
-  using namespace adore;
-  PromptShape s;
-  const int rc = prompt_shape(cfg, q_start, k_start, &s);
-  if (rc != ADORE_OK) return rc;
-  if (!prompt_rows_ok(q, cfg->dtype) || !prompt_rows_ok(k, cfg->dtype) || !prompt_rows_ok(v, cfg->dtype) ||
-      !prompt_rows_ok(out, cfg->dtype) || (rest && (cfg->dtype != ADORE_BF16 || !prompt_rows_ok(rest, cfg->dtype))))
-    return ADORE_E_INVALID;
-  if (s.q_tokens == 0) return ADORE_OK;
-  const hipStream_t st = static_cast<hipStream_t>(hip_stream);
-  return cfg->dtype == ADORE_BF16 ? attend_typed<bf16_t>(*cfg, s, q, k, v, out, lse, rest, st)
-                                  : attend_typed<float>(*cfg, s, q, k, v, out, lse, rest, st);
+  adore::PromptShape s;
+  const int rc = adore::prompt_shape(cfg, q_start, k_start, &s);
+  return rc != ADORE_OK ? rc : adore::attend_prompts<false>(cfg, s, q, k, v, out, lse, rest, hip_stream);
+}
+
+int adore_window_attention(const adore_prompt_config *cfg, const adore_window *window, const int32_t *q_start, const int32_t *k_start,
+                           const adore_rows *q, const adore_rows *k, const adore_rows *v, const adore_rows *out, float *lse,
+                           const adore_rows *rest, void *hip_stream) {
+  adore::PromptShape s;
+  int rc = adore::prompt_shape(cfg, q_start, k_start, &s);
+  if (rc == ADORE_OK) rc = adore::window_shape(window, &s);
+  return rc != ADORE_OK ? rc : adore::attend_prompts<true>(cfg, s, q, k, v, out, lse, rest, hip_stream);
 }
 
 int adore_prompt_scores(const adore_prompt_config *cfg, const int32_t *q_start, const int32_t *k_start, const adore_rows *q,

@@ -29,6 +29,9 @@ struct BackwardArgs {
   const float *lse;
   float *delta;                              // laid out like lse
   bool by_work;
+  // With a window, if set: what queries that are further than the window from the first keys give those (SinkPlan).
+  float *sink_part;
+  int sink_chunk, sink_slots;
 };
 
 // The products of 32 rows of dO with those of out (and what its rounding left), as dO goes by on its way to LDS (carry_rows): delta of row
@@ -76,7 +79,7 @@ constexpr int kDqStage = 2 * (SW > 1 ? 32 * SW : kDqKeys<T>) * Tile<T, DH>::kRow
 template <typename T, int DH, int SW>
 constexpr int kDqWords = kDqStage<T, DH, SW> + (kDqStage<T, DH, SW> > 128 * Tile<T, DH>::kRow ? kDqStage<T, DH, SW> : 128 * Tile<T, DH>::kRow);
 
-template <typename T, int DH, int SW>
+template <typename T, int DH, int SW, bool WIN>
 __global__ __launch_bounds__(256) ADORE_WAVES(sizeof(T) == 4 || SW > 1 ? 1 : DH == 128 ? 2 : 3) void prompt_dq_kernel(const BackwardArgs<T> a) {
   constexpr int NT = 256, BQ = Shared<SW>::kRows, KT = SW > 1 ? 32 * SW : kDqKeys<T>, KB = SW > 1 ? 1 : KT / 32, DB = DH / 32, ST = DH / 16;
   typedef Tile<T, DH> L;
@@ -98,15 +101,22 @@ __global__ __launch_bounds__(256) ADORE_WAVES(sizeof(T) == 4 || SW > 1 ? 1 : DH 
   const int64_t row = int64_t(sq.q_first) + q0, es = int64_t(sizeof(T));
   const char *kp = reinterpret_cast<const char *>(a.k.p + sq.b * a.k.seq + sq.k_first * a.k.token + hk * a.k.head);
   const char *vp = reinterpret_cast<const char *>(a.v.p + sq.b * a.v.seq + sq.k_first * a.v.token + hk * a.v.head);
-  const int last = min(block * BQ + BQ, sq.nq) - 1 + off, tiles = last < 0 ? 0 : last / KT + 1;
+  const int last = min(block * BQ + BQ, sq.nq) - 1 + off, upto = last < 0 ? 0 : last / KT + 1;
+  const WindowTiles<KT> win(a.s, block * BQ + off, last, upto);     // (WIN)
+  const int tiles = WIN ? win.total : upto;
   const int mine = rows > 0 ? q0 + rows - 1 + off : -1, seen = q0 + c + off;
   const float scale = a.s.scale_log2;
   const uint32_t base0 = __builtin_amdgcn_readfirstlane(lds_offset(smem)), share = base0 + uint32_t(wave) * 1024u;
   Reader<T, DH> read(base0 + uint32_t(mate.part * 32 * L::kRow), lane);
   const TileLoad<T, DH, KT, NT> lk(a.k.token * es, tid), lv(a.v.token * es, tid);
+  if (WIN && win.sinks == 0) {
+    kp += win.skip * (KT * a.k.token * es);
+    vp += win.skip * (KT * a.v.token * es);
+  }
   if (tiles > 0) {
-    lk(kp, sq.nk, share);
-    lv(vp, sq.nk, share + kTile);
+    const int left = sq.nk - (WIN ? win.tile(0) * KT : 0);
+    lk(kp, left, share);
+    lv(vp, left, share + kTile);
   }
   unsigned char *own = smem + 2 * kTile + wave * (32 * L::kRow);    // the wave's share of the second stage
   const uint32_t own_ahead = uint32_t(2 * kTile + (wave - mate.part) * (32 * L::kRow));
@@ -152,21 +162,22 @@ __global__ __launch_bounds__(256) ADORE_WAVES(sizeof(T) == 4 || SW > 1 ? 1 : DH 
   const int hidden = max(block * BQ + off + 1, 0) / KT;    // the first tile that not all of the workgroup's queries see all of
   int from = INT_MAX;                                      // first key of the first such tile where an element of K is not finite
   for (int it = 0; it < tiles; ++it) {
-    const int k0 = it * KT + mate.part * 32;
+    const int tile = WIN ? win.tile(it) : it, k0 = tile * KT + mate.part * 32;
     arrived();
     __syncthreads();
-    if (it >= hidden) {
+    if (tile >= hidden || (WIN && tile * KT < win.partial && tile * KT + KT > a.s.sinks)) {
       const bool found = any_of_four(find_not_finite<T, DH, KT, NT>(smem + (it & 1) * 2 * kTile), reinterpret_cast<int *>(smem + kDqWords<T, DH, SW>));
-      if (__builtin_amdgcn_readfirstlane(found)) from = min(from, it * KT);
+      if (__builtin_amdgcn_readfirstlane(found)) from = min(from, tile * KT);
     }
     if (it + 1 < tiles) {
       const uint32_t next = share + uint32_t(~it & 1) * uint32_t(2 * kTile);
-      kp += KT * a.k.token * es;
-      vp += KT * a.v.token * es;
-      lk(kp, sq.nk - (it + 1) * KT, next);
-      lv(vp, sq.nk - (it + 1) * KT, next + kTile);
+      const int following = WIN ? win.tile(it + 1) : it + 1;
+      kp += (WIN ? following - tile : 1) * (KT * a.k.token * es);
+      vp += (WIN ? following - tile : 1) * (KT * a.v.token * es);
+      lk(kp, sq.nk - following * KT, next);
+      lv(vp, sq.nk - following * KT, next + kTile);
     }
-    if (k0 > mine || it * KT >= from) {
+    if (k0 > mine || tile * KT >= from || (WIN && k0 + 32 * KB <= q0 + off - a.s.window + 1 && k0 >= a.s.sinks)) {
       read.move(it & 1 ? uint32_t(-2 * kTile) : uint32_t(2 * kTile));
       continue;
     }
@@ -189,6 +200,14 @@ __global__ __launch_bounds__(256) ADORE_WAVES(sizeof(T) == 4 || SW > 1 ? 1 : DH 
         for (int r = 0; r < 16; ++r)
           if (k0 + kb * 32 + 8 * (r >> 2) + 4 * h + (r & 3) > seen) s[r] = -INFINITY;
       }
+      const bool behind = WIN && k0 + kb * 32 <= q0 + 31 + off - a.s.window && k0 + kb * 32 + 32 > a.s.sinks;     // ... because they are too far back
+      if (behind) {
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          const int key = k0 + kb * 32 + 8 * (r >> 2) + 4 * h + (r & 3);
+          if (key <= seen - a.s.window && key >= a.s.sinks) s[r] = -INFINITY;
+        }
+      }
 #pragma unroll
       for (int t = 0; t < ST; ++t) {
         pin();
@@ -202,6 +221,13 @@ __global__ __launch_bounds__(256) ADORE_WAVES(sizeof(T) == 4 || SW > 1 ? 1 : DH 
 #pragma unroll
         for (int r = 0; r < 16; ++r)
           if (k0 + kb * 32 + 8 * (r >> 2) + 4 * h + (r & 3) > seen) g[r] = delta;
+      }
+      if (behind) {
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          const int key = k0 + kb * 32 + 8 * (r >> 2) + 4 * h + (r & 3);
+          if (key <= seen - a.s.window && key >= a.s.sinks) g[r] = delta;
+        }
       }
 #pragma unroll
       for (int r = 0; r < 8; ++r) g[r] = s[r] * (g[r] - delta);
@@ -245,6 +271,7 @@ __global__ __launch_bounds__(256) ADORE_WAVES(sizeof(T) == 4 || SW > 1 ? 1 : DH 
   const T *const dr = a.d_out.p + sq.b * a.d_out.seq + query * a.d_out.token + head * a.d_out.head + 4 * h;
 #pragma unroll 1
   for (int i = from; i <= mine; ++i) {
+    if (WIN && i >= a.s.sinks) i = max(i, win.low);            // (keys in between nobody sees)
     const int64_t key = int64_t(sq.k_first) + i;
     const T *const kr = a.k.p + sq.b * a.k.seq + key * a.k.token + hk * a.k.head + 4 * h;
     const T *const vr = a.v.p + sq.b * a.v.seq + key * a.v.token + hk * a.v.head + 4 * h;
@@ -259,7 +286,7 @@ __global__ __launch_bounds__(256) ADORE_WAVES(sizeof(T) == 4 || SW > 1 ? 1 : DH 
     w = add_lane_xor<32>(w);
     x = add_lane_xor<32>(x);
     x = __builtin_amdgcn_exp2f(fmaf(w, scale, -lse)) * (x - delta);
-    if (i <= seen) {
+    if (WIN ? in_window(a.s, i, seen) : i <= seen) {
 #pragma unroll
       for (int db = 0; db < DB; ++db)
 #pragma unroll
@@ -280,7 +307,42 @@ __global__ __launch_bounds__(256) ADORE_WAVES(sizeof(T) == 4 || SW > 1 ? 1 : DH 
 template <typename T, int DH, int SW>
 constexpr bool kValuesInRegisters = SW > 1 && DH * sizeof(T) == 512;
 
-template <typename T, int DH, int SW>
+// With a window a block of keys is seen by few queries, but the first keys by all that follow: one workgroup would go over a whole prompt
+// while the others go over a window.  So the queries behind the window (p - j >= window) are cut into chunks, each a workgroup's, whose
+// sums for 32 first keys (a wave's registers, fp32) go to memory; the workgroup of the block that holds the keys adds them to its own.
+// A sequence's chunks: n places from `first` on.  find_chunk: a place's sequence and chunk (all 64 lanes of a wave call it together).
+struct Chunks {
+  int first, n;
+  __device__ __forceinline__ Chunks(const PromptShape &a, const Sequence &s, int chunk) {
+    n = s.nk > a.window ? (s.nq + chunk - 1) / chunk : 0;      // (else no query is further than the window from any key)
+    // packed: of the sequences that have chunks no two are in the same run of window + 1 keys (whatever the starts hold: no place is
+    // beyond SinkPlan::slots)
+    first = a.q_start ? s.q_first / chunk + min(s.b, s.k_first / (a.window + 1)) : s.b * ((a.q_tokens + chunk - 1) / chunk);
+  }
+};
+__device__ __forceinline__ bool find_chunk(const PromptShape &a, int place, int chunk, Sequence &s, int &at) {
+  const int lane = threadIdx.x & 63;
+  for (int b0 = 0; b0 < a.batch; b0 += 64) {
+    const int b = min(b0 + lane, a.batch - 1);
+    const Chunks mine(a, sequence_at(a, b), chunk);
+    const uint64_t here = __builtin_amdgcn_ballot_w64(place >= mine.first && place < mine.first + mine.n);
+    if (here) {
+      s = sequence_at(a, __builtin_amdgcn_readfirstlane(min(b0 + int(__builtin_ctzll(here)), a.batch - 1)));
+      at = place - Chunks(a, s, chunk).first;
+      return true;
+    }
+  }
+  return false;
+}
+// The sums of place `place`, kv head hk, for keys 32 i .. 32 i + 31: dk's registers of 64 lanes, then dv's.
+template <int DH>
+__device__ __forceinline__ size_t sink_sums(const PromptShape &a, int place, int hk, int i) {
+  return ((size_t(place) * a.kv_heads + hk) * ((min(a.sinks, a.k_tokens) + 63) / 64 * 2) + i) * (64 * DH);
+}
+
+enum { kCausal, kWindow, kSinks };           // every pair; pairs in the window; the others, which the first keys have
+
+template <typename T, int DH, int SW, int MODE>
 __global__ __launch_bounds__(256) ADORE_WAVES(sizeof(T) == 2 && SW == 1 ? 2 : 1) void prompt_dkv_kernel(const BackwardArgs<T> a) {
   constexpr int NT = 256, BK = Shared<SW>::kRows, QT = 32 * SW, DB = DH / 32, ST = DH / 16;
   typedef Tile<T, DH> L;
@@ -292,8 +354,14 @@ __global__ __launch_bounds__(256) ADORE_WAVES(sizeof(T) == 2 && SW == 1 ? 2 : 1)
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), c = lane & 31, h = lane >> 5;
   const int hk = blockIdx.x % a.s.kv_heads;
   Sequence sq;
-  int block;
-  if (!find_block<BK, false>(a.s, blockIdx.x / a.s.kv_heads, a.by_work, sq, block)) {
+  int block, place = 0, chunk = 0;
+  if constexpr (MODE == kSinks) {
+    const int item = blockIdx.x / a.s.kv_heads;
+    block = item / a.sink_slots;
+    place = item - block * a.sink_slots;
+    if (!find_chunk(a.s, place, a.sink_chunk, sq, chunk)) return;
+    chunk *= a.sink_chunk;
+  } else if (!find_block<BK, false>(a.s, blockIdx.x / a.s.kv_heads, a.by_work, sq, block)) {
     const SpareRows spare = spare_rows<BK>(a.s.k_start, a.s.batch, a.s.k_tokens, block);
     zero_rows<T, DH>(a.dk, hk, spare, tid, NT);
     zero_rows<T, DH>(a.dv, hk, spare, tid, NT);
@@ -307,18 +375,39 @@ __global__ __launch_bounds__(256) ADORE_WAVES(sizeof(T) == 2 && SW == 1 ? 2 : 1)
   // Queries that some of the block's keys are hidden from, if one of them is not finite, or its weights are not numbers (log-sum-exp or
   // delta tells), are added one by one when the tiles are done.  So are those of a last tile that is not full: the rows it lacks repeat
   // the last query's with weights of 0, which do not hide it where it is not finite.
+  // (With a window they are all added one by one then: those that some of the keys are too far behind for too.)
   const int base = max(-off, 0), unseen = block * BK - off - base;       // (of the block's first key, from base on)
-  const int diagonal = base + max(unseen, 0) / QT * QT, behind = min(base + (max(unseen + BK - 1, 0) + QT - 1) / QT * QT, sq.nq);
-  const int end = sq.nq > behind ? base + (sq.nq - base) / QT * QT : sq.nq;
+  const int sinks = MODE == kWindow ? (a.sink_part ? 0 : a.s.sinks) : a.s.sinks;     // whose queries behind the window are this workgroup's
+  const bool all = MODE == kCausal || (MODE == kWindow && block * BK < sinks);     // every query from the diagonal on
+  const int diagonal = MODE == kSinks ? chunk + max(block * BK + a.s.window - off - chunk, 0) / QT * QT : base + max(unseen, 0) / QT * QT;
+  const int limit = MODE == kSinks ? min(chunk + a.sink_chunk, sq.nq)
+                                   : all ? sq.nq : min(sq.nq, max(block * BK + BK - 1 + a.s.window - off, diagonal));     // of those the last one
+  const int tiled = MODE == kCausal ? sq.nq : min(diagonal + (max(limit - diagonal, 0) + QT - 1) / QT * QT, sq.nq);    // ... with those that fill its tile
+  const int behind = MODE == kCausal ? min(base + (max(unseen + BK - 1, 0) + QT - 1) / QT * QT, sq.nq) : limit;
+  const int end = MODE == kCausal ? (sq.nq > behind ? base + (sq.nq - base) / QT * QT : sq.nq) : limit;
+  auto sees = [&](int key, int position) {                  // of a pair that this workgroup goes over
+    if constexpr (MODE == kCausal) return key <= position;
+    if constexpr (MODE == kSinks) return key < sinks && position - key >= a.s.window;
+    return key <= position && (position - key < a.s.window || key < sinks);
+  };
   bool odd = false;
   for (int j = 0; j < a.s.group; ++j) {
     const size_t row0 = row_value(a.s.q_start != nullptr, sq.b, sq.q_first, a.s.q_tokens, a.s.heads, hk * a.s.group + j);
     auto look = [&](int i) { odd |= !(subtrahend(a.lse[row0 + i]) < INFINITY && fabsf(a.delta[row0 + i]) < INFINITY); };
-    for (int i = diagonal + tid; i < behind; i += NT) look(i);
-    if (end < sq.nq && tid == NT - 1) look(sq.nq - 1);
+    if constexpr (MODE == kCausal) {
+      for (int i = diagonal + tid; i < behind; i += NT) look(i);
+      if (end < sq.nq && tid == NT - 1) look(sq.nq - 1);
+    } else {
+      // on the diagonal, and from the first that is too far from some of the keys
+      const int near = MODE == kSinks ? diagonal : min(base + max(unseen + BK - 1, 0), tiled);
+      const int far = MODE == kSinks ? diagonal : max(block * BK + a.s.window - off, near);
+      for (int i = diagonal + tid; i < near; i += NT) look(i);
+      for (int i = far + tid; i < tiled; i += NT) look(i);
+      if (tiled == sq.nq && diagonal < tiled && tid == NT - 1) look(sq.nq - 1);
+    }
   }
   odd = any_of_four(__builtin_amdgcn_ballot_w64(odd) != 0, reinterpret_cast<int *>(s_delta + 2 * QT));
-  const int first = odd ? behind : diagonal, stop = odd ? end : sq.nq;
+  const int first = odd ? behind : diagonal, stop = odd ? end : MODE == kCausal ? sq.nq : limit;
   const int per = first < stop ? (stop - first + QT - 1) / QT : 0, tiles = per * a.s.group;
   const float scale = a.s.scale_log2;
   const bool packed = a.s.q_start != nullptr;
@@ -399,10 +488,13 @@ __global__ __launch_bounds__(256) ADORE_WAVES(sizeof(T) == 2 && SW == 1 ? 2 : 1)
       if (!VR && t >= ST - 4) y[t - ST + 4] = read.by_row(va, 0, t - ST + 4);
     }
     pin();
-    if (q0 + off < k0 + 31) {                               // some of the queries do not see some of the wave's keys
+    // some of the queries do not see some of the wave's keys
+    const bool partial = MODE == kSinks ? k0 + 31 >= sinks || q0 + off - k0 - 31 < a.s.window
+                                        : q0 + off < k0 + 31 || (MODE == kWindow && q0 + off + 31 - k0 >= a.s.window && k0 + 31 >= sinks);
+    if (partial) {
 #pragma unroll
       for (int r = 0; r < 16; ++r)
-        if (k0 + c > q0 + 8 * (r >> 2) + 4 * h + (r & 3) + off) s[r] = -INFINITY;
+        if (!sees(k0 + c, q0 + 8 * (r >> 2) + 4 * h + (r & 3) + off)) s[r] = -INFINITY;
     }
     auto next_of = [&](int i) {                             // columns in the order of the last four groups of products
       const int db = i % DB, t = i / DB;
@@ -422,6 +514,11 @@ __global__ __launch_bounds__(256) ADORE_WAVES(sizeof(T) == 2 && SW == 1 ? 2 : 1)
       }
     }
     pin();
+    if (MODE != kCausal && partial) {                       // (a key that nobody sees may hold anything)
+#pragma unroll
+      for (int r = 0; r < 16; ++r)
+        if (!sees(k0 + c, q0 + 8 * (r >> 2) + 4 * h + (r & 3) + off)) g[r] = rows_delta[8 * (r >> 2) + (r & 3)];
+    }
     // dv takes p; meanwhile g becomes p (g - delta)
     auto scaled = [&](int r4) {
       const f32x4 delta = *reinterpret_cast<const f32x4 *>(rows_delta + 8 * r4);
@@ -480,7 +577,7 @@ __global__ __launch_bounds__(256) ADORE_WAVES(sizeof(T) == 2 && SW == 1 ? 2 : 1)
     for (int j = 0; j < a.s.group; ++j) {
       const int head = hk * a.s.group + j;
       const size_t row0 = row_value(packed, sq.b, sq.q_first, a.s.q_tokens, a.s.heads, head);
-      for (int i = diagonal < behind ? diagonal : end; i < sq.nq; i = i + 1 == behind ? end : i + 1) {
+      for (int i = diagonal < behind ? diagonal : end; i < (MODE == kCausal ? sq.nq : limit); i = i + 1 == behind ? end : i + 1) {
         const int64_t query = int64_t(sq.q_first) + i;
         const T *qr = a.q.p + sq.b * a.q.seq + query * a.q.token + head * a.q.head + 4 * h;
         const T *dr = a.d_out.p + sq.b * a.d_out.seq + query * a.d_out.token + head * a.d_out.head + 4 * h;
@@ -496,7 +593,7 @@ __global__ __launch_bounds__(256) ADORE_WAVES(sizeof(T) == 2 && SW == 1 ? 2 : 1)
         x = add_lane_xor<32>(x);
         w = __builtin_amdgcn_exp2f(fmaf(w, scale, -subtrahend(a.lse[row0 + i])));
         x = w * (x - a.delta[row0 + i]);
-        if (k0 + c <= i + off) {
+        if (sees(k0 + c, i + off)) {
 #pragma unroll
           for (int db = 0; db < DB; ++db)
 #pragma unroll
@@ -510,42 +607,63 @@ __global__ __launch_bounds__(256) ADORE_WAVES(sizeof(T) == 2 && SW == 1 ? 2 : 1)
       }
     }
   }
+  if constexpr (MODE == kSinks) {
+    float *const to = a.sink_part + sink_sums<DH>(a.s, place, hk, k0 / 32);
+    put_sums(dk, to, lane);
+    put_sums(dv, to + 32 * DH, lane);
+    return;
+  }
+  if (MODE == kWindow && a.sink_part && k0 < a.s.sinks) {
+    const Chunks chunks(a.s, sq, a.sink_chunk);
+    for (int i = chunks.first; i < chunks.first + chunks.n; ++i) {
+      const float *const sums = a.sink_part + sink_sums<DH>(a.s, i, hk, k0 / 32);
+      add_sums(dk, sums, 1.f, lane);
+      add_sums(dv, sums + 32 * DH, 1.f, lane);
+    }
+  }
   store_rows<T, DH>(dk, a.s.scale, own, reinterpret_cast<char *>(a.dk.p + sq.b * a.dk.seq + row * a.dk.token + hk * a.dk.head), a.dk.token * es, rows,
                     nullptr, 0, lane);
   store_rows<T, DH>(dv, 1.f, own, reinterpret_cast<char *>(a.dv.p + sq.b * a.dv.seq + row * a.dv.token + hk * a.dv.head), a.dv.token * es, rows,
                     nullptr, 0, lane);
 }
 
-template <typename T, int DH, int SW>
+template <typename T, int DH, int SW, bool WIN>
 hipError_t launch_dq(BackwardArgs<T> a, hipStream_t st) {
   constexpr int lds = kDqWords<T, DH, SW> + 16;
   static_assert(SW == 1 || 4 * (SW - 1) / SW * 256 * (DH / 2) <= kDqStage<T, DH, SW>, "the parts' sums lie in the first stage");
-  const hipError_t e = allow_lds(&prompt_dq_kernel<T, DH, SW>, lds);
+  const hipError_t e = allow_lds(&prompt_dq_kernel<T, DH, SW, WIN>, lds);
   if (e != hipSuccess) return e;
   const long long blocks = blocks_at_most(a.s.q_start, a.s.batch, a.s.q_tokens, Shared<SW>::kRows) * a.s.heads;
   a.by_work = blocks < 1024;
-  hipLaunchKernelGGL((prompt_dq_kernel<T, DH, SW>), dim3(unsigned(blocks)), dim3(256), lds, st, a);
+  hipLaunchKernelGGL((prompt_dq_kernel<T, DH, SW, WIN>), dim3(unsigned(blocks)), dim3(256), lds, st, a);
   return hipGetLastError();
 }
 
-template <typename T, int DH, int SW>
+template <typename T, int DH, int SW, int MODE>
 hipError_t launch_dkv(BackwardArgs<T> a, hipStream_t st) {
   // two stages of Q and dO, V, a stage's log-sum-exps and deltas twice, four words
   constexpr int rows = 4 * 32 * SW + (kValuesInRegisters<T, DH, SW> ? 0 : Shared<SW>::kRows), lds = rows * Tile<T, DH>::kRow + 4 * 32 * SW * 4 + 16;
-  const hipError_t e = allow_lds(&prompt_dkv_kernel<T, DH, SW>, lds);
+  const hipError_t e = allow_lds(&prompt_dkv_kernel<T, DH, SW, MODE>, lds);
   if (e != hipSuccess) return e;
-  const long long blocks = blocks_at_most(a.s.k_start, a.s.batch, a.s.k_tokens, Shared<SW>::kRows) * a.s.kv_heads;
+  const int sinks = a.s.sinks < a.s.k_tokens ? a.s.sinks : a.s.k_tokens;
+  const long long items = MODE == kSinks ? (long long)a.sink_slots * ((sinks + Shared<SW>::kRows - 1) / Shared<SW>::kRows)
+                                         : blocks_at_most(a.s.k_start, a.s.batch, a.s.k_tokens, Shared<SW>::kRows);
+  const long long blocks = items * a.s.kv_heads;
   a.by_work = blocks < 2048;   // 1024, with 4 to 64 tiles of 4 heads each: 796 -> 610 us
-  hipLaunchKernelGGL((prompt_dkv_kernel<T, DH, SW>), dim3(unsigned(blocks)), dim3(256), lds, st, a);
+  hipLaunchKernelGGL((prompt_dkv_kernel<T, DH, SW, MODE>), dim3(unsigned(blocks)), dim3(256), lds, st, a);
   return hipGetLastError();
 }
 
-template <typename T, int DH>
+template <typename T, int DH, bool WIN>
 hipError_t launch_backward(const BackwardArgs<T> &a, hipStream_t st) {
   constexpr int SW = DH * sizeof(T) == 512 ? 2 : 4;  // (as many as two stages leave LDS for)
+  constexpr int MODE = WIN ? kWindow : kCausal;
   hipError_t e = hipSuccess;
-  if (a.s.q_tokens > 0) e = share_queries<T>(a.s) ? launch_dq<T, DH, SW>(a, st) : launch_dq<T, DH, 1>(a, st);
-  if (e == hipSuccess && a.s.k_tokens > 0) e = share_keys<T>(a.s) ? launch_dkv<T, DH, SW>(a, st) : launch_dkv<T, DH, 1>(a, st);
+  if (a.s.q_tokens > 0) e = share_queries<T>(a.s) ? launch_dq<T, DH, SW, WIN>(a, st) : launch_dq<T, DH, 1, WIN>(a, st);
+  if constexpr (WIN) {
+    if (e == hipSuccess && a.sink_part) e = launch_dkv<T, DH, SW, kSinks>(a, st);
+  }
+  if (e == hipSuccess && a.s.k_tokens > 0) e = share_keys<T>(a.s) ? launch_dkv<T, DH, SW, MODE>(a, st) : launch_dkv<T, DH, 1, MODE>(a, st);
   return e;
 }
 
@@ -554,7 +672,33 @@ size_t delta_bytes(const adore_prompt_config &c, bool packed) {
   return (n * sizeof(float) + 255) / 256 * 256 + 256;    // never 0: that says "not taken"
 }
 
-template <typename T>
+// How the queries behind the window of the first keys are cut (slots 0: not at all, the workgroup of a block of keys goes over them).
+struct SinkPlan {
+  int chunk, slots;
+  size_t bytes;
+};
+SinkPlan plan_sinks(const PromptShape &s, int head_dim, bool packed) {
+  SinkPlan p = {0, 0, 0};
+  const long long sinks = s.sinks < s.k_tokens ? s.sinks : s.k_tokens, groups = (sinks + 63) / 64 * 2;
+  const long long queries = (long long)s.q_tokens * (packed ? 1 : s.batch);
+  if (sinks == 0 || s.k_tokens <= s.window) return p;
+  if (queries * s.group < 2048) return p;    // (a launch more)
+  // 512 workgroups, chunks of 256 queries or more
+  long long chunk = (queries * s.kv_heads * groups / 2 / 512 + 127) / 128 * 128;
+  if (chunk < 256) chunk = 256;
+  long long longest = s.q_tokens;
+  if (chunk > longest) chunk = (longest + 127) / 128 * 128;
+  const long long long_ones = (long long)s.k_tokens / (s.window + 1);
+  const long long slots = packed ? s.q_tokens / chunk + (s.batch < long_ones ? s.batch : long_ones) + 1 : s.batch * ((s.q_tokens + chunk - 1) / chunk);
+  const long long bytes = slots * s.kv_heads * groups * 64 * head_dim * 4;
+  if (bytes > (256ll << 20)) return p;       // (many short sequences: there is little to cut)
+  p.chunk = int(chunk);
+  p.slots = int(slots);
+  p.bytes = size_t(bytes);
+  return p;
+}
+
+template <typename T, bool WIN>
 int backward_typed(const adore_prompt_config &c, const PromptShape &s, const adore_rows *d_out, const adore_rows *q, const adore_rows *k,
                    const adore_rows *v, const adore_rows *out, const adore_rows *rest, const float *lse, const adore_rows *dq,
                    const adore_rows *dk, const adore_rows *dv, void *workspace, hipStream_t st) {
@@ -571,8 +715,36 @@ int backward_typed(const adore_prompt_config &c, const PromptShape &s, const ado
   a.dv = rows_of<T>(dv);
   a.lse = lse;
   a.delta = static_cast<float *>(workspace);
-  const hipError_t e = c.head_dim == 128 ? launch_backward<T, 128>(a, st) : launch_backward<T, 64>(a, st);
+  a.sink_part = nullptr;
+  a.sink_chunk = a.sink_slots = 0;
+  if constexpr (WIN) {
+    const SinkPlan p = plan_sinks(s, c.head_dim, s.q_start != nullptr);
+    if (p.slots > 0) {
+      a.sink_part = reinterpret_cast<float *>(static_cast<char *>(workspace) + delta_bytes(c, s.q_start != nullptr));
+      a.sink_chunk = p.chunk;
+      a.sink_slots = p.slots;
+    }
+  }
+  const hipError_t e = c.head_dim == 128 ? launch_backward<T, 128, WIN>(a, st) : launch_backward<T, 64, WIN>(a, st);
   return e == hipSuccess ? ADORE_OK : ADORE_E_HIP;
+}
+
+size_t backward_bytes(const adore_prompt_config &c, const PromptShape &s, bool packed, bool window) {
+  return delta_bytes(c, packed) + (window ? plan_sinks(s, c.head_dim, packed).bytes : 0);
+}
+
+template <bool WIN>
+int backward_prompts(const adore_prompt_config *cfg, const PromptShape &s, const adore_rows *d_out, const adore_rows *q, const adore_rows *k,
+                     const adore_rows *v, const adore_rows *out, const adore_rows *rest, const float *lse, const adore_rows *dq,
+                     const adore_rows *dk, const adore_rows *dv, void *workspace, size_t workspace_bytes, void *hip_stream) {
+  for (const adore_rows *r : {d_out, q, k, v, out, dq, dk, dv})
+    if (!prompt_rows_ok(r, cfg->dtype)) return ADORE_E_INVALID;
+  if (!lse || !workspace || (rest && (cfg->dtype != ADORE_BF16 || !prompt_rows_ok(rest, cfg->dtype)))) return ADORE_E_INVALID;
+  if (workspace_bytes < backward_bytes(*cfg, s, s.q_start != nullptr, WIN) || (reinterpret_cast<uintptr_t>(workspace) & 255) != 0)
+    return ADORE_E_WORKSPACE;
+  const hipStream_t st = static_cast<hipStream_t>(hip_stream);
+  return cfg->dtype == ADORE_BF16 ? backward_typed<bf16_t, WIN>(*cfg, s, d_out, q, k, v, out, rest, lse, dq, dk, dv, workspace, st)
+                                  : backward_typed<float, WIN>(*cfg, s, d_out, q, k, v, out, rest, lse, dq, dk, dv, workspace, st);
 }
 
 }  // namespace
@@ -585,24 +757,35 @@ size_t adore_prompt_backward_workspace_bytes(const adore_prompt_config *cfg, int
   adore::PromptShape s;
   const int32_t some = 0, *start = packed ? &some : nullptr;   // (not read: the checks look at whether there are starts)
   if (adore::prompt_shape(cfg, start, start, &s) != ADORE_OK) return 0;
-  return adore::delta_bytes(*cfg, packed != 0);
+  return adore::backward_bytes(*cfg, s, packed != 0, false);
 }
 
 int adore_prompt_attention_backward(const adore_prompt_config *cfg, const int32_t *q_start, const int32_t *k_start, const adore_rows *d_out,
                                     const adore_rows *q, const adore_rows *k, const adore_rows *v, const adore_rows *out,
                                     const adore_rows *rest, const float *lse, const adore_rows *dq, const adore_rows *dk, const adore_rows *dv,
                                     void *workspace, size_t workspace_bytes, void *hip_stream) {
-  using namespace adore;
-  PromptShape s;
-  const int rc = prompt_shape(cfg, q_start, k_start, &s);
-  if (rc != ADORE_OK) return rc;
-  for (const adore_rows *r : {d_out, q, k, v, out, dq, dk, dv})
-    if (!prompt_rows_ok(r, cfg->dtype)) return ADORE_E_INVALID;
-  if (!lse || !workspace || (rest && (cfg->dtype != ADORE_BF16 || !prompt_rows_ok(rest, cfg->dtype)))) return ADORE_E_INVALID;
-  if (workspace_bytes < delta_bytes(*cfg, q_start != nullptr) || (reinterpret_cast<uintptr_t>(workspace) & 255) != 0) return ADORE_E_WORKSPACE;
-  const hipStream_t st = static_cast<hipStream_t>(hip_stream);
-  return cfg->dtype == ADORE_BF16 ? backward_typed<bf16_t>(*cfg, s, d_out, q, k, v, out, rest, lse, dq, dk, dv, workspace, st)
-                                  : backward_typed<float>(*cfg, s, d_out, q, k, v, out, rest, lse, dq, dk, dv, workspace, st);
+  adore::PromptShape s;
+  const int rc = adore::prompt_shape(cfg, q_start, k_start, &s);
+  return rc != ADORE_OK ? rc
+                        : adore::backward_prompts<false>(cfg, s, d_out, q, k, v, out, rest, lse, dq, dk, dv, workspace, workspace_bytes, hip_stream);
+}
+
+size_t adore_window_backward_workspace_bytes(const adore_prompt_config *cfg, const adore_window *window, int32_t packed) {
+  adore::PromptShape s;
+  const int32_t some = 0, *start = packed ? &some : nullptr;
+  if (adore::prompt_shape(cfg, start, start, &s) != ADORE_OK || adore::window_shape(window, &s) != ADORE_OK) return 0;
+  return adore::backward_bytes(*cfg, s, packed != 0, true);
+}
+
+int adore_window_attention_backward(const adore_prompt_config *cfg, const adore_window *window, const int32_t *q_start, const int32_t *k_start,
+                                    const adore_rows *d_out, const adore_rows *q, const adore_rows *k, const adore_rows *v,
+                                    const adore_rows *out, const adore_rows *rest, const float *lse, const adore_rows *dq,
+                                    const adore_rows *dk, const adore_rows *dv, void *workspace, size_t workspace_bytes, void *hip_stream) {
+  adore::PromptShape s;
+  int rc = adore::prompt_shape(cfg, q_start, k_start, &s);
+  if (rc == ADORE_OK) rc = adore::window_shape(window, &s);
+  return rc != ADORE_OK ? rc
+                        : adore::backward_prompts<true>(cfg, s, d_out, q, k, v, out, rest, lse, dq, dk, dv, workspace, workspace_bytes, hip_stream);
 }
 
 }  // extern "C"

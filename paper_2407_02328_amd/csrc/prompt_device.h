@@ -44,10 +44,12 @@ struct PromptShape {
   const int32_t *q_start, *k_start;   // [batch + 1], or null: every sequence has q_tokens / k_tokens
   int batch, heads, kv_heads, group, q_tokens, k_tokens;
   float scale, scale_log2;            // and times log2(e)
+  int window, sinks;                  // of kernels with a window: a query sees its last `window` keys and the first `sinks`
 };
 
 int prompt_shape(const adore_prompt_config *c, const int32_t *q_start, const int32_t *k_start, PromptShape *s);
 bool prompt_rows_ok(const adore_rows *r, int dtype);
+int window_shape(const adore_window *w, PromptShape *s);
 
 struct Sequence {
   int b;
@@ -168,6 +170,27 @@ __device__ __forceinline__ void zero_rows(const Rows<T> &to, int head, const Spa
   for (int i = tid; i < spare.n * kChunks; i += threads)
     *reinterpret_cast<u32x4 *>(reinterpret_cast<char *>(to.p + int64_t(spare.at(i / kChunks)) * to.token + head * to.head) + i % kChunks * 16) =
         u32x4{0, 0, 0, 0};
+}
+
+// ---- windows ----
+// The query at position p (its index + nk - nq) sees keys j <= p with p - j < window or j < sinks.  What a workgroup of queries goes over: the
+// tiles that hold first keys, then those from its first query's window on; tiles in between are left out.
+template <int KT>
+struct WindowTiles {
+  int sinks, skip, total;                     // tiles with first keys, tiles left out behind them, tiles gone over
+  int low;                                    // the first key that not only a first one may be: from here on windows begin
+  int partial;                                // keys in front of it (that are no sinks) some query of the workgroup does not see
+  __device__ __forceinline__ WindowTiles(const PromptShape &a, int first, int last, int tiles) {
+    sinks = min((a.sinks + KT - 1) / KT, tiles);
+    low = max(first - a.window + 1, 0);
+    skip = max(low / KT - sinks, 0);
+    total = tiles - skip;
+    partial = last - a.window + 1;
+  }
+  __device__ __forceinline__ int tile(int it) const { return it < sinks ? it : it + skip; }
+};
+__device__ __forceinline__ bool in_window(const PromptShape &a, int key, int position) {
+  return key <= position && (position - key < a.window || key < a.sinks);
 }
 
 // Where fp32 values per row of a sequence and head are (lse, scores, ...): [heads][packed rows], or [batch][heads][tokens].
@@ -442,12 +465,14 @@ __device__ __forceinline__ bool any_of_four(bool mine, int *s) {
   return (s[0] | s[1] | s[2] | s[3]) != 0;
 }
 
-// acc (element 32 db + .., column c) += what is not finite of rows from .. to - 1 at `rows`, up to the last that the lane's column sees.
+// acc (element 32 db + .., column c) += what is not finite of rows from .. to - 1 at `rows`, from the first to the last that the lane's
+// column sees.
 template <typename T, int DH>
-__device__ __forceinline__ void add_not_finite(f32x16 (&acc)[DH / 32], const char *rows, int64_t stride, int from, int to, int seen, int lane) {
+__device__ __forceinline__ void add_not_finite(f32x16 (&acc)[DH / 32], const char *rows, int64_t stride, int from, int to, int first, int seen,
+                                               int lane) {
 #pragma unroll 1
   for (int i = from; i < to; ++i) {
-    if (i > seen) continue;
+    if (i < first || i > seen) continue;
     const T *row = reinterpret_cast<const T *>(rows + i * stride) + 4 * (lane >> 5);
 #pragma unroll
     for (int db = 0; db < DH / 32; ++db)
