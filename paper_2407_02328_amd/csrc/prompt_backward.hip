@@ -385,10 +385,12 @@ __global__ __launch_bounds__(256) ADORE_WAVES(sizeof(T) == 2 && SW == 1 ? 2 : 1)
   const int tiled = MODE == kCausal ? sq.nq : min(diagonal + (max(limit - diagonal, 0) + QT - 1) / QT * QT, sq.nq);    // ... with those that fill its tile
   const int behind = MODE == kCausal ? min(base + (max(unseen + BK - 1, 0) + QT - 1) / QT * QT, sq.nq) : limit;
   const int end = MODE == kCausal ? (sq.nq > behind ? base + (sq.nq - base) / QT * QT : sq.nq) : limit;
-  auto sees = [&](int key, int position) {                  // of a pair that this workgroup goes over
-    if constexpr (MODE == kCausal) return key <= position;
-    if constexpr (MODE == kSinks) return key < sinks && position - key >= a.s.window;
-    return key <= position && (position - key < a.s.window || key < sinks);
+  // Of the pairs of the lane's key: those whose query is at least (kSinks), or less than this far behind it.
+  const int reach = MODE == kSinks ? (k0 + c < sinks ? a.s.window : INT_MAX) : k0 + c < sinks ? INT_MAX : a.s.window;
+  auto hidden = [&](int behind_it) {                        // query's position - key
+    if constexpr (MODE == kCausal) return behind_it < 0;
+    if constexpr (MODE == kSinks) return behind_it < reach;
+    return uint32_t(behind_it) >= uint32_t(reach);
   };
   bool odd = false;
   for (int j = 0; j < a.s.group; ++j) {
@@ -417,10 +419,13 @@ __global__ __launch_bounds__(256) ADORE_WAVES(sizeof(T) == 2 && SW == 1 ? 2 : 1)
   // The tile after the last one loaded: its head's rows, its first query.  From the last query back to the diagonal: the workgroups of
   // a head start with the same tiles, one reads what the others find in the L2.
   const int final = first + (per - 1) * QT;
+  // With a window the workgroups of a head have ranges that overlap: each begins with the tile whose number is a multiple of their length,
+  // so that they are at the same tile at the same time all the same (from their last ones on: @@ / @@ us, 8 x 2048 tokens of 32 heads over 8).
+  const int begin = MODE == kWindow && per > 0 ? final - (final / QT) % per * QT : final;
   const char *qp = reinterpret_cast<const char *>(a.q.p + sq.b * a.q.seq + sq.q_first * a.q.token + hk * a.s.group * a.q.head);
   const char *dp = reinterpret_cast<const char *>(a.d_out.p + sq.b * a.d_out.seq + sq.q_first * a.d_out.token + hk * a.s.group * a.d_out.head);
   size_t at = row_value(packed, sq.b, sq.q_first, a.s.q_tokens, a.s.heads, hk * a.s.group);
-  int next = final;
+  int next = begin;
   float row_lse = 0.f, row_delta = 0.f;
   auto load = [&](int stage) {
     lq(qp + next * (a.q.token * es), sq.nq - next, share + uint32_t(stage * 2 * kTile));
@@ -431,8 +436,9 @@ __global__ __launch_bounds__(256) ADORE_WAVES(sizeof(T) == 2 && SW == 1 ? 2 : 1)
       row_delta = there ? a.delta[at + next + tid] : 0.f;
     }
     next -= QT;
-    if (next < first) {
-      next = final;
+    if (MODE == kWindow && next < first) next = final;
+    if (MODE == kWindow ? next == begin : next < first) {
+      next = begin;
       qp += a.q.head * es;
       dp += a.d_out.head * es;
       at += a.s.q_tokens;
@@ -464,7 +470,7 @@ __global__ __launch_bounds__(256) ADORE_WAVES(sizeof(T) == 2 && SW == 1 ? 2 : 1)
   f32x16 dk[DB], dv[DB];
 #pragma unroll
   for (int db = 0; db < DB; ++db) dk[db] = dv[db] = f32x16{0.f};
-  int tile = final + QT;
+  int tile = begin + QT;
   for (int it = 0; it < tiles; ++it) {
     tile -= QT;
     if (tile < first) tile = final;
@@ -494,7 +500,7 @@ __global__ __launch_bounds__(256) ADORE_WAVES(sizeof(T) == 2 && SW == 1 ? 2 : 1)
     if (partial) {
 #pragma unroll
       for (int r = 0; r < 16; ++r)
-        if (!sees(k0 + c, q0 + 8 * (r >> 2) + 4 * h + (r & 3) + off)) s[r] = -INFINITY;
+        if (hidden(q0 + off - k0 + (4 * h - c) + 8 * (r >> 2) + (r & 3))) s[r] = -INFINITY;
     }
     auto next_of = [&](int i) {                             // columns in the order of the last four groups of products
       const int db = i % DB, t = i / DB;
@@ -514,11 +520,6 @@ __global__ __launch_bounds__(256) ADORE_WAVES(sizeof(T) == 2 && SW == 1 ? 2 : 1)
       }
     }
     pin();
-    if (MODE != kCausal && partial) {                       // (a key that nobody sees may hold anything)
-#pragma unroll
-      for (int r = 0; r < 16; ++r)
-        if (!sees(k0 + c, q0 + 8 * (r >> 2) + 4 * h + (r & 3) + off)) g[r] = rows_delta[8 * (r >> 2) + (r & 3)];
-    }
     // dv takes p; meanwhile g becomes p (g - delta)
     auto scaled = [&](int r4) {
       const f32x4 delta = *reinterpret_cast<const f32x4 *>(rows_delta + 8 * r4);
@@ -553,6 +554,39 @@ __global__ __launch_bounds__(256) ADORE_WAVES(sizeof(T) == 2 && SW == 1 ? 2 : 1)
     read.move(it & 1 ? uint32_t(-2 * kTile) : uint32_t(2 * kTile));
   }
   __syncthreads();
+  if (MODE == kWindow && a.sink_part && block * BK < a.s.sinks) {
+    // What the chunks gave the block's first keys.
+    const Chunks chunks(a.s, sq, a.sink_chunk);
+    if constexpr (SW > 1) {
+      if (k0 < min(a.s.sinks, sq.nk))                       // a part's share of the chunks goes the way of its sums
+        for (int i = chunks.first + mate.part; i < chunks.first + chunks.n; i += SW) {
+          const float *const sums = a.sink_part + sink_sums<DH>(a.s, i, hk, k0 / 32);
+          add_sums(dk, sums, 1.f, lane);
+          add_sums(dv, sums + 32 * DH, 1.f, lane);
+        }
+    } else {
+      // All threads add up, in V's place (a wave whose registers hold its sums loads one after the other: 568 us for 387).
+      static_assert(64 * DH * 4 <= 4 * kWave, "sums of a wave's keys");
+      f32x4 *const total = reinterpret_cast<f32x4 *>(smem + kVAt);
+      for (int w = 0; w < 4 && block * BK + 32 * w < min(a.s.sinks, sq.nk); ++w) {
+        for (int i = tid; i < 16 * DH; i += NT) {
+          if (block * BK + 32 * w + i % 8 * 4 >= a.s.sinks) continue;
+          const f32x4 *from = reinterpret_cast<const f32x4 *>(a.sink_part + sink_sums<DH>(a.s, chunks.first, hk, block * (BK / 32) + w)) + i;
+          const size_t step = sink_sums<DH>(a.s, 1, 0, 0) / 4;
+          f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+          for (int j = 0; j < chunks.n; ++j) sum += from[j * step];
+          total[i] = sum;
+        }
+        __syncthreads();
+        if (wave == w && block * BK + 32 * w + c / 4 * 4 < a.s.sinks) {
+          add_sums(dk, reinterpret_cast<const float *>(total), 1.f, lane);
+          add_sums(dv, reinterpret_cast<const float *>(total) + 32 * DH, 1.f, lane);
+        }
+        __syncthreads();
+      }
+    }
+  }
   if constexpr (SW > 1) {
     constexpr int kFloats = 64 * 16 * DB * 2, kPart = Shared<SW>::kRowWaves * kFloats;
     static_assert(4 * kWave + (SW - 1) * kPart * 4 <= 4 * kTile, "the parts' sums lie in the stages, behind the waves' own rows");
@@ -593,7 +627,7 @@ __global__ __launch_bounds__(256) ADORE_WAVES(sizeof(T) == 2 && SW == 1 ? 2 : 1)
         x = add_lane_xor<32>(x);
         w = __builtin_amdgcn_exp2f(fmaf(w, scale, -subtrahend(a.lse[row0 + i])));
         x = w * (x - a.delta[row0 + i]);
-        if (sees(k0 + c, i + off)) {
+        if (!hidden(i + off - k0 - c)) {
 #pragma unroll
           for (int db = 0; db < DB; ++db)
 #pragma unroll
@@ -613,13 +647,16 @@ __global__ __launch_bounds__(256) ADORE_WAVES(sizeof(T) == 2 && SW == 1 ? 2 : 1)
     put_sums(dv, to + 32 * DH, lane);
     return;
   }
-  if (MODE == kWindow && a.sink_part && k0 < a.s.sinks) {
-    const Chunks chunks(a.s, sq, a.sink_chunk);
-    for (int i = chunks.first; i < chunks.first + chunks.n; ++i) {
-      const float *const sums = a.sink_part + sink_sums<DH>(a.s, i, hk, k0 / 32);
-      add_sums(dk, sums, 1.f, lane);
-      add_sums(dv, sums + 32 * DH, 1.f, lane);
-    }
+  if (MODE == kWindow && k0 + a.s.window <= off && k0 + 31 >= a.s.sinks) {
+    // a key that no query sees may hold anything
+    const bool seen = k0 + c + a.s.window > off || k0 + c < a.s.sinks;
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        dk[db][r] = seen ? dk[db][r] : 0.f;
+        dv[db][r] = seen ? dv[db][r] : 0.f;
+      }
   }
   store_rows<T, DH>(dk, a.s.scale, own, reinterpret_cast<char *>(a.dk.p + sq.b * a.dk.seq + row * a.dk.token + hk * a.dk.head), a.dk.token * es, rows,
                     nullptr, 0, lane);
@@ -683,8 +720,8 @@ SinkPlan plan_sinks(const PromptShape &s, int head_dim, bool packed) {
   const long long queries = (long long)s.q_tokens * (packed ? 1 : s.batch);
   if (sinks == 0 || s.k_tokens <= s.window) return p;
   if (queries * s.group < 2048) return p;    // (a launch more)
-  // 512 workgroups, chunks of 256 queries or more
-  long long chunk = (queries * s.kv_heads * groups / 2 / 512 + 127) / 128 * 128;
+  // 256 workgroups, chunks of 256 queries or more
+  long long chunk = (queries * s.kv_heads * groups / 2 / 256 + 127) / 128 * 128;
   if (chunk < 256) chunk = 256;
   long long longest = s.q_tokens;
   if (chunk > longest) chunk = (longest + 127) / 128 * 128;
