@@ -65,7 +65,8 @@ struct StepArgs {
   int splits;
 };
 
-constexpr int kStepWaves = 4;
+constexpr int kStepWaves = 4;         // (512 rows of 512 slots: 23.5 us, with 8 25.5, with 2 23.1 but long rows 52 for 50)
+constexpr int kMaxSplits = 64;       // of a row: a lane each where they are joined
 
 // The sums of a wave's slots for 16 heads: o[i] (row = element 16 i + 4 quarter + r, column = head c) relative to `top`, and the lane's share
 // of the sum of weights.
@@ -180,17 +181,38 @@ __global__ __launch_bounds__(64 * kStepWaves) void ring_step_kernel(const StepAr
   sums.top = -INFINITY;
   sums.sum = 0.f;
   u32x4 kx[N], vx[N];
-  const int end = (held + kSlots - 1) / kSlots;
-  for (int block = split * NW + wave; block < end; block += a.splits * NW) {
-    const T *const p = cache + size_t(block) * (2 * L::kElems) + lane * EPL;
+  const int end = (held + kSlots - 1) / kSlots, step = a.splits * NW;
+  auto load = [&](int block, u32x4 (&k)[N], u32x4 (&v)[N]) {
+    const u32x4 *const p = reinterpret_cast<const u32x4 *>(cache + size_t(block) * (2 * L::kElems)) + lane;
 #pragma unroll
-    for (int i = 0; i < N; ++i) kx[i] = *reinterpret_cast<const u32x4 *>(p + i * 64 * EPL);
+    for (int i = 0; i < N; ++i) k[i] = p[i * 64];
 #pragma unroll
-    for (int i = 0; i < N; ++i) vx[i] = *reinterpret_cast<const u32x4 *>(p + L::kElems + i * 64 * EPL);
+    for (int i = 0; i < N; ++i) v[i] = p[(N + i) * 64];
+  };
+  auto take = [&](int block, const u32x4 (&k)[N], u32x4 (&v)[N]) {
     const int left = held - block * kSlots;
     uint32_t visible = left >= kSlots ? 0xffffffffu : (1u << left) - 1u;
     if (next / kSlots == block) visible &= ~(1u << (next % kSlots));    // (its row is about to be another)
-    take_block<T, DH>(sums, qf, kx, vx, visible, scale, quarter);
+    take_block<T, DH>(sums, qf, k, v, visible, scale, quarter);
+  };
+  int block = split * NW + wave;
+  if constexpr (N <= 8) {                    // the next block is on its way while one is worked on
+    u32x4 ky[N], vy[N];
+    if (block < end) load(block, kx, vx);
+    while (block < end) {
+      if (block + step < end) load(block + step, ky, vy);
+      take(block, kx, vx);
+      block += step;
+      if (block >= end) break;
+      if (block + step < end) load(block + step, kx, vx);
+      take(block, ky, vy);
+      block += step;
+    }
+  } else {
+    for (; block < end; block += step) {
+      load(block, kx, vx);
+      take(block, kx, vx);
+    }
   }
   if (split == 0 && wave == NW - 1) {
     // the new token: slot 0 of a block of its own, and its place in the ring
@@ -256,32 +278,31 @@ __global__ __launch_bounds__(64 * kStepWaves) void ring_step_kernel(const StepAr
   if (alone && a.s.tiles == 1 && tid == 0) a.cursor[row] = position + 1;     // (all waves have read it)
 }
 
-// Rows that several workgroups shared: their sums together.  A workgroup: a row's 16 heads.
+// Rows that several workgroups shared: their sums together.  A workgroup: a head of a row, a thread: an element.
 template <typename T, int DH>
-__global__ __launch_bounds__(256) void ring_join_kernel(const StepArgs<T> a) {
-  const int item = blockIdx.x, tile = item % a.s.tiles, row = item / a.s.tiles, b = row / a.s.kv_heads, hk = row - b * a.s.kv_heads;
-  const int heads = min(kHeads, a.s.group - tile * kHeads);
-  const float scale = a.s.scale_log2;
+__global__ __launch_bounds__(DH) void ring_join_kernel(const StepArgs<T> a) {
+  __shared__ float s_factor[kMaxSplits];
+  const int h = blockIdx.x % a.s.group, row = blockIdx.x / a.s.group, e = threadIdx.x, lane = e & 63;
+  const size_t first = (size_t(row) * a.s.tiles + h / kHeads) * a.splits * kHeads + h % kHeads;
   if (a.splits > 1) {
-    for (int i = threadIdx.x; i < heads * (DH / 4); i += 256) {
-      const int h = i / (DH / 4), e = i % (DH / 4) * 4;
-      const size_t first = size_t(item) * a.splits * kHeads + h;
-      float top = -INFINITY, total = 0.f;
-      for (int j = 0; j < a.splits; ++j) top = fmaxf(top, a.part_ml[2 * (first + size_t(j) * kHeads)]);
-      f32x4 o = {0.f, 0.f, 0.f, 0.f};
-      for (int j = 0; j < a.splits; ++j) {
-        const size_t at = first + size_t(j) * kHeads;
-        const float t = a.part_ml[2 * at], f = t == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((t - top) * scale);
-        total = fmaf(a.part_ml[2 * at + 1], f, total);
-        o += *reinterpret_cast<const f32x4 *>(a.part_o + at * DH + e) * f;
-      }
-      const float by = total > 0.f || total != total ? 1.f / total : 0.f;
-      T *to = a.out + (size_t(b) * a.s.heads + size_t(hk) * a.s.group + tile * kHeads + h) * DH + e;
+    // (every wave for itself: up to 64 parts, one a lane)
+    const bool mine = lane < a.splits;
+    const size_t at = 2 * (first + size_t(mine ? lane : 0) * kHeads);
+    const float top = mine ? a.part_ml[at] : -INFINITY, part = mine ? a.part_ml[at + 1] : 0.f;
+    float m = top;
 #pragma unroll
-      for (int j = 0; j < 4; ++j) store_elem(to + j, o[j] * by);
-    }
+    for (int off = 1; off < 64; off *= 2) m = fmaxf(m, __shfl_xor(m, off));
+    const float f = top == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((top - m) * a.s.scale_log2);
+    const float total = wave_sum(part * f), by = total > 0.f || total != total ? 1.f / total : 0.f;
+    if (e < 64 && mine) s_factor[lane] = f;
+    __syncthreads();
+    const float *from = a.part_o + first * DH + e;
+    float o = 0.f;
+#pragma unroll 8
+    for (int j = 0; j < a.splits; ++j) o = fmaf(from[size_t(j) * (kHeads * DH)], s_factor[j], o);
+    store_elem(a.out + (size_t(row) * a.s.group + h) * DH + e, o * by);
   }
-  if (tile == 0 && threadIdx.x == 0) a.cursor[row] = max(a.cursor[row], 0) + 1;
+  if (h == 0 && e == 0) a.cursor[row] = max(a.cursor[row], 0) + 1;
 }
 
 // ---- rows in and out ---------------------------------------------------------------------------------------------------------
@@ -301,12 +322,15 @@ __global__ __launch_bounds__(256) void ring_fill_kernel(const FillArgs<T> a) {
   typedef Ring<T, DH> L;
   constexpr int EPL = L::EPL, kRowChunks = DH / EPL;
   __shared__ __align__(16) T s_v[kSlots][DH + EPL];
-  const int block = blockIdx.x % a.s.blocks, row = blockIdx.x / a.s.blocks, b = row / a.s.kv_heads, hk = row - b * a.s.kv_heads;
+  // kv head fastest: a token's heads are side by side where prompts are packed
+  const int hk = blockIdx.x % a.s.kv_heads, item = blockIdx.x / a.s.kv_heads, block = item % a.s.blocks, b = item / a.s.blocks;
+  const int row = b * a.s.kv_heads + hk;
   int first = 0, n = a.k_tokens;
   if (a.k_start) span(a.k_start, b, a.k_tokens, first, n);
   // rows that were left out lie behind the first tokens, and only where the ring has no place for them
   const int seen = a.seen && n >= a.s.slots ? max(a.seen[b], n) : n, held = min(n, a.s.slots);
   if (block == 0 && threadIdx.x == 0) a.cursor[row] = seen;
+  if (block * kSlots >= held) return;
   auto token_in = [&](int slot) {            // which of the rows; -1: none
     if (slot >= held) return -1;
     if (slot < a.s.sinks || seen <= a.s.slots) return slot;
@@ -405,8 +429,11 @@ int ring_shape(const adore_ring_config *c, RingShape *s) {
 
 int splits_of(const RingShape &s) {
   const long long groups = (long long)s.batch * s.kv_heads * s.tiles;
-  const long long want = (1024 + groups - 1) / groups, able = (s.blocks + 2 * kStepWaves - 1) / (2 * kStepWaves);
-  return int(groups >= 512 || able <= 1 ? 1 : want < able ? want : able);
+  // One workgroup for each unit, whose waves have a block on its way while they work on another: 4 sequences of 8 kv heads, 16384 slots
+  // 43.3 us, with 512 workgroups 48.7, 1024 49.7, 2048 47.2 (of 8 waves 44.9 and 50.2 with 256 and 512).
+  const long long want = (256 + groups - 1) / groups, able = (s.blocks + 2 * kStepWaves - 1) / (2 * kStepWaves);
+  const long long n = able <= 1 ? 1 : want < able ? want : able;
+  return int(n < kMaxSplits ? n : kMaxSplits);
 }
 
 size_t ring_parts(const RingShape &s) { return size_t(s.batch) * s.kv_heads * s.tiles * splits_of(s) * kHeads; }
@@ -420,7 +447,7 @@ hipError_t launch_step(const StepArgs<T> &a, hipStream_t st) {
   hipLaunchKernelGGL((ring_step_kernel<T, DH>), dim3(items * unsigned(a.splits)), dim3(64 * kStepWaves), 0, st, a);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || (a.splits == 1 && a.s.tiles == 1)) return e;
-  hipLaunchKernelGGL((ring_join_kernel<T, DH>), dim3(items), dim3(256), 0, st, a);
+  hipLaunchKernelGGL((ring_join_kernel<T, DH>), dim3(unsigned(a.s.batch) * unsigned(a.s.heads)), dim3(DH), 0, st, a);
   return hipGetLastError();
 }
 
