@@ -480,59 +480,63 @@ class Rotary:
         self.turns = torch.tensor([t - (1 << 64) if t >> 63 else t for t in turns], dtype=torch.int64)     # (torch has no operations on uint64)
         self._there = {}
 
-    def on(self, device: torch.device) -> torch.Tensor:
-        """The table on a device."""
-        if device not in self._there:
-            self._there[device] = self.turns.to(device)
-        return self._there[device]
+    def on(self, device: torch.device) -> int:
+        """The table's address on a device."""
+        there = self._there.get(device)
+        if there is None:
+            there = self._there[device] = self.turns.to(device)
+        return there.data_ptr()
 
 
 class _Heads:
     """The rows of a call on queries and keys, packed [tokens, heads, head_dim] or dense [batch, heads, tokens, head_dim]."""
 
     def __init__(self, q, k, positions, rotary, q_weight, k_weight, eps):
+        # (a token's call takes the GPU less than the host: attributes that cost least)
         code = _CODES.get(q.dtype)
         index = q.get_device()
         if code is None or index < 0:
             raise ValueError(f"q: expected a bf16 or fp32 GPU tensor, got {q.device} {q.dtype}")
         self.device, self.index, self.dtype = q.device, index, q.dtype
-        qs = self.q_shape = q.shape
-        if len(qs) not in (3, 4):
+        self.q_shape = qs = q.shape
+        self.packed = packed = len(qs) == 3
+        if packed:
+            tokens, heads, d = qs
+            batch = 1
+        elif len(qs) == 4:
+            batch, heads, tokens, d = qs
+        else:
             raise ValueError("q: expected [tokens, heads, head_dim] or [batch, heads, tokens, head_dim]")
-        self.packed = len(qs) == 3
-        batch, heads, tokens = (1, qs[1], qs[0]) if self.packed else (qs[0], qs[1], qs[2])
         kv = 0
         self.k_shape = None
         if k is not None:
-            self.k_shape = k.shape
-            kv = k.shape[1] if k.dim() == len(qs) else 0
-            if kv == 0 or k.shape != (qs[:1] + k.shape[1:2] + qs[2:]):
-                raise ValueError(f"k: expected q's shape {tuple(qs)} but for the heads, got {tuple(k.shape)}")
+            self.k_shape = ks = k.shape
+            if len(ks) != len(qs) or ks[0] != qs[0] or ks[2:] != qs[2:] or ks[1] == 0:
+                raise ValueError(f"k: expected q's shape {tuple(qs)} but for the heads, got {tuple(ks)}")
+            kv = ks[1]
+        elif k_weight is not None:
+            raise ValueError("k_weight: there is no k")
         if not eps >= 0.0:
             raise ValueError("eps: expected a number that is not negative")
-        if rotary is None and q_weight is None and k_weight is None:
-            raise ValueError("rotary: expected one, or weights of norms")
-        self.positions = (None, 0, 0)
-        if rotary is not None:
-            if rotary.rotary_dim > qs[-1]:
-                raise ValueError(f"rotary: expected one of at most {qs[-1]} elements")
-            want = (tokens,) if self.packed else (batch, tokens)
-            if not isinstance(positions, torch.Tensor) or positions.dtype is not torch.int32 or positions.get_device() != index or \
-                    (positions.shape != want and positions.shape != want[-1:]):
-                raise ValueError(f"positions: expected int32 {list(want)}{'' if self.packed else f' or [{tokens}]'} on {self.device}")
-            stride = positions.stride()
-            self.positions = (positions.data_ptr() or 16, stride[0] if len(stride) == 2 and batch > 1 else 0, stride[-1] if tokens > 1 else 0)
-            self.turns = rotary.on(self.device).data_ptr()
-            self.cfg = AdoreRotateConfig(batch, heads, kv, qs[-1], tokens, code, rotary.rotary_dim, int(rotary.interleaved), rotary.magnitude, eps)
-        else:
-            self.turns = None
-            self.cfg = AdoreRotateConfig(batch, heads, kv, qs[-1], tokens, code, 0, 0, 1.0, eps)
-        self.weights = tuple(None if w is None else self.weight(w, n) for w, n in ((q_weight, "q_weight"), (k_weight, "k_weight")))
-        if k is None and k_weight is not None:
-            raise ValueError("k_weight: there is no k")
+        self.q_weight = None if q_weight is None else self.weight(q_weight, d, "q_weight")
+        self.k_weight = None if k_weight is None else self.weight(k_weight, d, "k_weight")
+        if rotary is None:
+            if q_weight is None and k_weight is None:
+                raise ValueError("rotary: expected one, or weights of norms")
+            self.angles = (None, None, 0, 0)
+            self.cfg = AdoreRotateConfig(batch, heads, kv, d, tokens, code, 0, 0, 1.0, eps)
+            return
+        if rotary.rotary_dim > d:
+            raise ValueError(f"rotary: expected one of at most {d} elements")
+        if not isinstance(positions, torch.Tensor) or positions.dtype is not torch.int32 or positions.get_device() != index or \
+                (positions.shape != (tokens,) and (packed or positions.shape != (batch, tokens))):
+            raise ValueError(f"positions: expected int32 {[tokens] if packed else f'[{batch}, {tokens}] or [{tokens}]'} on {self.device}")
+        stride = positions.stride()
+        self.angles = (rotary.on(self.device), positions.data_ptr() or 16, stride[0] if len(stride) == 2 and batch > 1 else 0,
+                       stride[-1] if tokens > 1 else 0)
+        self.cfg = AdoreRotateConfig(batch, heads, kv, d, tokens, code, rotary.rotary_dim, rotary.interleaved, rotary.magnitude, eps)
 
-    def weight(self, w, name):
-        d = self.q_shape[-1]
+    def weight(self, w, d, name):
         if not isinstance(w, torch.Tensor) or w.dtype is not torch.float32 or w.get_device() != self.index or w.shape != (d,) or not w.is_contiguous() or \
                 w.data_ptr() % 16:
             raise ValueError(f"{name}: expected contiguous fp32 [{d}] on {self.device}, 16-byte aligned")
@@ -542,11 +546,12 @@ class _Heads:
         if not isinstance(t, torch.Tensor) or t.shape != shape or t.dtype is not self.dtype or t.get_device() != self.index:
             raise ValueError(f"{name}: expected a {self.dtype} tensor of shape {tuple(shape)} on {self.device}")
         stride = t.stride()
-        if shape[-1] > 1 and stride[-1] != 1:
-            raise ValueError(f"{name}: its last dimension has to be dense")
-        stride = tuple(0 if n <= 1 else s for n, s in zip(shape, stride))
-        if written and any(n > 1 and s == 0 for n, s in zip(shape, stride)):
-            raise ValueError(f"{name}: its rows lie on one another")
+        if stride[-1] != 1 or 0 in stride or 1 in shape or 0 in shape:
+            if shape[-1] > 1 and stride[-1] != 1:
+                raise ValueError(f"{name}: its last dimension has to be dense")
+            stride = tuple(0 if n <= 1 else s for n, s in zip(shape, stride))      # of one row: any
+            if written and any(n > 1 and s == 0 for n, s in zip(shape, stride)):
+                raise ValueError(f"{name}: its rows lie on one another")
         ptr = t.data_ptr() or 16
         if self.packed:
             return ctypes.byref(AdoreRows(ptr, 0, stride[0], stride[1]))
@@ -554,13 +559,15 @@ class _Heads:
 
     def result(self, t, shape, name: str):
         """A tensor to write to, made here unless given, and its rows; two Nones where there is none."""
-        if shape is None:
-            if t is not None:
+        if t is not None:
+            if shape is None:
                 raise ValueError(f"{name}: there is no k")
+            return t, self.rows(t, shape, name, True)
+        if shape is None:
             return None, None
-        if t is None:
-            t = torch.empty(shape, dtype=self.dtype, device=self.device)
-        return t, self.rows(t, shape, name, True)
+        t = torch.empty(shape, dtype=self.dtype, device=self.device)
+        head = shape[-1] * (1 if self.packed else shape[2])
+        return t, ctypes.byref(AdoreRows(t.data_ptr() or 16, shape[1] * head, head * shape[1] if self.packed else shape[3], head))
 
 
 def rotate_heads(q: torch.Tensor, k: Optional[torch.Tensor], positions: Optional[torch.Tensor], rotary: Optional[Rotary], *,
@@ -576,8 +583,8 @@ def rotate_heads(q: torch.Tensor, k: Optional[torch.Tensor], positions: Optional
 
     Where q, k or weights require gradients the results have them (torch's backward pass is rotate_heads_backward, once); q_out and
     k_out cannot be given then."""
-    inputs = (q, k, q_weight, k_weight)
-    if torch.is_grad_enabled() and any(isinstance(t, torch.Tensor) and t.requires_grad for t in inputs):
+    if torch.is_grad_enabled() and (q.requires_grad or (k is not None and k.requires_grad) or
+                                    (q_weight is not None and q_weight.requires_grad) or (k_weight is not None and k_weight.requires_grad)):
         if q_out is not None or k_out is not None:
             raise ValueError("q_out, k_out: cannot be given where gradients are required (call under torch.no_grad())")
         return _RotateHeads.apply(q, k, q_weight, k_weight, positions, rotary, eps)
@@ -589,7 +596,7 @@ def _rotate(q, k, positions, rotary, q_weight, k_weight, eps, q_out=None, k_out=
     h = _Heads(q, k, positions, rotary, q_weight, k_weight, eps)
     q_out, q_to = h.result(q_out, h.q_shape, "q_out")
     k_out, k_to = h.result(k_out, h.k_shape, "k_out")
-    _call(lib, h.index, lib.adore_rotate_heads, ctypes.byref(h.cfg), h.turns, *h.positions, *h.weights, h.rows(q, h.q_shape, "q"),
+    _call(lib, h.index, lib.adore_rotate_heads, ctypes.byref(h.cfg), *h.angles, h.q_weight, h.k_weight, h.rows(q, h.q_shape, "q"),
           None if k is None else h.rows(k, h.k_shape, "k"), q_to, k_to, _stream(h.index))
     return q_out, k_out
 
@@ -629,12 +636,12 @@ def rotate_heads_backward(d_q: torch.Tensor, d_k: Optional[torch.Tensor], q: tor
         raise ValueError("d_k: there is no k")
     dq, dq_to = h.result(dq, h.q_shape, "dq")
     dk, dk_to = h.result(dk, h.k_shape, "dk")
-    dqw, dkw = (None if w is None else torch.empty(h.q_shape[-1], dtype=torch.float32, device=h.device) for w in h.weights)
+    dqw, dkw = (None if w is None else torch.empty(h.q_shape[-1], dtype=torch.float32, device=h.device) for w in (q_weight, k_weight))
     need, space = 0, None
     if dqw is not None or dkw is not None:
         need = lib.adore_rotate_backward_workspace_bytes(ctypes.byref(h.cfg))
         space = torch.empty(max(need, 1), dtype=torch.uint8, device=h.device)
-    _call(lib, h.index, lib.adore_rotate_heads_backward, ctypes.byref(h.cfg), h.turns, *h.positions, *h.weights,
+    _call(lib, h.index, lib.adore_rotate_heads_backward, ctypes.byref(h.cfg), *h.angles, h.q_weight, h.k_weight,
           h.rows(d_q, h.q_shape, "d_q"), None if k is None else h.rows(d_k, h.k_shape, "d_k"), h.rows(q, h.q_shape, "q"),
           None if k is None else h.rows(k, h.k_shape, "k"), dq_to, dk_to, None if dqw is None else dqw.data_ptr(),
           None if dkw is None else dkw.data_ptr(), None if space is None else space.data_ptr(), need, _stream(h.index))

@@ -358,6 +358,7 @@ __global__ __launch_bounds__(256) void rotate_weights_kernel(const float *part, 
   __shared__ float s_sum[32][8];
   const int column = threadIdx.x & 7, row = threadIdx.x >> 3, at = blockIdx.x * 8 + column;
   float sum = 0.f;
+#pragma unroll 16
   for (int i = row; i < n; i += 32) sum += part[size_t(i) * (2 * DH) + at];
   s_sum[row][column] = sum;
   __syncthreads();
@@ -370,7 +371,7 @@ __global__ __launch_bounds__(256) void rotate_weights_kernel(const float *part, 
 }
 
 // ---- host ----------------------------------------------------------------------------------------------------------------
-constexpr long long kMostParts = 1024;       // workgroups whose sums of the weights' gradients are added up
+constexpr long long kMostParts = 512;        // workgroups whose sums of the weights' gradients are added up: as many as have a place
 
 int rotate_shape(const adore_rotate_config *c, RotateShape *s) {
   if (!c || c->batch <= 0 || c->heads <= 0 || c->kv_heads < 0 || c->tokens < 0 || (c->dtype != ADORE_F32 && c->dtype != ADORE_BF16) ||
