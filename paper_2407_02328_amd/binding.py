@@ -582,7 +582,7 @@ def rotate_heads(q: torch.Tensor, k: Optional[torch.Tensor], positions: Optional
     dense last dimension (views of one projection).  k may be None; so may rotary, for norms alone.
 
     Where q, k or weights require gradients the results have them (torch's backward pass is rotate_heads_backward, once); q_out and
-    k_out cannot be given then."""
+    k_out cannot be given then.  A step that is captured into a graph calls the two itself, under torch.no_grad()."""
     if torch.is_grad_enabled() and (q.requires_grad or (k is not None and k.requires_grad) or
                                     (q_weight is not None and q_weight.requires_grad) or (k_weight is not None and k_weight.requires_grad)):
         if q_out is not None or k_out is not None:

@@ -310,17 +310,19 @@ constexpr bool kValuesInRegisters = SW > 1 && DH * sizeof(T) == 512;
 // With a window a block of keys is seen by few queries, but the first keys by all that follow: one workgroup would go over a whole prompt
 // while the others go over a window.  So the queries behind the window (p - j >= window) are cut into chunks, each a workgroup's, whose
 // sums for 32 first keys (a wave's registers, fp32) go to memory; the workgroup of the block that holds the keys adds them to its own.
-// A sequence's chunks: n places from `first` on.  find_chunk: a place's sequence and chunk (all 64 lanes of a wave call it together).
+// A sequence's chunks: n places from `first` on.  find_chunk: a place's sequence and first query (all 64 lanes of a wave call it together).
 struct Chunks {
   int first, n;
+  int from;                                  // the first query that is as far as the window from key 0
   __device__ __forceinline__ Chunks(const PromptShape &a, const Sequence &s, int chunk) {
-    n = s.nk > a.window ? (s.nq + chunk - 1) / chunk : 0;      // (else no query is further than the window from any key)
+    from = max(a.window - (s.nk - s.nq), 0);
+    n = s.nq > from ? (s.nq - from + chunk - 1) / chunk : 0;
     // packed: of the sequences that have chunks no two are in the same run of window + 1 keys (whatever the starts hold: no place is
     // beyond SinkPlan::slots)
     first = a.q_start ? s.q_first / chunk + min(s.b, s.k_first / (a.window + 1)) : s.b * ((a.q_tokens + chunk - 1) / chunk);
   }
 };
-__device__ __forceinline__ bool find_chunk(const PromptShape &a, int place, int chunk, Sequence &s, int &at) {
+__device__ __forceinline__ bool find_chunk(const PromptShape &a, int place, int chunk, Sequence &s, int &query) {
   const int lane = threadIdx.x & 63;
   for (int b0 = 0; b0 < a.batch; b0 += 64) {
     const int b = min(b0 + lane, a.batch - 1);
@@ -328,7 +330,8 @@ __device__ __forceinline__ bool find_chunk(const PromptShape &a, int place, int 
     const uint64_t here = __builtin_amdgcn_ballot_w64(place >= mine.first && place < mine.first + mine.n);
     if (here) {
       s = sequence_at(a, __builtin_amdgcn_readfirstlane(min(b0 + int(__builtin_ctzll(here)), a.batch - 1)));
-      at = place - Chunks(a, s, chunk).first;
+      const Chunks found(a, s, chunk);
+      query = found.from + (place - found.first) * chunk;
       return true;
     }
   }
@@ -360,7 +363,6 @@ __global__ __launch_bounds__(256) ADORE_WAVES(sizeof(T) == 2 && SW == 1 ? 2 : 1)
     block = item / a.sink_slots;
     place = item - block * a.sink_slots;
     if (!find_chunk(a.s, place, a.sink_chunk, sq, chunk)) return;
-    chunk *= a.sink_chunk;
   } else if (!find_block<BK, false>(a.s, blockIdx.x / a.s.kv_heads, a.by_work, sq, block)) {
     const SpareRows spare = spare_rows<BK>(a.s.k_start, a.s.batch, a.s.k_tokens, block);
     zero_rows<T, DH>(a.dk, hk, spare, tid, NT);
@@ -420,7 +422,8 @@ __global__ __launch_bounds__(256) ADORE_WAVES(sizeof(T) == 2 && SW == 1 ? 2 : 1)
   // a head start with the same tiles, one reads what the others find in the L2.
   const int final = first + (per - 1) * QT;
   // With a window the workgroups of a head have ranges that overlap: each begins with the tile whose number is a multiple of their length,
-  // so that they are at the same tile at the same time all the same (from their last ones on: @@ / @@ us, 8 x 2048 tokens of 32 heads over 8).
+  // so that they are at the same tile at the same time all the same (from their last ones on 1027 us a step for 1018, 8 x 2048 tokens of
+  // 32 heads over 8, window 508).
   const int begin = MODE == kWindow && per > 0 ? final - (final / QT) % per * QT : final;
   const char *qp = reinterpret_cast<const char *>(a.q.p + sq.b * a.q.seq + sq.q_first * a.q.token + hk * a.s.group * a.q.head);
   const char *dp = reinterpret_cast<const char *>(a.d_out.p + sq.b * a.d_out.seq + sq.q_first * a.d_out.token + hk * a.s.group * a.d_out.head);

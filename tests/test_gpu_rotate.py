@@ -324,6 +324,15 @@ def test_autograd():
         ones = torch.ones_like(dq)
         assert torch.equal(y.grad[:, :4], P.rotate_heads_backward(ones, None, y.detach()[:, :4], None, pos, rotary)[0])
         assert bool((y.grad[:, 4:] == 0).all())
+        z = x.detach()[:, :4].clone().requires_grad_()
+        only, none = P.rotate_heads(z, None, pos, rotary, q_weight=qw.detach())
+        assert none is None
+        only.backward(dq)
+        assert torch.equal(z.grad, want[0])
+        alone = kw.detach().clone().requires_grad_()             # a weight's gradient, the rows have none
+        _, k = P.rotate_heads(x.detach()[:, :4], x.detach()[:, 4:6], pos, rotary, k_weight=alone)
+        k.backward(dk)
+        assert torch.equal(alone.grad, want[3])
         with pytest.raises(ValueError):
             P.rotate_heads(y[:, :4], None, pos, rotary, q_out=torch.empty_like(dq))
 

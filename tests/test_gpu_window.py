@@ -88,6 +88,24 @@ def run(torch, P, nq, nk, H, Hk, d, dt, window, sinks, *, seed=1, spare=3, spoil
         a, b = a + n, b + m
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("nq,nk,window,sinks", [(700, 690, 50, 4), (900, 200, 20, 2), (1500, 1499, 1, 40), (600, 3, 2, 2)])
+def test_many_queries_of_which_the_first_see_nothing(nq, nk, window, sinks, d, dtype):
+    """Their rows may hold anything, in tiles with queries that are behind the window of the first keys."""
+    torch, P = _mods()
+    dt = dtype_of(torch, dtype)
+    for bad in (0.5, math.nan):
+
+        def spoil(q, k, v, do):
+            q[:nq - nk], do[:nq - nk] = bad, bad
+
+        (x, got), = run(torch, P, [nq], [nk], 8, 2, d, dt, window, sinks, spoil=spoil)
+        x[0][:nq - nk], x[3][:nq - nk] = 0.0, 0.0
+        check(torch, got, reference(torch, *x, d ** -0.5, window, sinks), dt, d)
+        assert bool((got["out"][:nq - nk] == 0).all()) and bool((got["dq"][:nq - nk] == 0).all()) and bool((got["lse"][:, :nq - nk] == -math.inf).all())
+
+
 def dtype_of(torch, name):
     return torch.bfloat16 if name == "bf16" else torch.float32
 

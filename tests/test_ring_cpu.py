@@ -78,3 +78,31 @@ def test_the_binding_refuses_what_does_not_fit():
         WindowCache(window=4, scale=-1.0, **how)
     with pytest.raises(ValueError):
         WindowCache(window=4, cache=torch.zeros((1, 2, 1, 64 * 64), dtype=torch.bfloat16), **how)       # not on the GPU
+
+
+def test_calls_take_place_on_the_device_of_their_tensors(monkeypatch):
+    import torch
+    from paper_2407_02328_amd import WindowCache, binding
+    from tests.test_devices_cpu import Machine, OnGpu, on_gpu
+    m, empty = Machine(), torch.empty
+    monkeypatch.setattr(binding, "load_library", lambda: m)
+    monkeypatch.setattr(binding, "_stream", lambda index: 0)
+    monkeypatch.setattr(binding, "_current", lambda: m.current, raising=False)
+    monkeypatch.setattr(torch.cuda, "device", m.device)
+    monkeypatch.setattr(torch, "empty", lambda *args, device=None, **kw: empty(*args, **kw).as_subclass(OnGpu))
+    cache, cursor = on_gpu((2 * 2 * 2 * 64 * 64 + 128,)), on_gpu((2, 2), torch.int32)
+    at = -cache.data_ptr() % 256 // 2
+    cache = cache[at:at + 2 * 2 * 2 * 64 * 64].view(2, 2, 2, 64 * 64)
+    c = WindowCache(batch=2, heads=4, kv_heads=2, head_dim=64, window=60, sinks=4, dtype="bf16", cache=cache, cursor=cursor)
+    c.fill(on_gpu((2, 2, 5, 64)), on_gpu((2, 2, 5, 64)), seen=on_gpu((2,), torch.int32))
+    c.step(on_gpu((2, 4, 64)), on_gpu((2, 2, 64)), on_gpu((2, 2, 64)))
+    c.read()
+    assert m.calls == [("adore_ring_fill", 1), ("adore_ring_step", 1), ("adore_ring_read", 1)] and m.current == 0
+    for bad in (lambda: c.fill(on_gpu((2, 2, 5, 64)), on_gpu((2, 2, 5, 64)), seen=on_gpu((3,), torch.int32)),
+                lambda: c.fill(on_gpu((2, 2, 5, 64)), on_gpu((2, 2, 4, 64))), lambda: c.fill(on_gpu((2, 1, 5, 64)), on_gpu((2, 1, 5, 64))),
+                lambda: c.step(on_gpu((2, 2, 64)), on_gpu((2, 2, 64)), on_gpu((2, 2, 64))),
+                lambda: c.step(on_gpu((2, 4, 64), torch.float32), on_gpu((2, 2, 64)), on_gpu((2, 2, 64))),
+                lambda: c.step(on_gpu((2, 64, 4)).transpose(1, 2), on_gpu((2, 2, 64)), on_gpu((2, 2, 64))), lambda: c.read(k=on_gpu((2, 2, 60, 64)))):
+        with pytest.raises(ValueError):
+            bad()
+    assert len(m.calls) == 3

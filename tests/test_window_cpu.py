@@ -72,10 +72,12 @@ def test_places_of_chunks_lie_in_the_workspace(lib):  # noqa: F811
         for b in range(batch):
             q0, k0 = cut(qs[b]), cut(ks[b])
             nq, nk = max(cut(qs[b + 1]) - q0, 0), max(cut(ks[b + 1]) - k0, 0)
-            if nk <= W or nq == 0:
+            far = nq - max(W - (nk - nq), 0)           # queries as far as the window from the first key
+            if far <= 0:
                 continue
+            assert nk > W
             first = q0 // chunk + min(b, k0 // (W + 1))
-            mine = set(range(first, first + -(-nq // chunk)))
+            mine = set(range(first, first + -(-far // chunk)))
             assert max(mine) < slots
             if sorted_starts:
                 assert not mine & taken
