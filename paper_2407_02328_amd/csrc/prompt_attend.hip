@@ -101,12 +101,13 @@ void prompt_attend_kernel(const AttendArgs<T> a) {
   const float slack = fminf(8.f / scale, FLT_MAX);    // (finite: ahead of the first keys, top + slack has to be less than any product)
   const int hidden = max(block * BQ + off + 1, 0) / KT;               // the first tile that not all of the workgroup's queries see all of
   bool found = false;                           // ... where a value is not finite
+  bool careful = !WIN;                          // whether tiles are looked through for those: with a window a third of them would be
   for (int it = 0; it < tiles; ++it) {
     const int tile = WIN ? win.tile(it) : it;
     const int k0 = tile * KT + mate.part * 32;  // the wave's first key of the tile
     arrived();
     __syncthreads();
-    if (tile >= hidden || (WIN && tile * KT < win.partial && tile * KT + KT > a.s.sinks)) {
+    if (careful && (tile >= hidden || (WIN && tile * KT < win.partial && tile * KT + KT > a.s.sinks))) {
       found |= make_finite<T, DH, KT, NT>(smem + (it & 1) * 2 * kTile + kTile);
       __syncthreads();
     }
@@ -206,6 +207,29 @@ void prompt_attend_kernel(const AttendArgs<T> a) {
       sum += (part[0] + part[1]) + (part[2] + part[3]);
     }
     read.move(it & 1 ? uint32_t(-2 * kTile) : uint32_t(2 * kTile));
+    if (WIN && !careful && it + 1 == tiles) {
+      // A hidden value that is not finite has made its product with a weight of 0 NaN.  Then all of it once more, carefully.
+      float bad = 0.f;
+#pragma unroll
+      for (int db = 0; db < DB; ++db)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) bad = fmaf(o[db][r], 0.f, bad);
+      __syncthreads();
+      if (any_of_four(__builtin_amdgcn_ballot_w64(bad != 0.f) != 0, reinterpret_cast<int *>(smem + 4 * 32 * L::kRow))) {
+        __syncthreads();
+        careful = true;
+#pragma unroll
+        for (int db = 0; db < DB; ++db) o[db] = f32x16{0.f};
+        top = -INFINITY;
+        sum = 0.f;
+        kp += (win.tile(0) - tile) * ks;
+        vp += (win.tile(0) - tile) * vs;
+        lk(kp, sq.nk - win.tile(0) * KT, share);
+        lv(vp, sq.nk - win.tile(0) * KT, share + kTile);
+        if (tiles & 1) read.move(uint32_t(-2 * kTile));
+        it = -1;
+      }
+    }
   }
   __syncthreads();
   found = any_of_four(found, reinterpret_cast<int *>(smem + 4 * 32 * L::kRow));
