@@ -161,11 +161,32 @@ __global__ __launch_bounds__(256) ADORE_WAVES(sizeof(T) == 4 || SW > 1 ? 1 : DH 
   for (int db = 0; db < DB; ++db) dq[db] = f32x16{0.f};
   const int hidden = max(block * BQ + off + 1, 0) / KT;    // the first tile that not all of the workgroup's queries see all of
   int from = INT_MAX;                                      // first key of the first such tile where an element of K is not finite
-  for (int it = 0; it < tiles; ++it) {
+  bool careful = !WIN;                                     // whether tiles are looked through for those: with a window a third of them would be
+  for (int it = 0;; ++it) {
+    if (it >= tiles) {
+      if (careful || tiles == 0) break;
+      // A hidden key that is not finite has made its product with a weight of 0 NaN.  Then all of it once more, carefully.
+      float bad = 0.f;
+#pragma unroll
+      for (int db = 0; db < DB; ++db)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) bad = fmaf(dq[db][r], 0.f, bad);
+      __syncthreads();
+      if (!any_of_four(__builtin_amdgcn_ballot_w64(bad != 0.f) != 0, reinterpret_cast<int *>(smem + kDqWords<T, DH, SW>))) break;
+      careful = true;
+#pragma unroll
+      for (int db = 0; db < DB; ++db) dq[db] = f32x16{0.f};
+      kp += (win.tile(0) - win.tile(tiles - 1)) * (KT * a.k.token * es);
+      vp += (win.tile(0) - win.tile(tiles - 1)) * (KT * a.v.token * es);
+      lk(kp, sq.nk - win.tile(0) * KT, share);
+      lv(vp, sq.nk - win.tile(0) * KT, share + kTile);
+      if (tiles & 1) read.move(uint32_t(-2 * kTile));
+      it = 0;
+    }
     const int tile = WIN ? win.tile(it) : it, k0 = tile * KT + mate.part * 32;
     arrived();
     __syncthreads();
-    if (tile >= hidden || (WIN && tile * KT < win.partial && tile * KT + KT > a.s.sinks)) {
+    if (careful && (tile >= hidden || (WIN && tile * KT < win.partial && tile * KT + KT > a.s.sinks))) {
       const bool found = any_of_four(find_not_finite<T, DH, KT, NT>(smem + (it & 1) * 2 * kTile), reinterpret_cast<int *>(smem + kDqWords<T, DH, SW>));
       if (__builtin_amdgcn_readfirstlane(found)) from = min(from, tile * KT);
     }
