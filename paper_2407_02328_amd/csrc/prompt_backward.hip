@@ -579,36 +579,28 @@ __global__ __launch_bounds__(256) ADORE_WAVES(sizeof(T) == 2 && SW == 1 ? 2 : 1)
   }
   __syncthreads();
   if (MODE == kWindow && a.sink_part && block * BK < a.s.sinks) {
-    // What the chunks gave the block's first keys.
+    // What the chunks gave the block's first keys: all threads add up 32 keys' sums, in the stages' place, and the wave that has the keys
+    // takes them (a wave by itself, whose registers are full, loads one after the other: 568 us for 387 at 8 x 2048 tokens).
+    static_assert(64 * DH * 4 <= 4 * kTile, "sums of a wave's keys");
     const Chunks chunks(a.s, sq, a.sink_chunk);
-    if constexpr (SW > 1) {
-      if (k0 < min(a.s.sinks, sq.nk))                       // a part's share of the chunks goes the way of its sums
-        for (int i = chunks.first + mate.part; i < chunks.first + chunks.n; i += SW) {
-          const float *const sums = a.sink_part + sink_sums<DH>(a.s, i, hk, k0 / 32);
-          add_sums(dk, sums, 1.f, lane);
-          add_sums(dv, sums + 32 * DH, 1.f, lane);
-        }
-    } else {
-      // All threads add up, in V's place (a wave whose registers hold its sums loads one after the other: 568 us for 387).
-      static_assert(64 * DH * 4 <= 4 * kWave, "sums of a wave's keys");
-      f32x4 *const total = reinterpret_cast<f32x4 *>(smem + kVAt);
-      for (int w = 0; w < 4 && block * BK + 32 * w < min(a.s.sinks, sq.nk); ++w) {
-        for (int i = tid; i < 16 * DH; i += NT) {
-          if (block * BK + 32 * w + i % 8 * 4 >= a.s.sinks) continue;
-          const f32x4 *from = reinterpret_cast<const f32x4 *>(a.sink_part + sink_sums<DH>(a.s, chunks.first, hk, block * (BK / 32) + w)) + i;
-          const size_t step = sink_sums<DH>(a.s, 1, 0, 0) / 4;
-          f32x4 sum = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll 4
-          for (int j = 0; j < chunks.n; ++j) sum += from[j * step];
-          total[i] = sum;
-        }
-        __syncthreads();
-        if (wave == w && block * BK + 32 * w + c / 4 * 4 < a.s.sinks) {
-          add_sums(dk, reinterpret_cast<const float *>(total), 1.f, lane);
-          add_sums(dv, reinterpret_cast<const float *>(total) + 32 * DH, 1.f, lane);
-        }
-        __syncthreads();
+    f32x4 *const total = reinterpret_cast<f32x4 *>(smem);
+    const size_t step = sink_sums<DH>(a.s, 1, 0, 0) / 4;
+    for (int w = 0; w < BK / 32 && block * BK + 32 * w < min(a.s.sinks, sq.nk); ++w) {
+      const f32x4 *const sums = reinterpret_cast<const f32x4 *>(a.sink_part + sink_sums<DH>(a.s, chunks.first, hk, block * (BK / 32) + w));
+      const int fours = min((a.s.sinks - block * BK - 32 * w + 3) / 4, 8);       // four keys at a time, those that are first ones
+      for (int item = tid; item < 2 * DH * fours; item += NT) {
+        const int i = item / fours * 8 + item % fours;
+        f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 8
+        for (int j = 0; j < chunks.n; ++j) sum += sums[i + j * step];
+        total[i] = sum;
       }
+      __syncthreads();
+      if (mate.rows == w && mate.part == 0 && block * BK + 32 * w + c / 4 * 4 < a.s.sinks) {
+        add_sums(dk, reinterpret_cast<const float *>(total), 1.f, lane);
+        add_sums(dv, reinterpret_cast<const float *>(total) + 32 * DH, 1.f, lane);
+      }
+      __syncthreads();
     }
   }
   if constexpr (SW > 1) {
@@ -738,17 +730,24 @@ struct SinkPlan {
   int chunk, slots;
   size_t bytes;
 };
+constexpr int32_t kSome = 0;               // (starts that nobody reads: there are some)
 SinkPlan plan_sinks(const PromptShape &s, int head_dim, bool packed) {
   SinkPlan p = {0, 0, 0};
   const long long sinks = s.sinks < s.k_tokens ? s.sinks : s.k_tokens, groups = (sinks + 63) / 64 * 2;
   const long long queries = (long long)s.q_tokens * (packed ? 1 : s.batch);
   if (sinks == 0 || s.k_tokens <= s.window) return p;
-  if (queries * s.group < 2048) return p;    // (a launch more)
-  // 256 workgroups, chunks of 256 queries or more
+  // It is a launch more, against one workgroup for each kv head that goes over so many more queries than the others (of a sequence twice
+  // as long as the average, where lengths differ).  Not cut / cut, us (sequences x tokens, heads / kv heads, window; 4 first keys):
+  //   64 elements    3 x 128, 4 / 4, 32: 17 / 25;  4 x 256, 8 / 8, 32: 20 / 28;  512, 4 / 2, 64: 32 / 35;  2048, 4 / 4, 1000: 52 / 50;
+  //                  2 x 2048, 8 / 2, 100: 133 / 60;  60000, 4 / 4, 1000: 2824 / 408
+  //   128 elements   8 x 512, 8 / 2, 64: 69 / 76;  32 x 512, 16 / 4, 128: 249 / 232;  4 x 1000, 4 / 1, 200: 102 / 88;  1024, 8 / 2, 128: 93 / 69;
+  //                  4096, 8 / 2, 256: 350 / 105;  16384, 8 / 1, 512: 2669 / 390;  8 x 2048, 32 / 8, 508: 873 / 757
+  const long long average = length_of(packed ? &kSome : nullptr, s.batch, s.q_tokens), most = 2 * average < s.q_tokens ? 2 * average : s.q_tokens;
+  if ((most - s.window - 128) * s.group < 1024) return p;
+  // 256 workgroups, chunks of 128 queries or more (256: 76 us for 69 at 1024 tokens, 109 for 105 at 4096, 748 for 757 at 8 x 2048)
   long long chunk = (queries * s.kv_heads * groups / 2 / 256 + 127) / 128 * 128;
-  if (chunk < 256) chunk = 256;
-  long long longest = s.q_tokens;
-  if (chunk > longest) chunk = (longest + 127) / 128 * 128;
+  if (chunk < 128) chunk = 128;
+  if (chunk > s.q_tokens) chunk = (s.q_tokens + 127) / 128 * 128;
   const long long long_ones = (long long)s.k_tokens / (s.window + 1);
   const long long slots = packed ? s.q_tokens / chunk + (s.batch < long_ones ? s.batch : long_ones) + 1 : s.batch * ((s.q_tokens + chunk - 1) / chunk);
   const long long bytes = slots * s.kv_heads * groups * 64 * head_dim * 4;

@@ -195,24 +195,9 @@ __global__ __launch_bounds__(64 * kStepWaves) void ring_step_kernel(const StepAr
     if (next / kSlots == block) visible &= ~(1u << (next % kSlots));    // (its row is about to be another)
     take_block<T, DH>(sums, qf, k, v, visible, scale, quarter);
   };
-  int block = split * NW + wave;
-  if constexpr (N <= 8) {                    // the next block is on its way while one is worked on
-    u32x4 ky[N], vy[N];
-    if (block < end) load(block, kx, vx);
-    while (block < end) {
-      if (block + step < end) load(block + step, ky, vy);
-      take(block, kx, vx);
-      block += step;
-      if (block >= end) break;
-      if (block + step < end) load(block + step, kx, vx);
-      take(block, ky, vy);
-      block += step;
-    }
-  } else {
-    for (; block < end; block += step) {
-      load(block, kx, vx);
-      take(block, kx, vx);
-    }
+  for (int block = split * NW + wave; block < end; block += step) {
+    load(block, kx, vx);
+    take(block, kx, vx);
   }
   if (split == 0 && wave == NW - 1) {
     // the new token: slot 0 of a block of its own, and its place in the ring

@@ -39,7 +39,7 @@ struct RotatePlan {
   long long waves;
 };
 
-constexpr int kRowsAtOnce = 4;               // of a group: their loads are under way together
+constexpr int kRowsAtOnce = 2;               // of a group: their loads are under way together
 
 template <typename T>
 struct Eight;                                // eight elements, as they are
@@ -266,7 +266,7 @@ __global__ __launch_bounds__(256) void rotate_heads_kernel(const RotateArgs<T> a
 // rotate_weights_kernel the workgroups: no atomics, equal inputs give equal bits.
 template <typename T, int DH, bool SIDE>
 __global__ __launch_bounds__(256) void rotate_backward_kernel(const RotateArgs<T> a) {
-  constexpr int U = sizeof(T) == 2 ? kRowsAtOnce : kRowsAtOnce / 2, G = DH / 16;
+  constexpr int U = 1, G = DH / 16;          // (rows at once; two: 68.7 us for 61.5, 16384 tokens of 32 and 8 heads of 64)
   __shared__ float s_sum[4][2][DH];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, all = a.s.heads + a.s.kv_heads;
   const Lane<DH> mine(a.s, lane);
@@ -401,7 +401,7 @@ RotatePlan plan_rotation(const RotateShape &s, int head_dim) {
   while (side > 1 && side / 2 >= all) side /= 2;
   p.wide = groups / side;
   const long long steps = (all + side - 1) / side, tokens = (s.all + p.wide - 1) / p.wide;
-  p.parts = int(tokens * steps <= 4096 ? steps : (steps + 7) / 8);
+  p.parts = int(tokens * steps <= 2560 ? steps : (steps + 7) / 8);
   p.waves = tokens * p.parts;
   return p;
 }
