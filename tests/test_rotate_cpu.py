@@ -131,7 +131,9 @@ class TestShapes:
         monkeypatch.setattr(binding, "_stream", lambda index: 0)
         monkeypatch.setattr(binding, "_current", lambda: m.current, raising=False)
         monkeypatch.setattr(torch.cuda, "device", m.device)
+        strided = torch.empty_strided
         monkeypatch.setattr(torch, "empty", lambda *args, device=None, **kw: empty(*args, **kw).as_subclass(OnGpu))
+        monkeypatch.setattr(torch, "empty_strided", lambda *args, device=None, **kw: strided(*args, **kw).as_subclass(OnGpu))
         return m
 
     def test_on_their_device_and_to_q_s_shape(self, machine, monkeypatch):
