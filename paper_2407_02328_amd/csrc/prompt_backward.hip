@@ -11,6 +11,10 @@
 // 8 x 2048 tokens of 32 heads over 8, 128 elements: dq 441 us (0.94 PFLOP/s), dk and dv 606 us (0.91).  The matrix unit is busy 46 and
 // 43 % of the cycles, vector instructions take 42 and 28 %, LDS 26 and 33 %: nothing bounds alone.  A wave's operands, products and
 // arithmetic wait for one another, and the registers leave two waves a SIMD to fill in.
+//
+// With a window: the same products over what is seen, and the first keys' queries in a launch of their own (Chunks).  8 x 2048 tokens of 32 heads
+// over 8, 128 elements, window 508 and 4 first keys: dq 324 us, the first keys 73 (Q and dO once more, 268 MB), dk and dv 359: tiles of 32
+// queries as fast as above, 20 a block of 128 keys where 16 would do.  A wave that leaves out the tiles it sees nothing of: 148 registers spilled.
 #include <hip/hip_runtime.h>
 
 #include <climits>

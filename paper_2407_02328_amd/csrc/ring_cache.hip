@@ -12,7 +12,9 @@
 //          V [DH / 16][t][quarter][c][4]:        element 16 i + c, slot 16 t + 4 quarter + e
 // S^T = K Q^T leaves lane (quarter, c) the weights of head c and exactly those slots that P^T's operand in O^T += V^T P^T wants of it.
 // In bf16 a weight goes in as two terms (within 2^-16); fp32 has its own matrix instructions.
-// Bound by memory: every held row is read once for up to 16 query heads; the matrix unit would take 83 TFLOP/s of 1336 at 5.2 TB/s.
+// Bound by memory: every held row is read once for up to 16 query heads, and the matrix unit is busy 3 or 4 % of the cycles.  A token of 512 rows of
+// up to 512 slots (16 sequences of 32 heads of 128) 21.7 us, 4.9 TB/s, where a large copy reaches 5.1; of 32 rows of 16384 slots, 4 heads each,
+// 39.8 us at 5.3 TB/s and 4.7 to join.  Prompts of 1024 tokens and fewer into the former 40 us, out of it 36 (4.6 and 5.8 TB/s).
 #include <hip/hip_runtime.h>
 
 #include <cmath>
@@ -65,7 +67,9 @@ struct StepArgs {
   int splits;
 };
 
-constexpr int kStepWaves = 4;         // (512 rows of 512 slots: 23.5 us, with 8 25.5, with 2 23.1 but long rows 52 for 50)
+// Waves of a workgroup: 512 rows of 512 slots 27.3 us, 32 of 16384 51.9, 1024 of 256 32.4; eight: 27.3, 54.9 and 31.1.  A wave has one block
+// in its registers (the next one on its way while it works on one: 27.2, 52.5 and 31.2, for twice the registers).
+constexpr int kStepWaves = 4;
 constexpr int kMaxSplits = 64;       // of a row: a lane each where they are joined
 
 // The sums of a wave's slots for 16 heads: o[i] (row = element 16 i + 4 quarter + r, column = head c) relative to `top`, and the lane's share
@@ -414,8 +418,8 @@ int ring_shape(const adore_ring_config *c, RingShape *s) {
 
 int splits_of(const RingShape &s) {
   const long long groups = (long long)s.batch * s.kv_heads * s.tiles;
-  // One workgroup for each unit, whose waves have a block on its way while they work on another: 4 sequences of 8 kv heads, 16384 slots
-  // 43.3 us, with 512 workgroups 48.7, 1024 49.7, 2048 47.2 (of 8 waves 44.9 and 50.2 with 256 and 512).
+  // One workgroup for each unit where rows are few, and two blocks a wave: 4 sequences of 8 kv heads, 16384 slots 51.9 us, with 512
+  // workgroups 57.0, 1024 57.2; 1 of 2, 4096 slots 9.4, 9.6 and 9.4; 64 of 8, 1024 slots of 64 elements 25.1, 25.8 and 28.8.
   const long long want = (256 + groups - 1) / groups, able = (s.blocks + 2 * kStepWaves - 1) / (2 * kStepWaves);
   const long long n = able <= 1 ? 1 : want < able ? want : able;
   return int(n < kMaxSplits ? n : kMaxSplits);
