@@ -399,7 +399,8 @@ int adore_prompt_scores(const adore_prompt_config *cfg, const int32_t *q_start, 
  * adore_prompt_attention and its gradients for queries that see less: the query at position p = i + nk - nq sees keys
  *   j <= p with p - j < window or j < sinks
  * (itself among them; a window that no sequence exceeds is plain causal attention).  Everything else as above, what hidden rows may hold
- * too; tiles that no query of a block sees are not read.  adore_ring_step (below) is the same for single tokens.
+ * too; tiles that no query of a block sees are not read.  adore_ring_step (below) is the same for single tokens; adore_prompt_scores knows no
+ * window (its scores add up with the log-sum-exps of plain attention only).
  * Errors also: E_INVALID (window null or < 1, sinks < 0). */
 typedef struct {
   int32_t window; /* >= 1: keys up to the query's own */

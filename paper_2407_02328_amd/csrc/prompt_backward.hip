@@ -734,20 +734,20 @@ struct SinkPlan {
   int chunk, slots;
   size_t bytes;
 };
-constexpr int32_t kSome = 0;               // (starts that nobody reads: there are some)
 SinkPlan plan_sinks(const PromptShape &s, int head_dim, bool packed) {
   SinkPlan p = {0, 0, 0};
   const long long sinks = s.sinks < s.k_tokens ? s.sinks : s.k_tokens, groups = (sinks + 63) / 64 * 2;
   const long long queries = (long long)s.q_tokens * (packed ? 1 : s.batch);
   if (sinks == 0 || s.k_tokens <= s.window) return p;
-  // It is a launch more, against one workgroup for each kv head that goes over so many more queries than the others (of a sequence twice
-  // as long as the average, where lengths differ).  Not cut / cut, us (sequences x tokens, heads / kv heads, window; 4 first keys):
+  // It is a launch more, against one workgroup for each kv head that goes over so many more queries than the others.  Not cut / cut, us
+  // (sequences x tokens, heads / kv heads, window; 4 first keys):
   //   64 elements    3 x 128, 4 / 4, 32: 17 / 25;  4 x 256, 8 / 8, 32: 20 / 28;  512, 4 / 2, 64: 32 / 35;  2048, 4 / 4, 1000: 52 / 50;
   //                  2 x 2048, 8 / 2, 100: 133 / 60;  60000, 4 / 4, 1000: 2824 / 408
   //   128 elements   8 x 512, 8 / 2, 64: 69 / 76;  32 x 512, 16 / 4, 128: 249 / 232;  4 x 1000, 4 / 1, 200: 102 / 88;  1024, 8 / 2, 128: 93 / 69;
   //                  4096, 8 / 2, 256: 350 / 105;  16384, 8 / 1, 512: 2669 / 390;  8 x 2048, 32 / 8, 508: 873 / 757
-  const long long average = length_of(packed ? &kSome : nullptr, s.batch, s.q_tokens), most = 2 * average < s.q_tokens ? 2 * average : s.q_tokens;
-  if ((most - s.window - 128) * s.group < 1024) return p;
+  // Packed lengths are not known here, and one may be nearly all: 8192 tokens before 60 sequences of 100, 8 / 2 heads, 256: 1851 / 198; 2000
+  // before 40 of 50, 128: 326 / 83; 8 x 512, 64: 73 / 80.
+  if (((long long)s.q_tokens - s.window - 128) * s.group < (packed ? 4096 : 1024)) return p;
   // 256 workgroups, chunks of 128 queries or more (256: 76 us for 69 at 1024 tokens, 109 for 105 at 4096, 748 for 757 at 8 x 2048)
   long long chunk = (queries * s.kv_heads * groups / 2 / 256 + 127) / 128 * 128;
   if (chunk < 128) chunk = 128;
