@@ -300,7 +300,9 @@ hipError_t launch_attend_shared(AttendArgs<T> a, hipStream_t st) {
   const hipError_t e = allow_lds(&prompt_attend_kernel<T, DH, REST, SW, WIN>, lds);
   if (e != hipSuccess) return e;
   const long long blocks = blocks_at_most(a.s.q_start, a.s.batch, a.s.q_tokens, Shared<SW>::kRows) * a.s.heads;
-  a.by_work = blocks < 1024;      // two for each place: beyond, what a sequence's blocks share counts for more (4096: 198 / 229 us)
+  // Up to two for each place: beyond, what a sequence's blocks share counts for more (4096: 198 / 229 us).  With a unit for each the order is
+  // nothing, and finding it 2 us (5 sequences of 17 to 500 tokens 9.8 us / 11.4, gradients 30.2 / 33.2).
+  a.by_work = blocks > 256 && blocks < 1024;
   hipLaunchKernelGGL((prompt_attend_kernel<T, DH, REST, SW, WIN>), dim3(unsigned(blocks)), dim3(256), lds, st, a);
   return hipGetLastError();
 }
@@ -465,7 +467,7 @@ hipError_t launch_scores_shared(ScoreArgs<T> a, hipStream_t st) {
   const hipError_t e = allow_lds(&prompt_scores_kernel<T, DH, SW>, lds);
   if (e != hipSuccess) return e;
   const long long blocks = blocks_at_most(a.s.k_start, a.s.batch, a.s.k_tokens, Shared<SW>::kRows) * a.s.kv_heads;
-  a.by_work = blocks < 1024;      // (as above; 1512: 177 / 197 us)
+  a.by_work = blocks > 256 && blocks < 1024;      // (as above; 1512: 177 / 197 us)
   hipLaunchKernelGGL((prompt_scores_kernel<T, DH, SW>), dim3(unsigned(blocks)), dim3(256), lds, st, a);
   return hipGetLastError();
 }

@@ -691,7 +691,7 @@ hipError_t launch_dq(BackwardArgs<T> a, hipStream_t st) {
   const hipError_t e = allow_lds(&prompt_dq_kernel<T, DH, SW, WIN>, lds);
   if (e != hipSuccess) return e;
   const long long blocks = blocks_at_most(a.s.q_start, a.s.batch, a.s.q_tokens, Shared<SW>::kRows) * a.s.heads;
-  a.by_work = blocks < 1024;
+  a.by_work = blocks > 256 && blocks < 1024;      // (as in prompt_attend.hip)
   hipLaunchKernelGGL((prompt_dq_kernel<T, DH, SW, WIN>), dim3(unsigned(blocks)), dim3(256), lds, st, a);
   return hipGetLastError();
 }
@@ -706,7 +706,7 @@ hipError_t launch_dkv(BackwardArgs<T> a, hipStream_t st) {
   const long long items = MODE == kSinks ? (long long)a.sink_slots * ((sinks + Shared<SW>::kRows - 1) / Shared<SW>::kRows)
                                          : blocks_at_most(a.s.k_start, a.s.batch, a.s.k_tokens, Shared<SW>::kRows);
   const long long blocks = items * a.s.kv_heads;
-  a.by_work = blocks < 2048;   // 1024, with 4 to 64 tiles of 4 heads each: 796 -> 610 us
+  a.by_work = blocks > 256 && blocks < 2048;   // 1024, with 4 to 64 tiles of 4 heads each: 796 -> 610 us
   hipLaunchKernelGGL((prompt_dkv_kernel<T, DH, SW, MODE>), dim3(unsigned(blocks)), dim3(256), lds, st, a);
   return hipGetLastError();
 }
@@ -747,7 +747,7 @@ SinkPlan plan_sinks(const PromptShape &s, int head_dim, bool packed) {
   //                  4096, 8 / 2, 256: 350 / 105;  16384, 8 / 1, 512: 2669 / 390;  8 x 2048, 32 / 8, 508: 873 / 757
   // Packed lengths are not known here, and one may be nearly all: 8192 tokens before 60 sequences of 100, 8 / 2 heads, 256: 1851 / 198; 2000
   // before 40 of 50, 128: 326 / 83; 8 x 512, 64: 73 / 80.
-  if (((long long)s.q_tokens - s.window - 128) * s.group < (packed ? 4096 : 1024)) return p;
+  if (((long long)s.q_tokens - s.window - 128) * s.group < (packed ? 2048 : 1024)) return p;
   // 256 workgroups, chunks of 128 queries or more (256: 76 us for 69 at 1024 tokens, 109 for 105 at 4096, 748 for 757 at 8 x 2048)
   long long chunk = (queries * s.kv_heads * groups / 2 / 256 + 127) / 128 * 128;
   if (chunk < 128) chunk = 128;
