@@ -273,7 +273,7 @@ class _Prompts:
         if code is None or index < 0:
             raise ValueError(f"q: expected a bf16 or fp32 GPU tensor, got {q.device} {q.dtype}")
         self.device, self.index, self.dtype = q.device, index, q.dtype
-        self.q_shape, self.k_shape = qs, ks = q.shape, k.shape
+        self.q_shape, self.k_shape = qs, ks = tuple(q.shape), tuple(k.shape)      # (torch.empty takes a Size half a microsecond longer)
         self.q_odd, self.k_odd = 1 in qs or 0 in qs, 1 in ks or 0 in ks
         self.packed = packed = q_start is not None
         if len(qs) != (3 if packed else 4) or len(ks) != len(qs):
