@@ -123,7 +123,8 @@ struct Lane {
   }
 };
 
-// Cosines and sines of a token's pairs, times the magnitude.
+// Cosines and sines of a token's pairs, times the magnitude (1 and 0 for elements that are not turned, whose lanes do not use them: an infinity times
+// 0 would be another element's NaN).
 __device__ __forceinline__ void angles(const RotateShape &s, int pair, long long token, bool there, float (&cs)[8], float (&sn)[8]) {
   if (pair < 0 || !there) {
 #pragma unroll
@@ -255,7 +256,7 @@ __global__ __launch_bounds__(256) void rotate_heads_kernel(const RotateArgs<T> a
 #pragma unroll
           for (int i = 0; i < 16; ++i) f[i] *= r * (k ? w[1][i] : w[0][i]);
         }
-        rotated(f, cs, sn, SIDE);
+        if (mine.pair >= 0) rotated(f, cs, sn, SIDE);
         if (it.there && h < all) {
           T *row = to(h);
           Eight<T>::store(row + mine.first, f);
@@ -310,7 +311,7 @@ __global__ __launch_bounds__(256) void rotate_backward_kernel(const RotateArgs<T
         float g[16], f[16];
         d[u][0].values(g);
         d[u][1].values(g + 8);
-        rotated(g, cs, sn, SIDE);
+        if (mine.pair >= 0) rotated(g, cs, sn, SIDE);
         x[u][0].values(f);
         x[u][1].values(f + 8);
         float sum = 0.f, dot = 0.f;

@@ -278,6 +278,32 @@ def test_rows_that_are_not_finite_stay_among_themselves():
             assert bool(torch.isfinite(dq[fine]).all()) and not bool(torch.isfinite(got[1][7, 1, 5])) and bool(torch.isfinite(got[1][7, 1, 6]))
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("interleaved", [False, True])
+def test_what_is_not_turned_stays_as_it_is(interleaved, dtype):
+    """Elements behind the turned part come through to the bit, and what is not finite among them reaches no other element."""
+    torch, P = _mods()
+    dt = dtype_of(torch, dtype)
+    for d, R in ((64, 16), (64, 48), (128, 32), (128, 96)):
+        q = draw(torch, (9, 2, d), dt, 1)
+        pos = torch.arange(9, dtype=torch.int32, device=DEV)
+        rotary = P.Rotary(R, interleaved=interleaved, magnitude=1.5)
+        want, _ = P.rotate_heads(q, None, pos, rotary)
+        assert torch.equal(want[..., R:], q[..., R:])
+        back = P.rotate_heads_backward(q, None, q, None, pos, rotary)[0]
+        assert torch.equal(back[..., R:], q[..., R:])
+        for bad in (math.inf, math.nan):
+            for e in (R, d - 1, (R + d) // 2):
+                x = q.clone()
+                x[4, 1, e] = bad
+                got, _ = P.rotate_heads(x, None, pos, rotary)
+                grad = P.rotate_heads_backward(x, None, q, None, pos, rotary)[0]
+                for y, z in ((got, want), (grad, back)):
+                    other = torch.ones_like(y, dtype=torch.bool)
+                    other[4, 1, e] = False
+                    assert torch.equal(y[other], z[other]) and not bool(torch.isfinite(y[4, 1, e]))
+
+
 def test_gradients_against_differences():
     """Central differences in 64 bits of the fp32 outputs: h = 2^-6 leaves h^2 / 6 of the third derivative, and rounding 2^-24 sqrt(n) / h."""
     torch, P = _mods()
