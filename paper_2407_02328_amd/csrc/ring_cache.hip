@@ -13,8 +13,11 @@
 // S^T = K Q^T leaves lane (quarter, c) the weights of head c and exactly those slots that P^T's operand in O^T += V^T P^T wants of it.
 // In bf16 a weight goes in as two terms (within 2^-16); fp32 has its own matrix instructions.
 // Bound by memory: every held row is read once for up to 16 query heads, and the matrix unit is busy 3 or 4 % of the cycles.  A token of 512 rows of
-// up to 512 slots (16 sequences of 32 heads of 128) 21.7 us, 4.9 TB/s, where a large copy reaches 5.1; of 32 rows of 16384 slots, 4 heads each,
-// 39.8 us at 5.3 TB/s and 4.7 to join.  Prompts of 1024 tokens and fewer into the former 40 us, out of it 36 (4.6 and 5.8 TB/s).
+// up to 512 slots (16 sequences of 32 heads of 128) 20.9 us, 5.1 TB/s, which a large copy reaches; of 32 rows of 16384 slots, 4 heads each,
+// 34.6 us at 6.1 TB/s and 4.7 to join.  Prompts of 1024 tokens and fewer into the former 29 us, out of it 38.
+// Blocks, and rows in and out, are read past the caches, which a model's other layers would overwrite before the next token: 32 rows of 16384
+// slots 46.4 us for 51.1, 512 of 512 25.1 for 27.4, in 29 for 40.  (8 rows of 4096, 16 MB, stepped again and again with nothing between, 10.7
+// for 10.1.)
 #include <hip/hip_runtime.h>
 
 #include <cmath>
@@ -67,8 +70,9 @@ struct StepArgs {
   int splits;
 };
 
-// Waves of a workgroup: 512 rows of 512 slots 27.3 us, 32 of 16384 51.9, 1024 of 256 32.4; eight: 27.3, 54.9 and 31.1.  A wave has one block
-// in its registers (the next one on its way while it works on one: 27.2, 52.5 and 31.2, for twice the registers).
+// Waves of a workgroup: 512 rows of 512 slots 25.1 us, 32 of 16384 46.4, 64 of 16384 82.7, 1024 of 256 28.6; eight: 25.3, 49.8, 84.3 and 28.5
+// (128 rows of 1024 in fp32 36.7 and 32.6).  A wave has one block in its registers: the next one on its way while it works on one gained
+// nothing (32 of 16384 with loads through the caches 52.5 for 51.9) for twice the registers.
 constexpr int kStepWaves = 4;
 constexpr int kMaxSplits = 64;       // of a row: a lane each where they are joined
 
@@ -189,9 +193,9 @@ __global__ __launch_bounds__(64 * kStepWaves) void ring_step_kernel(const StepAr
   auto load = [&](int block, u32x4 (&k)[N], u32x4 (&v)[N]) {
     const u32x4 *const p = reinterpret_cast<const u32x4 *>(cache + size_t(block) * (2 * L::kElems)) + lane;
 #pragma unroll
-    for (int i = 0; i < N; ++i) k[i] = p[i * 64];
+    for (int i = 0; i < N; ++i) k[i] = __builtin_nontemporal_load(p + i * 64);
 #pragma unroll
-    for (int i = 0; i < N; ++i) v[i] = p[(N + i) * 64];
+    for (int i = 0; i < N; ++i) v[i] = __builtin_nontemporal_load(p + (N + i) * 64);
   };
   auto take = [&](int block, const u32x4 (&k)[N], u32x4 (&v)[N]) {
     const int left = held - block * kSlots;
@@ -332,8 +336,8 @@ __global__ __launch_bounds__(256) void ring_fill_kernel(const FillArgs<T> a) {
     const int slot = i / kRowChunks, e = i % kRowChunks * EPL, token = token_in(block * kSlots + slot);
     u32x4 k = {0, 0, 0, 0}, v = {0, 0, 0, 0};
     if (token >= 0) {
-      k = *reinterpret_cast<const u32x4 *>(kp + token * a.k.token + e);
-      v = *reinterpret_cast<const u32x4 *>(vp + token * a.v.token + e);
+      k = __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(kp + token * a.k.token + e));
+      v = __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(vp + token * a.v.token + e));
     }
     *reinterpret_cast<u32x4 *>(to + L::k_at(slot, e)) = k;
     *reinterpret_cast<u32x4 *>(&s_v[slot][e]) = v;
@@ -367,7 +371,7 @@ __global__ __launch_bounds__(256) void ring_read_kernel(const ReadArgs<T> a) {
   const T *const from = a.cache + (size_t(row) * a.s.blocks + block) * (2 * L::kElems);
   for (int i = threadIdx.x; i < kSlots / EPL * DH; i += 256) {
     const int e = i % 16 + i / (16 * (kSlots / EPL)) * 16, slot = i / 16 % (kSlots / EPL) * EPL;
-    const u32x4 w = *reinterpret_cast<const u32x4 *>(from + L::kElems + L::v_at(slot, e));
+    const u32x4 w = __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(from + L::kElems + L::v_at(slot, e)));
     T x[EPL];
     *reinterpret_cast<u32x4 *>(x) = w;
 #pragma unroll
@@ -385,7 +389,7 @@ __global__ __launch_bounds__(256) void ring_read_kernel(const ReadArgs<T> a) {
     }
     u32x4 k = {0, 0, 0, 0}, v = {0, 0, 0, 0};
     if (slot < held) {
-      k = *reinterpret_cast<const u32x4 *>(from + L::k_at(in, e));
+      k = __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(from + L::k_at(in, e)));
       v = *reinterpret_cast<const u32x4 *>(&s_v[in][e]);
     }
     const size_t at = (size_t(row) * a.s.slots + place) * DH + e;
@@ -418,8 +422,8 @@ int ring_shape(const adore_ring_config *c, RingShape *s) {
 
 int splits_of(const RingShape &s) {
   const long long groups = (long long)s.batch * s.kv_heads * s.tiles;
-  // One workgroup for each unit where rows are few, and two blocks a wave: 4 sequences of 8 kv heads, 16384 slots 51.9 us, with 512
-  // workgroups 57.0, 1024 57.2; 1 of 2, 4096 slots 9.4, 9.6 and 9.4; 64 of 8, 1024 slots of 64 elements 25.1, 25.8 and 28.8.
+  // One workgroup for each unit where rows are few, and two blocks a wave: 4 sequences of 8 kv heads, 16384 slots 46.3 us, with 512
+  // workgroups 51.8, 1024 51.8; 1 of 2, 4096 slots 9.9, 9.8 and 10.0; 64 of 8, 1024 slots of 64 elements 23.8, 23.8 and 26.3.
   const long long want = (256 + groups - 1) / groups, able = (s.blocks + 2 * kStepWaves - 1) / (2 * kStepWaves);
   const long long n = able <= 1 ? 1 : want < able ? want : able;
   return int(n < kMaxSplits ? n : kMaxSplits);

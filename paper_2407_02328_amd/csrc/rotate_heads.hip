@@ -11,8 +11,9 @@
 //
 // Bound by memory: a row is read once and written once.  A row of DH elements is DH / 16 lanes, 8 elements of each half of the pairs a lane
 // (two loads of 16 bytes in bf16), and a wave takes a run of one token's heads, so that sines are made once for up to eight rows.
-// 14578 tokens of 32 and 32 heads of 128 in bf16 94 us, 5.1 TB/s, which is what a large copy reaches; 29159 of 32 and 8 with norms 106 us (5.6
-// TB/s), their gradients 200 (4.5: two tensors in, one out, and 225 registers that leave two waves a SIMD) and 4.5 for the weights' sums.
+// 14578 tokens of 32 and 32 heads of 128 in bf16 93 us, 5.1 TB/s, which is what a large copy reaches (75 us where the results' memory was written
+// just before and the last level holds it); 29159 of 32 and 8 with norms 109 us (5.5 TB/s), their gradients 192 (4.7: two tensors in, one out,
+// and 225 registers that leave two waves a SIMD) and 4.5 for the weights' sums.
 #include <hip/hip_runtime.h>
 
 #include <cmath>
@@ -41,8 +42,8 @@ struct RotatePlan {
   long long waves;
 };
 
-// Rows of a group whose loads are under way together: two 103.6 us, one 105.5, four 103.6 (16384 tokens of 64 heads of 128); with norms 16384
-// tokens of 40 heads of 64 34.8, 33.1 and 37.2.
+// Rows of a group whose loads are under way together, one / two / four (us): 16384 tokens of 64 heads of 128 106.5 / 103.7 / 99.7, as part of a
+// layer without a difference; 4096 of 40 18.3 / 17.8 / 18.3; with norms 16384 of 40 heads of 64 41.5 / 41.8 / 44.7, 29159 of 128 115 / 114 / 123.
 constexpr int kRowsAtOnce = 2;
 
 template <typename T>
@@ -50,7 +51,10 @@ struct Eight;                                // eight elements, as they are
 template <>
 struct Eight<bf16_t> {
   u32x4 u;
-  __device__ __forceinline__ void load(const bf16_t *p) { u = *reinterpret_cast<const u32x4 *>(p); }
+  // Not kept by the caches, which then hold the results for attention: a projection to 32 and 8 heads of 128, rotation and attention of
+  // 16384 tokens take 382 us instead of 393, of 32768 767 for 780, of 4096 108 either way.  (With norms 393 for 400; alone, where nothing
+  // reads the results, 29159 normed tokens 109 for 101 and their gradients 192 for 200.)
+  __device__ __forceinline__ void load(const bf16_t *p) { u = __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(p)); }
   __device__ __forceinline__ void none() { u = u32x4{0, 0, 0, 0}; }
   __device__ __forceinline__ void values(float *f) const {
 #pragma unroll
@@ -66,6 +70,7 @@ struct Eight<bf16_t> {
 template <>
 struct Eight<float> {
   f32x4 a, b;
+  // In fp32 a lane's two loads share their lines, which have to stay for the second: 115.7 us, not kept 122.7 (14579 tokens of 32 and 8 heads).
   __device__ __forceinline__ void load(const float *p) {
     a = *reinterpret_cast<const f32x4 *>(p);
     b = *reinterpret_cast<const f32x4 *>(p + 4);
@@ -271,7 +276,7 @@ __global__ __launch_bounds__(256) void rotate_heads_kernel(const RotateArgs<T> a
 // rotate_weights_kernel the workgroups: no atomics, equal inputs give equal bits.
 template <typename T, int DH, bool SIDE>
 __global__ __launch_bounds__(256) void rotate_backward_kernel(const RotateArgs<T> a) {
-  constexpr int U = 1, G = DH / 16;          // (rows at once; two: 68.7 us for 61.5, 16384 tokens of 32 and 8 heads of 64)
+  constexpr int U = 1, G = DH / 16;          // (rows at once; two: 76.8 us for 71.4, 16384 tokens of 32 and 8 heads of 64)
   __shared__ float s_sum[4][2][DH];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, all = a.s.heads + a.s.kv_heads;
   const Lane<DH> mine(a.s, lane);
