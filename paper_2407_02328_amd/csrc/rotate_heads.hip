@@ -161,9 +161,22 @@ __device__ __forceinline__ void rotated(float (&f)[16], const float (&cs)[8], co
   }
 }
 
+// The mean of a row's squares, of which a lane has 16 elements; all 64 lanes of a wave call it together.  The mean may be a number where the
+// sum is beyond fp32, or one of the squares: then once more of sixteenths, whose squares add up to at most half the mean.
 template <int DH>
-__device__ __forceinline__ float row_sum(float v) {
-  return group_sum<DH / 16>(v);
+__device__ __forceinline__ float mean_of_squares(const float (&f)[16]) {
+  float sum = 0.f;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) sum = fmaf(f[i], f[i], sum);
+  float mean = group_sum<DH / 16>(sum) * (1.f / DH);
+  if (__builtin_amdgcn_ballot_w64(!(mean < INFINITY))) {
+    sum = 0.f;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) sum = fmaf(f[i] * 0.0625f, f[i] * 0.0625f, sum);
+    sum = group_sum<DH / 16>(sum) * (256.f / DH);
+    if (!(mean < INFINITY)) mean = sum;
+  }
+  return mean;
 }
 
 // A wave's item: a token for each lane, and the heads of the wave's groups of lanes: first + mine, then `step` further on.
@@ -253,11 +266,7 @@ __global__ __launch_bounds__(256) void rotate_heads_kernel(const RotateArgs<T> a
         x[u][0].values(f);
         x[u][1].values(f + 8);
         if constexpr (NORM) {
-          float sum = 0.f;
-#pragma unroll
-          for (int i = 0; i < 16; ++i) sum = fmaf(f[i], f[i], sum);
-          sum = group_sum<DH / 16>(sum);
-          const float r = (k ? a.s.weight[1] : a.s.weight[0]) ? 1.f / sqrtf(sum * (1.f / DH) + a.s.eps) : 1.f;
+          const float mean = mean_of_squares<DH>(f), r = (k ? a.s.weight[1] : a.s.weight[0]) ? 1.f / sqrtf(mean + a.s.eps) : 1.f;
 #pragma unroll
           for (int i = 0; i < 16; ++i) f[i] *= r * (k ? w[1][i] : w[0][i]);
         }
@@ -319,10 +328,8 @@ __global__ __launch_bounds__(256) void rotate_backward_kernel(const RotateArgs<T
         if (mine.pair >= 0) rotated(g, cs, sn, SIDE);
         x[u][0].values(f);
         x[u][1].values(f + 8);
-        float sum = 0.f, dot = 0.f;
-#pragma unroll
-        for (int i = 0; i < 16; ++i) sum = fmaf(f[i], f[i], sum);
-        const float r = 1.f / sqrtf(group_sum<G>(sum) * (1.f / DH) + a.s.eps);
+        float dot = 0.f;
+        const float r = 1.f / sqrtf(mean_of_squares<DH>(f) + a.s.eps);
         const bool some = it.there && h < all, normed = k ? a.s.weight[1] : a.s.weight[0];
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
