@@ -616,7 +616,8 @@ def _sixteen(t):
 class _RotateHeads(torch.autograd.Function):
     @staticmethod
     def forward(ctx, q, k, q_weight, k_weight, positions, rotary, eps):
-        ctx.save_for_backward(q, k, q_weight, k_weight, positions)
+        # (a tensor without weights is not read backwards: kept, it would hold the whole projection)
+        ctx.save_for_backward(None if q_weight is None else q, None if k_weight is None else k, q_weight, k_weight, positions)
         ctx.rest = rotary, eps
         return _rotate(q, k, positions, rotary, q_weight, k_weight, eps)
 
@@ -625,7 +626,7 @@ class _RotateHeads(torch.autograd.Function):
     def backward(ctx, d_q, d_k):
         q, k, q_weight, k_weight, positions = ctx.saved_tensors
         rotary, eps = ctx.rest
-        grads = rotate_heads_backward(_sixteen(d_q), _sixteen(d_k), q, k, positions, rotary, q_weight=q_weight, k_weight=k_weight, eps=eps)
+        grads = _rotate_back(_Heads(d_q, d_k, positions, rotary, q_weight, k_weight, eps), _sixteen(d_q), _sixteen(d_k), q, k, None, None)
         return *(g if want else None for g, want in zip(grads, ctx.needs_input_grad)), None, None, None
 
 
@@ -635,20 +636,26 @@ def rotate_heads_backward(d_q: torch.Tensor, d_k: Optional[torch.Tensor], q: tor
     """adore_rotate_heads_backward on torch's current stream: (dq, dk, dq_weight, dk_weight) of sum(d_q * q_out) + sum(d_k * k_out), None
     for what is not there.  The other arguments as rotate_heads took them; dq and dk are allocated here unless given (the places of q
     and k in the gradient of one projection, say, or d_q and d_k themselves)."""
-    lib = load_library()
     h = _Heads(q, k, positions, rotary, q_weight, k_weight, eps)
     if k is None and d_k is not None:
         raise ValueError("d_k: there is no k")
+    return _rotate_back(h, d_q, d_k, q, k, dq, dk)
+
+
+def _rotate_back(h, d_q, d_k, q, k, dq, dk):
+    """rotate_heads_backward for what h says; q and k may be None where they have no weights."""
+    lib = load_library()
     dq, dq_to = h.result(dq, h.q_shape, "dq")
     dk, dk_to = h.result(dk, h.k_shape, "dk")
-    dqw, dkw = (None if w is None else torch.empty(h.q_shape[-1], dtype=torch.float32, device=h.device) for w in (q_weight, k_weight))
+    dqw, dkw = (None if w is None else torch.empty(h.q_shape[-1], dtype=torch.float32, device=h.device) for w in (h.q_weight, h.k_weight))
     need, space = 0, None
     if dqw is not None or dkw is not None:
         need = lib.adore_rotate_backward_workspace_bytes(ctypes.byref(h.cfg))
         space = torch.empty(max(need, 1), dtype=torch.uint8, device=h.device)
     _call(lib, h.index, lib.adore_rotate_heads_backward, ctypes.byref(h.cfg), *h.angles, h.q_weight, h.k_weight,
-          h.rows(d_q, h.q_shape, "d_q"), None if k is None else h.rows(d_k, h.k_shape, "d_k"), h.rows(q, h.q_shape, "q"),
-          None if k is None else h.rows(k, h.k_shape, "k"), dq_to, dk_to, None if dqw is None else dqw.data_ptr(),
+          h.rows(d_q, h.q_shape, "d_q"), None if h.k_shape is None else h.rows(d_k, h.k_shape, "d_k"),
+          None if q is None else h.rows(q, h.q_shape, "q"), None if k is None else h.rows(k, h.k_shape, "k"), dq_to, dk_to,
+          None if dqw is None else dqw.data_ptr(),
           None if dkw is None else dkw.data_ptr(), None if space is None else space.data_ptr(), need, _stream(h.index))
     return dq, dk, dqw, dkw
 
