@@ -12,6 +12,7 @@ import os
 from typing import Dict, Optional
 
 import torch
+from torch.autograd import forward_ad
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libadore.so")
@@ -248,6 +249,13 @@ _stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda index:
 _current = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
 
 
+def _no_tangents(*tensors):
+    """For calls without forward-mode derivatives: a tensor that has one is refused, whose answer would go on without."""
+    if getattr(forward_ad, "_current_level", 0) >= 0 and any(isinstance(t, torch.Tensor) and forward_ad.unpack_dual(t).tangent is not None
+                                                             for t in tensors):
+        raise ValueError("there are no forward-mode derivatives of this call")
+
+
 def _call(lib, index: int, function, *args):
     """A call of the library whose kernels go to the current device, which has to be that of its tensors."""
     if _current() == index:
@@ -362,7 +370,9 @@ def prompt_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, *, q_sta
     the backward pass takes the same two.  prompt_scores knows no window.
 
     Where q, k or v require gradients, out has them: torch's backward pass is prompt_attention_backward (once; lse and rest have
-    none, and out cannot be given then).  A step that is captured into a graph calls the two itself, under torch.no_grad()."""
+    none, and out cannot be given then).  A step that is captured into a graph calls the two itself, under torch.no_grad().
+    There are no forward-mode derivatives: tensors with a tangent are refused."""
+    _no_tangents(q, k, v)
     if torch.is_grad_enabled() and (q.requires_grad or k.requires_grad or (isinstance(v, torch.Tensor) and v.requires_grad)):
         if out is not None:
             raise ValueError("out: cannot be given where gradients are required (call under torch.no_grad())")
@@ -419,6 +429,7 @@ def prompt_attention_backward(d_out: torch.Tensor, q: torch.Tensor, k: torch.Ten
     """adore_prompt_attention_backward on torch's current stream: (dq, dk, dv) of sum(d_out * out).  out, lse and rest as
     prompt_attention returned them for these q, k, v, starts, scale, window and sinks; dq, dk, dv are allocated here unless given (the places of
     q, k and v in the gradient of one projection, say)."""
+    _no_tangents(d_out, q, k, v, out)
     lib = load_library()
     p = _Prompts(q, k, q_start, k_start, scale)
     def gradient(t, shape, name):
@@ -587,7 +598,9 @@ def rotate_heads(q: torch.Tensor, k: Optional[torch.Tensor], positions: Optional
     dense last dimension (views of one projection).  k may be None; so may rotary, for norms alone.
 
     Where q, k or weights require gradients the results have them (torch's backward pass is rotate_heads_backward, once); q_out and
-    k_out cannot be given then.  A step that is captured into a graph calls the two itself, under torch.no_grad()."""
+    k_out cannot be given then.  A step that is captured into a graph calls the two itself, under torch.no_grad().  There are no
+    forward-mode derivatives: tensors with a tangent are refused."""
+    _no_tangents(q, k, q_weight, k_weight)
     if torch.is_grad_enabled() and (q.requires_grad or (k is not None and k.requires_grad) or
                                     (q_weight is not None and q_weight.requires_grad) or (k_weight is not None and k_weight.requires_grad)):
         if q_out is not None or k_out is not None:
@@ -636,6 +649,7 @@ def rotate_heads_backward(d_q: torch.Tensor, d_k: Optional[torch.Tensor], q: tor
     """adore_rotate_heads_backward on torch's current stream: (dq, dk, dq_weight, dk_weight) of sum(d_q * q_out) + sum(d_k * k_out), None
     for what is not there.  The other arguments as rotate_heads took them; dq and dk are allocated here unless given (the places of q
     and k in the gradient of one projection, say, or d_q and d_k themselves)."""
+    _no_tangents(d_q, d_k, q, k, q_weight, k_weight)
     h = _Heads(q, k, positions, rotary, q_weight, k_weight, eps)
     if k is None and d_k is not None:
         raise ValueError("d_k: there is no k")
@@ -803,6 +817,7 @@ class WindowCache:
         """The prompts' first tokens and those of their last window: k, v [tokens, kv_heads, head_dim] with k_start (int32 [batch + 1]), or
         [batch, kv_heads, tokens, head_dim].  seen (int32 [batch]): how many tokens the sequences have had, where rows in between were left
         out (what read() gave, with new rows behind it)."""
+        _no_tangents(k, v)
         c = self.cfg
         p = _Prompts(k, k, k_start, k_start, None)
         if p.device != self.device or p.dtype != self.dtype or (p.batch, p.cfg.kv_heads, p.cfg.head_dim) != (c.batch, c.kv_heads, c.head_dim):
@@ -815,6 +830,7 @@ class WindowCache:
     def step(self, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, *, out: torch.Tensor = None) -> torch.Tensor:
         """One token of every sequence: q [batch, heads, head_dim], k and v [batch, kv_heads, head_dim], contiguous.  Returns out
         [batch, heads, head_dim]."""
+        _no_tangents(q, k, v)
         mine, rows = self._mine, self._rows
         at = (self._ptr(q, mine, "q"), self._ptr(k, rows, "k"), self._ptr(v, rows, "v"))
         if out is None:
