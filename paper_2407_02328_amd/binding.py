@@ -771,7 +771,8 @@ class WindowCache:
 
       cache   [batch, kv_heads, ceil((window + sinks) / 32), 64 * head_dim]      cursor   int32 [batch, kv_heads]: the next token's position
 
-    One stream at a time: every call works on the same buffers."""
+    One stream at a time: every call works on the same buffers.  There are no gradients: rows that require them are refused unless torch makes
+    none (torch.no_grad())."""
 
     def __init__(self, *, batch: int, heads: int, kv_heads: int, head_dim: int, window: int, sinks: int = 0, dtype, scale: float = None,
                  cache: torch.Tensor = None, cursor: torch.Tensor = None, device="cuda:0"):
@@ -817,7 +818,7 @@ class WindowCache:
         """The prompts' first tokens and those of their last window: k, v [tokens, kv_heads, head_dim] with k_start (int32 [batch + 1]), or
         [batch, kv_heads, tokens, head_dim].  seen (int32 [batch]): how many tokens the sequences have had, where rows in between were left
         out (what read() gave, with new rows behind it)."""
-        _no_tangents(k, v)
+        self._no_gradients(k, v)
         c = self.cfg
         p = _Prompts(k, k, k_start, k_start, None)
         if p.device != self.device or p.dtype != self.dtype or (p.batch, p.cfg.kv_heads, p.cfg.head_dim) != (c.batch, c.kv_heads, c.head_dim):
@@ -830,7 +831,7 @@ class WindowCache:
     def step(self, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, *, out: torch.Tensor = None) -> torch.Tensor:
         """One token of every sequence: q [batch, heads, head_dim], k and v [batch, kv_heads, head_dim], contiguous.  Returns out
         [batch, heads, head_dim]."""
-        _no_tangents(q, k, v)
+        self._no_gradients(q, k, v)
         mine, rows = self._mine, self._rows
         at = (self._ptr(q, mine, "q"), self._ptr(k, rows, "k"), self._ptr(v, rows, "v"))
         if out is None:
@@ -838,6 +839,12 @@ class WindowCache:
         _call(self.lib, self._index, self.lib.adore_ring_step, self._cfg, *at, *self._state, self._ptr(out, mine, "out"), *self._space,
               _stream(self._index))
         return out
+
+    @staticmethod
+    def _no_gradients(*tensors):
+        _no_tangents(*tensors)
+        if torch.is_grad_enabled() and any([isinstance(t, torch.Tensor) and t.requires_grad for t in tensors]):
+            raise ValueError("a ring has no gradients (call under torch.no_grad())")
 
     def _ptr(self, t, shape, name):
         if t.dtype is not self.dtype or t.shape != shape or t.get_device() != self._index or not t.is_contiguous() or t.data_ptr() % 16:
