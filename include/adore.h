@@ -422,8 +422,10 @@ int adore_window_attention_backward(const adore_prompt_config *cfg, const adore_
  *   the first rotary_dim elements of a head are pairs, j < rotary_dim / 2: (j, j + rotary_dim / 2), interleaved != 0: (2 j, 2 j + 1);
  *   with t = 2 pi position turns[j] / 2^64 a pair (a, b) becomes magnitude (a cos t - b sin t), magnitude (a sin t + b cos t);
  *   the other elements stay y.
- * bf16 or fp32 rows, all arithmetic in fp32 (angles in 64-bit fractions of a turn: any int32 position is as exact as a near one, within
- * 2^-33 turns), rounded once.  The mean of squares and eps together have to be a normal fp32 number.
+ * bf16 or fp32 rows, all arithmetic in fp32, rounded once.  Angles are 64-bit fractions of a turn: turns[j] is within 2^-65 turns and 2^-62 of the
+ * frequency (by parts the blend's own roundings besides), an angle within 2^-33 turns and |position| times that.  Where no frequency is more than
+ * a radian (base and factor at least 1) these are less than 3 * 2^-33 turns at any int32 position; a faster one loses more far away.
+ * The mean of squares and eps together have to be a normal fp32 number.
  * turns: adore_rotary_turns makes them (HOST memory, the caller copies them to the device): frequencies f_j = base^(-2 j / rotary_dim) as
  * fractions of a turn.  factor: 1 for frequencies as they are; with original = 0 all are divided by it; with original > 0 those that
  * make at most `low` turns over `original` positions are, those that make at least `high` are not, in between the share that is not

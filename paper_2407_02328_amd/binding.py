@@ -474,7 +474,8 @@ class Rotary:
 
     For longer texts than a model knows: factor with original=None divides all frequencies by it; with `original` positions, those that
     make at most `low` turns over them are divided, those that make at least `high` are not, in between the two are blended.
-    Made once; any int32 position, any device (a copy of `turns` for each: the first call there must not be one that is captured)."""
+    Made once; any int32 position (where base or factor is below 1, the faster frequencies are less exact far away), any device (a copy of
+    `turns` for each: the first call there must not be one that is captured)."""
 
     def __init__(self, rotary_dim: int, *, base: float = 10000.0, interleaved: bool = False, factor: float = 1.0, original: float = None,
                  low: float = 1.0, high: float = 32.0, magnitude: float = 1.0):

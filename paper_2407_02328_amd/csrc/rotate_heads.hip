@@ -6,8 +6,10 @@
 //   g = the same with -t of d_out;  dw = sum over rows of g x r;  dx = r (w g - x r mean(w g x r))
 //
 // Angles are counted in turns, 2^64 of them a whole one: f_j / 2 pi is a 64-bit fraction made once on the host, position times it is one
-// integer product whose overflow is the whole turns that do not matter, so that a far position is as exact as a near one (2^-33 turns)
-// and no table has an end.  The nearest quarter turn off, sine and cosine are their Taylor series up to pi / 4, within 2^-24.
+// integer product whose overflow is the whole turns that do not matter, and no table has an end.  The product is rounded to 2^-32 turns; the
+// fraction's own error, 2^-65 turns and 2^-62 of the frequency, grows with the position: with frequencies of up to a radian less than 2^-32 turns
+// at 2^31.  The nearest quarter turn off, sine and cosine are their Taylor series up to pi / 4, within 2^-24, with their argument's two roundings
+// within 1.6 of it.
 //
 // Bound by memory: a row is read once and written once.  A row of DH elements is DH / 16 lanes, 8 elements of each half of the pairs a lane
 // (two loads of 16 bytes in bf16), and a wave takes a run of one token's heads, so that sines are made once for up to eight rows.
