@@ -10,7 +10,8 @@ LIB = os.path.join(PKG, "libadore.so")
 SOURCES = ["adore_api.hip", "attend.hip", "controller.hip", "select.hip", "rebuild.hip", "forward_attend.hip", "rope.hip", "topk_attend.hip", "h2o.hip",
            "prompt_attend.hip", "prompt_backward.hip", "q4_cache.hip", "rotate_heads.hip",
            "ring_cache.hip"]
-HEADERS = ["adore_internal.h", "device_utils.h", "select_device.h", "ctrl_device.h", "prompt_device.h"]
+HEADERS = ["adore_internal.h", "device_utils.h", "select_device.h", "ctrl_device.h", "prompt_device.h",
+           "prompt_chunks.h"]
 
 HIPCC_FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared",

@@ -332,21 +332,7 @@ __global__ __launch_bounds__(256) ADORE_WAVES(sizeof(T) == 4 || SW > 1 ? 1 : DH 
 template <typename T, int DH, int SW>
 constexpr bool kValuesInRegisters = SW > 1 && DH * sizeof(T) == 512;
 
-// With a window a block of keys is seen by few queries, but the first keys by all that follow: one workgroup would go over a whole prompt
-// while the others go over a window.  So the queries behind the window (p - j >= window) are cut into chunks, each a workgroup's, whose
-// sums for 32 first keys (a wave's registers, fp32) go to memory; the workgroup of the block that holds the keys adds them to its own.
-// A sequence's chunks: n places from `first` on.  find_chunk: a place's sequence and first query (all 64 lanes of a wave call it together).
-struct Chunks {
-  int first, n;
-  int from;                                  // the first query that is as far as the window from key 0
-  __device__ __forceinline__ Chunks(const PromptShape &a, const Sequence &s, int chunk) {
-    from = max(a.window - (s.nk - s.nq), 0);
-    n = s.nq > from ? (s.nq - from + chunk - 1) / chunk : 0;
-    // packed: of the sequences that have chunks no two are in the same run of window + 1 keys (whatever the starts hold: no place is
-    // beyond SinkPlan::slots)
-    first = a.q_start ? s.q_first / chunk + min(s.b, s.k_first / (a.window + 1)) : s.b * ((a.q_tokens + chunk - 1) / chunk);
-  }
-};
+// A place's sequence and first query (Chunks); all 64 lanes of a wave call it together.
 __device__ __forceinline__ bool find_chunk(const PromptShape &a, int place, int chunk, Sequence &s, int &query) {
   const int lane = threadIdx.x & 63;
   for (int b0 = 0; b0 < a.batch; b0 += 64) {
@@ -361,11 +347,6 @@ __device__ __forceinline__ bool find_chunk(const PromptShape &a, int place, int 
     }
   }
   return false;
-}
-// The sums of place `place`, kv head hk, for keys 32 i .. 32 i + 31: dk's registers of 64 lanes, then dv's.
-template <int DH>
-__device__ __forceinline__ size_t sink_sums(const PromptShape &a, int place, int hk, int i) {
-  return ((size_t(place) * a.kv_heads + hk) * ((min(a.sinks, a.k_tokens) + 63) / 64 * 2) + i) * (64 * DH);
 }
 
 enum { kCausal, kWindow, kSinks };           // every pair; pairs in the window; the others, which the first keys have
@@ -727,39 +708,6 @@ hipError_t launch_backward(const BackwardArgs<T> &a, hipStream_t st) {
 size_t delta_bytes(const adore_prompt_config &c, bool packed) {
   const size_t n = size_t(c.heads) * c.q_tokens * (packed ? 1 : c.batch);
   return (n * sizeof(float) + 255) / 256 * 256 + 256;    // never 0: that says "not taken"
-}
-
-// How the queries behind the window of the first keys are cut (slots 0: not at all, the workgroup of a block of keys goes over them).
-struct SinkPlan {
-  int chunk, slots;
-  size_t bytes;
-};
-SinkPlan plan_sinks(const PromptShape &s, int head_dim, bool packed) {
-  SinkPlan p = {0, 0, 0};
-  const long long sinks = s.sinks < s.k_tokens ? s.sinks : s.k_tokens, groups = (sinks + 63) / 64 * 2;
-  const long long queries = (long long)s.q_tokens * (packed ? 1 : s.batch);
-  if (sinks == 0 || s.k_tokens <= s.window) return p;
-  // It is a launch more, against one workgroup for each kv head that goes over so many more queries than the others.  Not cut / cut, us
-  // (sequences x tokens, heads / kv heads, window; 4 first keys):
-  //   64 elements    3 x 128, 4 / 4, 32: 17 / 25;  4 x 256, 8 / 8, 32: 20 / 28;  512, 4 / 2, 64: 32 / 35;  2048, 4 / 4, 1000: 52 / 50;
-  //                  2 x 2048, 8 / 2, 100: 133 / 60;  60000, 4 / 4, 1000: 2824 / 408
-  //   128 elements   8 x 512, 8 / 2, 64: 69 / 76;  32 x 512, 16 / 4, 128: 249 / 232;  4 x 1000, 4 / 1, 200: 102 / 88;  1024, 8 / 2, 128: 93 / 69;
-  //                  4096, 8 / 2, 256: 350 / 105;  16384, 8 / 1, 512: 2669 / 390;  8 x 2048, 32 / 8, 508: 873 / 757
-  // Packed lengths are not known here, and one may be nearly all: 8192 tokens before 60 sequences of 100, 8 / 2 heads, 256: 1851 / 198; 2000
-  // before 40 of 50, 128: 326 / 83; 8 x 512, 64: 73 / 80.
-  if (((long long)s.q_tokens - s.window - 128) * s.group < (packed ? 2048 : 1024)) return p;
-  // 256 workgroups, chunks of 128 queries or more (256: 76 us for 69 at 1024 tokens, 109 for 105 at 4096, 748 for 757 at 8 x 2048)
-  long long chunk = (queries * s.kv_heads * groups / 2 / 256 + 127) / 128 * 128;
-  if (chunk < 128) chunk = 128;
-  if (chunk > s.q_tokens) chunk = (s.q_tokens + 127) / 128 * 128;
-  const long long long_ones = (long long)s.k_tokens / (s.window + 1);
-  const long long slots = packed ? s.q_tokens / chunk + (s.batch < long_ones ? s.batch : long_ones) + 1 : s.batch * ((s.q_tokens + chunk - 1) / chunk);
-  const long long bytes = slots * s.kv_heads * groups * 64 * head_dim * 4;
-  if (bytes > (256ll << 20)) return p;       // (many short sequences: there is little to cut)
-  p.chunk = int(chunk);
-  p.slots = int(slots);
-  p.bytes = size_t(bytes);
-  return p;
 }
 
 template <typename T, bool WIN>

@@ -12,6 +12,7 @@
 
 #include "adore.h"
 #include "device_utils.h"
+#include "prompt_chunks.h"
 
 namespace adore {
 
@@ -39,43 +40,9 @@ inline Rows<T> rows_of(const adore_rows *r) {
   return Rows<T>{static_cast<T *>(r->data), r->seq, r->token, r->head};
 }
 
-// A problem's sequences and heads.
-struct PromptShape {
-  const int32_t *q_start, *k_start;   // [batch + 1], or null: every sequence has q_tokens / k_tokens
-  int batch, heads, kv_heads, group, q_tokens, k_tokens;
-  float scale, scale_log2;            // and times log2(e)
-  int window, sinks;                  // of kernels with a window: a query sees its last `window` keys and the first `sinks`
-};
-
 int prompt_shape(const adore_prompt_config *c, const int32_t *q_start, const int32_t *k_start, PromptShape *s);
 bool prompt_rows_ok(const adore_rows *r, int dtype);
 int window_shape(const adore_window *w, PromptShape *s);
-
-struct Sequence {
-  int b;
-  int q_first, k_first;   // first rows in packed tensors (0 in dense ones)
-  int nq, nk;
-};
-
-// Starts are the caller's device memory: whatever they hold, rows stay within the packed tensors.
-__device__ __forceinline__ void span(const int32_t *start, int b, int total, int &first, int &n) {
-  const int s = min(max(start[b], 0), total), e = min(max(start[b + 1], 0), total);
-  first = s;
-  n = max(e - s, 0);
-}
-
-__device__ __forceinline__ Sequence sequence_at(const PromptShape &a, int b) {
-  Sequence s;
-  s.b = b;
-  s.q_first = s.k_first = 0;
-  s.nq = a.q_tokens;
-  s.nk = a.k_tokens;
-  if (a.q_start) {
-    span(a.q_start, b, a.q_tokens, s.q_first, s.nq);
-    span(a.k_start, b, a.k_tokens, s.k_first, s.nk);
-  }
-  return s;
-}
 
 // Blocks of `rows` rows that sequences have together, at most (a grid does not know the starts), and the rows that belong to none.
 inline long long blocks_at_most(const int32_t *start, int batch, int tokens, int rows) {
