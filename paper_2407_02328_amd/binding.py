@@ -251,9 +251,11 @@ _current = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_devi
 
 def _no_tangents(*tensors):
     """For calls without forward-mode derivatives: a tensor that has one is refused, whose answer would go on without."""
-    if getattr(forward_ad, "_current_level", 0) >= 0 and any(isinstance(t, torch.Tensor) and forward_ad.unpack_dual(t).tangent is not None
-                                                             for t in tensors):
-        raise ValueError("there are no forward-mode derivatives of this call")
+    # (an attribute of torch's own tells first whether there may be any: 0.2 us a call)
+    if getattr(forward_ad, "_current_level", 0) >= 0:
+        for t in tensors:
+            if isinstance(t, torch.Tensor) and forward_ad.unpack_dual(t).tangent is not None:
+                raise ValueError("there are no forward-mode derivatives of this call")
 
 
 def _call(lib, index: int, function, *args):
@@ -819,7 +821,9 @@ class WindowCache:
         """The prompts' first tokens and those of their last window: k, v [tokens, kv_heads, head_dim] with k_start (int32 [batch + 1]), or
         [batch, kv_heads, tokens, head_dim].  seen (int32 [batch]): how many tokens the sequences have had, where rows in between were left
         out (what read() gave, with new rows behind it)."""
-        self._no_gradients(k, v)
+        _no_tangents(k, v)
+        if torch.is_grad_enabled() and (k.requires_grad or (isinstance(v, torch.Tensor) and v.requires_grad)):
+            raise ValueError("k, v: a ring has no gradients (call under torch.no_grad())")
         c = self.cfg
         p = _Prompts(k, k, k_start, k_start, None)
         if p.device != self.device or p.dtype != self.dtype or (p.batch, p.cfg.kv_heads, p.cfg.head_dim) != (c.batch, c.kv_heads, c.head_dim):
@@ -832,7 +836,9 @@ class WindowCache:
     def step(self, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, *, out: torch.Tensor = None) -> torch.Tensor:
         """One token of every sequence: q [batch, heads, head_dim], k and v [batch, kv_heads, head_dim], contiguous.  Returns out
         [batch, heads, head_dim]."""
-        self._no_gradients(q, k, v)
+        _no_tangents(q, k, v)
+        if torch.is_grad_enabled() and (q.requires_grad or k.requires_grad or v.requires_grad):
+            raise ValueError("q, k, v: a ring has no gradients (call under torch.no_grad())")
         mine, rows = self._mine, self._rows
         at = (self._ptr(q, mine, "q"), self._ptr(k, rows, "k"), self._ptr(v, rows, "v"))
         if out is None:
@@ -840,12 +846,6 @@ class WindowCache:
         _call(self.lib, self._index, self.lib.adore_ring_step, self._cfg, *at, *self._state, self._ptr(out, mine, "out"), *self._space,
               _stream(self._index))
         return out
-
-    @staticmethod
-    def _no_gradients(*tensors):
-        _no_tangents(*tensors)
-        if torch.is_grad_enabled() and any([isinstance(t, torch.Tensor) and t.requires_grad for t in tensors]):
-            raise ValueError("a ring has no gradients (call under torch.no_grad())")
 
     def _ptr(self, t, shape, name):
         if t.dtype is not self.dtype or t.shape != shape or t.get_device() != self._index or not t.is_contiguous() or t.data_ptr() % 16:
