@@ -2,8 +2,8 @@
 
   train   q, k and v as views of one projection; rotate_heads norms and rotates q and k, prompt_attention with a window and first tokens
           that stay visible, torch's autograd through both
-  serve   the prompts once through the same, their rows into a WindowCache, then a token at a time: rotated by the cache's own count,
-          through WindowCache.step, captured once and replayed
+  serve   the prompts' keys and values, projected and rotated at once, into a WindowCache, then a token at a time: rotated by the cache's
+          own count, through WindowCache.step, captured once and replayed
 
     python -m examples.window_layer [--prompts 1024,700,333,1] [--window 252] [--sinks 4] [--tokens 64]
 """
@@ -71,9 +71,8 @@ def train(layer: Layer, x, target, start, positions, steps: int, rate: float):
 @torch.no_grad()
 def serve(layer: Layer, x, start, positions, following):
     """The prompts into a ring, then `following` [tokens, batch, hidden] through it; the cache, and the attention's output per token
-    [tokens, batch, heads, head_dim]."""
-    q, k, v = layer.project(x, positions)
-    layer.attend(q, k, v, start)
+    [tokens, batch, heads, head_dim].  (What the prompts' own tokens answer, layer.attend of the same rows, is not asked for here.)"""
+    _, k, v = layer.project(x, positions)
     batch = following.shape[1]
     cache = WindowCache(batch=batch, heads=layer.heads, kv_heads=layer.kv_heads, head_dim=layer.head_dim, window=layer.window, sinks=layer.sinks,
                         dtype=x.dtype)
