@@ -12,12 +12,14 @@
 //          V [DH / 16][t][quarter][c][4]:        element 16 i + c, slot 16 t + 4 quarter + e
 // S^T = K Q^T leaves lane (quarter, c) the weights of head c and exactly those slots that P^T's operand in O^T += V^T P^T wants of it.
 // In bf16 a weight goes in as two terms (within 2^-16); fp32 has its own matrix instructions.
-// Bound by memory: every held row is read once for up to 16 query heads, and the matrix unit is busy 3 or 4 % of the cycles.  A token of 512 rows of
+// Bound by memory: every held row is read once for each 16 query heads, and the matrix unit is busy 3 or 4 % of the cycles.  A token of 512 rows of
 // up to 512 slots (16 sequences of 32 heads of 128) 20.9 us, 5.1 TB/s, which a large copy reaches; of 32 rows of 16384 slots, 4 heads each,
 // 34.6 us at 6.1 TB/s and 4.7 to join.  Prompts of 1024 tokens and fewer into the former 29 us, out of it 38.
 // Blocks, and rows in and out, are read past the caches, which a model's other layers would overwrite before the next token: 32 rows of 16384
 // slots 46.4 us for 51.1, 512 of 512 25.1 for 27.4, in 29 for 40.  (8 rows of 4096, 16 MB, stepped again and again with nothing between, 10.7
-// for 10.1.)
+// for 10.1.)  Where a kv head has more than 16 query heads its rows are read more than once, past the caches too: 8 sequences of 64 heads over 2
+// and 16384 slots (three caches in turn) 31.9 us, through the caches 33.4; 16 of 48 over 1 and 4096 slots (six caches, which the last level holds
+// together) 27.8, through the caches 23.8.
 #include <hip/hip_runtime.h>
 
 #include <cmath>
@@ -70,11 +72,13 @@ struct StepArgs {
   int splits;
 };
 
-// Waves of a workgroup: 512 rows of 512 slots 25.1 us, 32 of 16384 46.4, 64 of 16384 82.7, 1024 of 256 28.6; eight: 25.3, 49.8, 84.3 and 28.5
-// (128 rows of 1024 in fp32 36.7 and 32.6).  A wave has one block in its registers: the next one on its way while it works on one gained
-// nothing (32 of 16384 with loads through the caches 52.5 for 51.9) for twice the registers.
+// Waves of a workgroup: 512 rows of 512 slots 25.1 us, 32 of 16384 46.4, 64 of 16384 82.7, 1024 of 256 28.6; eight: 25.3, 49.8, 84.3 and 28.5.
+// In fp32 rows of four heads of 128 elements (two to three caches in turn), 128 of 1024 36.5 / 32.3, 32 of 16384 116 / 95, 2 of 4096 19.6 / 23.9; of one
+// head 512 of 512 51.0 / 57.0, 1024 of 256 55.6 / 65.4: neither number is best for all.
+// A wave has one block in its registers: the next one on its way while it works on one gained nothing (32 of 16384 with loads through the caches
+// 52.5 for 51.9) for twice the registers.
 constexpr int kStepWaves = 4;
-constexpr int kMaxSplits = 64;       // of a row: a lane each where they are joined
+constexpr int kMaxSplits = 64;       // of a row: a lane each where they are joined (splits_of says what that costs)
 
 // The sums of a wave's slots for 16 heads: o[i] (row = element 16 i + 4 quarter + r, column = head c) relative to `top`, and the lane's share
 // of the sum of weights.
@@ -424,6 +428,8 @@ int splits_of(const RingShape &s) {
   const long long groups = (long long)s.batch * s.kv_heads * s.tiles;
   // One workgroup for each unit where rows are few, and two blocks a wave: 4 sequences of 8 kv heads, 16384 slots 46.3 us, with 512
   // workgroups 51.8, 1024 51.8; 1 of 2, 4096 slots 9.9, 9.8 and 10.0; 64 of 8, 1024 slots of 64 elements 23.8, 23.8 and 26.3.
+  // A row has kMaxSplits at most, so that fewer than four rows of more than 16384 slots leave units without work: one row of 2^16 slots 23 us
+  // (1.5 TB/s), one of 2^20 182 (3.0), two of 2^19 110 (4.9).
   const long long want = (256 + groups - 1) / groups, able = (s.blocks + 2 * kStepWaves - 1) / (2 * kStepWaves);
   const long long n = able <= 1 ? 1 : want < able ? want : able;
   return int(n < kMaxSplits ? n : kMaxSplits);

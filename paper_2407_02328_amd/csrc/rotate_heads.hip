@@ -14,8 +14,8 @@
 // Bound by memory: a row is read once and written once.  A row of DH elements is DH / 16 lanes, 8 elements of each half of the pairs a lane
 // (two loads of 16 bytes in bf16), and a wave takes a run of one token's heads, so that sines are made once for up to eight rows.
 // 14578 tokens of 32 and 32 heads of 128 in bf16 93 us, 5.1 TB/s, which is what a large copy reaches (75 us where the results' memory was written
-// just before and the last level holds it); 29159 of 32 and 8 with norms 109 us (5.5 TB/s), their gradients 192 (4.7: two tensors in, one out,
-// and 225 registers that leave two waves a SIMD) and 4.5 for the weights' sums.
+// just before and the last level holds it); 29159 of 32 and 8 with norms 109 us (5.5 TB/s), their gradients 195 (4.6: two tensors in, one out,
+// vector instructions in 68 % of the cycles) and 4.5 for the weights' sums; 14579 of 32 and 8 with norms in fp32 137 us (4.4 TB/s), their gradients 210 (4.3).
 #include <hip/hip_runtime.h>
 
 #include <cmath>
@@ -55,7 +55,9 @@ struct Eight<bf16_t> {
   u32x4 u;
   // Not kept by the caches, which then hold the results for attention: a projection to 32 and 8 heads of 128, rotation and attention of
   // 16384 tokens take 382 us instead of 393, of 32768 767 for 780, of 4096 108 either way.  (With norms 393 for 400; alone, where nothing
-  // reads the results, 29159 normed tokens 109 for 101 and their gradients 192 for 200.)
+  // reads the results, 29159 normed tokens 109 for 101 and their gradients 192 for 200.)  Also where pairs lie side by side or a part of the head
+  // is turned, whose lanes' two loads share a line: 16384 tokens of 32 and 8 heads of 128, behind something that has filled the caches, side by
+  // side 76.5 us for 89.0, 64 elements turned 75.4 for 88.6; with a projection and attention with a window around them 905 for 900 and 898 for 893.
   __device__ __forceinline__ void load(const bf16_t *p) { u = __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(p)); }
   __device__ __forceinline__ void none() { u = u32x4{0, 0, 0, 0}; }
   __device__ __forceinline__ void values(float *f) const {
@@ -72,7 +74,7 @@ struct Eight<bf16_t> {
 template <>
 struct Eight<float> {
   f32x4 a, b;
-  // In fp32 a lane's two loads share their lines, which have to stay for the second: 115.7 us, not kept 122.7 (14579 tokens of 32 and 8 heads).
+  // In fp32 past the caches loses: 115.7 us, so read 122.7 (14579 tokens of 32 and 8 heads).
   __device__ __forceinline__ void load(const float *p) {
     a = *reinterpret_cast<const f32x4 *>(p);
     b = *reinterpret_cast<const f32x4 *>(p + 4);
@@ -419,7 +421,7 @@ __global__ __launch_bounds__(256) void rotate_weights_kernel(const float *part, 
 }
 
 // ---- host ----------------------------------------------------------------------------------------------------------------
-constexpr long long kMostParts = 512;        // workgroups whose sums of the weights' gradients are added up: as many as have a place
+constexpr long long kMostParts = 512;        // workgroups whose sums of the weights' gradients are added up: two a unit (a third would have a place)
 
 int rotate_shape(const adore_rotate_config *c, RotateShape *s) {
   if (!c || c->batch <= 0 || c->heads <= 0 || c->kv_heads < 0 || c->tokens < 0 || (c->dtype != ADORE_F32 && c->dtype != ADORE_BF16) ||
